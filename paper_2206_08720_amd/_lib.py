@@ -37,6 +37,11 @@ EXPORTED_SYMBOLS = ("ntk_init", "ntk_compute", "ntk_free", "ntk_last_error", "nt
                     "ntk_set_stream", "ntk_workspace_bytes", "ntk_profile_enable",
                     "ntk_profile_read", "ntk_device_info", "ntk_mfma_peak",
                     "ntk_vector_product", "ntk_compute_static")
+# include/ntk_seq.h
+NTK_F32, NTK_BF16, NTK_F16 = 0, 1, 2
+NTK_ROTARY_PLAIN, NTK_ROTARY_LINEAR, NTK_ROTARY_BASE, NTK_ROTARY_RAMP = 0, 1, 2, 3
+EXPORTED_SEQ_SYMBOLS = ("ntk_rms_norm", "ntk_rms_norm_workspace", "ntk_rms_norm_bwd", "ntk_rotary_table", "ntk_rotary",
+                        "ntk_attention_workspace", "ntk_attention", "ntk_attention_bwd")
 STATIC_SCRATCH_BYTES = 64 * 1024 * 1024   # NTK_STATIC_SCRATCH_BYTES
 
 
@@ -49,6 +54,22 @@ class ntk_model_desc(ctypes.Structure):
     _fields_ = [("n_layers", ctypes.c_int), ("layers", ctypes.POINTER(ntk_layer_desc)),
                 ("in_h", ctypes.c_int), ("in_w", ctypes.c_int), ("in_c", ctypes.c_int),
                 ("out_dim", ctypes.c_int)]
+
+
+class ntk_view(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("stride_batch", ctypes.c_longlong), ("stride_position", ctypes.c_longlong),
+                ("stride_head", ctypes.c_longlong)]
+
+
+class ntk_rotary_scaling(ctypes.Structure):
+    _fields_ = [("kind", ctypes.c_int), ("factor", ctypes.c_double), ("original", ctypes.c_double), ("low", ctypes.c_double),
+                ("high", ctypes.c_double)]
+
+
+class ntk_attention_desc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int) for n in ("dtype", "batch", "q_len", "k_len", "heads", "kv_heads", "head_dim", "causal")] + [
+        ("scale", ctypes.c_float), ("softcap", ctypes.c_float), ("k_lens", ctypes.c_void_p), ("prefix", ctypes.c_void_p),
+        ("docs", ctypes.c_void_p), ("slopes", ctypes.c_void_p)]
 
 
 class NTKError(RuntimeError):
@@ -100,6 +121,19 @@ def load():
     lib.ntk_device_info.restype = ctypes.c_int
     lib.ntk_mfma_peak.argtypes = [ctypes.c_int, ctypes.POINTER(ctypes.c_double)]
     lib.ntk_mfma_peak.restype = ctypes.c_int
+    I, L, F = ctypes.c_int, ctypes.c_longlong, ctypes.c_float
+    V, D = ctypes.POINTER(ntk_view), ctypes.POINTER(ntk_attention_desc)
+    for name, args, res in (
+            ("ntk_rms_norm", [I, I, L, I, P, L, P, L, P, F, P, P, P, P], I),
+            ("ntk_rms_norm_workspace", [L, I], L),
+            ("ntk_rms_norm_bwd", [I, I, L, I, P, L, P, L, P, P, L, F, P, P, P, L, P], I),
+            ("ntk_rotary_table", [I, I, ctypes.c_double, ctypes.POINTER(ntk_rotary_scaling), P, P], I),
+            ("ntk_rotary", [I] * 9 + [V, V, P, I, P, I, V, V, P], I),
+            ("ntk_attention_workspace", [D, I], L),
+            ("ntk_attention", [D, V, V, V, V, P, P, L, P], I),
+            ("ntk_attention_bwd", [D, V, V, V, V, V, P, V, V, V, P, L, P], I)):
+        f = getattr(lib, name)
+        f.argtypes, f.restype = args, res
     _lib = lib
     return lib
 

@@ -1,0 +1,440 @@
+// attn_core.hpp -- the pieces the attention kernels are made of (kernels_attn.hip, kernels_attn_bwd.hip).
+//
+// The queries of one batch entry that share a key/value head are the rows of one matrix: row
+// r = i * group + g is query i of the head's g-th query head.  Products run on 32x32 MFMA tiles whose
+// columns are the rows owned by a lane's query (forward, dq) or key (dk, dv) and stay with that lane:
+//
+//   D = A B:  lane l holds D[8 (v / 4) + 4 (l / 32) + v % 4][l % 32] in register v,
+//   A, B:     lane l holds the 8 elements k = kmap(l / 32, i) of row (column) l % 32.
+//
+// Any order of k gives the same product as long as A and B agree, so the 16 values that a lane
+// holds of two groups of 16 rows of D are, converted, the B operand of the next product over those rows with
+// kmap(h, i) = 8 (i / 4) + 4 h + i % 4: the probabilities go from the score product into the
+// value product inside the registers, with no shuffle and no trip through LDS.  Softmax statistics
+// are one number a lane (two lanes share a column; they meet in one half-wave swap).
+//
+// fp32 runs through the same code: one step of 16 k is eight 32x32x2 fp32 MFMAs, the i-th of which
+// takes the i-th element of both operands.
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "gemm_core.hpp"
+#include "index_math.hpp"
+
+namespace ntk {
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
+typedef float f32x8 __attribute__((ext_vector_type(8)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+
+constexpr float kLog2e = 1.44269504088896340736f;
+constexpr float kLn2 = 0.69314718055994530942f;
+
+template <class T>
+struct Num;
+template <>
+struct Num<__bf16> {
+  using Frag = bf16x8;
+  using Four = bf16x4;
+  __device__ static __forceinline__ f32x16 mma(Frag a, Frag b, f32x16 c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+  }
+};
+template <>
+struct Num<_Float16> {
+  using Frag = f16x8;
+  using Four = f16x4;
+  __device__ static __forceinline__ f32x16 mma(Frag a, Frag b, f32x16 c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
+  }
+};
+template <>
+struct Num<float> {
+  using Frag = f32x8;
+  using Four = f32x4;
+  __device__ static __forceinline__ f32x16 mma(Frag a, Frag b, f32x16 c) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a[i], b[i], c, 0, 0, 0);
+    return c;
+  }
+};
+
+// A [batch, position, head, dim] array: dim contiguous, strides in elements.
+struct AttnView {
+  void* p;
+  long long sb, ss, sh;
+};
+
+struct AttnArgs {
+  AttnView q, k, v, o;             // backward: o is read
+  AttnView dout, dq, dk, dv;       // backward
+  float* lse;                      // [batch, heads, q_len]; may be null in the forward pass
+  const float* delta;              // backward: [batch, heads, q_len]
+  const int* lens;                 // [batch] or null
+  const int* prefix;               // [batch] or null
+  const int* docs;                 // [batch, k_len] or null
+  const float* slopes;             // [heads] or null
+  float* part;                     // partial results of key (row) ranges
+  int B, Sq, Sk, H, Hk, G, D;
+  int R;                           // Sq * G rows a key/value head
+  int tiles, splits;               // row (key) tiles a head, ranges the other axis is cut into
+  int causal;
+  float scale;                     // of the raw product
+  float c;                         // scale * log2(e)
+  float cap_in, cap_out;           // softcap > 0: 2 log2(e) scale / cap and cap log2(e); else 0
+  FastDiv gdiv;
+};
+
+// What a batch entry's queries see: query i stands at position off + i, the keys are 0 .. len - 1, and
+// a query at position p sees the keys below klim(p).
+struct AttnScope {
+  int len, off, prefix, causal;
+  __device__ __forceinline__ AttnScope(const AttnArgs& a, int b) {
+    len = a.lens ? min(max(a.lens[b], 0), a.Sk) : a.Sk;
+    off = len - a.Sq;
+    prefix = a.prefix ? min(max(a.prefix[b], 0), len) : 0;
+    causal = a.causal;
+  }
+  __device__ __forceinline__ int klim(int pos) const {
+    if (pos < 0) return 0;
+    return causal ? min(max(pos + 1, prefix), len) : len;
+  }
+};
+
+// ---- tiles in LDS ------------------------------------------------------------------------------
+// [rows][DP], unpadded; the 16-byte chunk c of row r sits at position c ^ swz(r).  swz is a bijection of
+// the rows that a ds_read_b128 phase of 16 lanes reads at one c, and keeps the four rows of a
+// transposed read (chunks c .. c + 3) in distinct banks; it depends on r % 16 only, and
+// swz(r + 8) = swz(r) ^ 2 for r % 16 < 8, so every address is one of a few lane constants plus an immediate.
+template <class T, int DP>
+struct AttnTile {
+  static constexpr int E = (int)sizeof(T);
+  static constexpr int RB = DP * E;            // bytes a row
+  static constexpr int CH = RB / 16;           // chunks a row
+  static constexpr int EC = 16 / E;            // elements a chunk
+  using Frag = typename Num<T>::Frag;
+  __device__ static __forceinline__ int swz(int r) {
+    if constexpr (CH >= 16) return ((r & 3) << 2) | ((r >> 2) & 3);
+    const int s = (r >> 1) & 7;
+    return ((s & 1) << 2) | (s >> 1);
+  }
+  __device__ static __forceinline__ int at(int r, int c) { return r * RB + ((c ^ swz(r)) << 4); }
+
+  // rows as the outer axis: elements 16 t + 8 h .. + 7 of row `row` (+ lane % 32)
+  __device__ static __forceinline__ Frag rows(const char* s, int row, int t, int lane) {
+    const int r = row + (lane & 31), h = lane >> 5;
+    if constexpr (E == 2) {
+      return *reinterpret_cast<const Frag*>(s + at(r, 2 * t + h));
+    } else {
+      const f32x4 lo = *reinterpret_cast<const f32x4*>(s + at(r, 4 * t + 2 * h));
+      const f32x4 hi = *reinterpret_cast<const f32x4*>(s + at(r, 4 * t + 2 * h + 1));
+      return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+    }
+  }
+  // the transpose: column 32 db + lane % 32 at the rows row + 8 (i / 4) + 4 h + i % 4
+  __device__ static __forceinline__ Frag cols(const char* s, int row, int db, int lane) {
+    const int h = lane >> 5;
+    if constexpr (E == 2) {
+      const int j = lane & 15, g = (lane >> 4) & 1;
+      const int r = row + 4 * h + (j >> 2);
+      const int c = 4 * db + 2 * g + ((j >> 1) & 1), b = (j & 1) * 8;
+      typedef __attribute__((address_space(3))) s16x4 L;
+      const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((L*)(s + at(r, c) + b));
+      const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((L*)(s + at(r + 8, c) + b));
+      typedef short s16x8 __attribute__((ext_vector_type(8)));
+      const s16x8 v = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+      return __builtin_bit_cast(Frag, v);
+    } else {
+      const int d = 32 * db + (lane & 31);
+      Frag f;
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        f[i] = *reinterpret_cast<const float*>(s + at(row + 8 * (i >> 2) + 4 * h + (i & 3), d >> 2) + (d & 3) * 4);
+      return f;
+    }
+  }
+};
+
+// 16 bytes of elements d0 .. of a row whose first `D` exist; element by element (any alignment).
+template <class T>
+__device__ __forceinline__ uint4 load_chunk_elems(const T* row, int d0, int D) {
+  constexpr int EC = 16 / (int)sizeof(T);
+  T e[EC];
+#pragma unroll
+  for (int i = 0; i < EC; ++i) e[i] = d0 + i < D ? row[d0 + i] : (T)0.f;
+  uint4 u;
+  __builtin_memcpy(&u, e, 16);
+  return u;
+}
+
+// Rows into LDS by WAVES waves, 1 KB an instruction.  VEC: 16-byte chunks straight into LDS through a buffer
+// resource, where rows start on 16 bytes, D is a whole number of chunks and a tile spans less than
+// 2 GiB (checked by the host); what lies past the operand reads zeros.  Else element by element.
+template <class T, int DP, int ROWS, int WAVES, bool VEC>
+struct AttnLoad {
+  using Tile = AttnTile<T, DP>;
+  static constexpr int BYTES = ROWS * Tile::RB;
+  static constexpr int NI = BYTES / (1024 * WAVES);
+  static_assert(NI * 1024 * WAVES == BYTES, "tile bytes split over the waves");
+  __device__ static __forceinline__ void place(int i, int wave, int lane, int& row, int& chunk) {
+    const int o = (i * WAVES + wave) * 64 + lane;     // 16-byte position in the tile
+    row = o / Tile::CH;
+    chunk = (o % Tile::CH) ^ Tile::swz(row);
+  }
+  // positions tile0 .. of one head: element offset of row r is r * ss
+  __device__ static __forceinline__ void positions(const T* head, long long ss, int tile0, int len, int D, char* lds,
+                                                   int wave, int lane) {
+    const int n = len - tile0;                        // rows that exist (> 0)
+    const T* base = head + (long long)tile0 * ss;
+    if constexpr (VEC) {
+      const int last = min(n, ROWS) - 1;
+      const auto rs = buffer_rsrc(base, (uint32_t)(last * ss * Tile::E + D * Tile::E));
+#pragma unroll
+      for (int i = 0; i < NI; ++i) {
+        int row, c;
+        place(i, wave, lane, row, c);
+        const uint32_t off = c * Tile::EC < D && row <= last ? (uint32_t)(row * (uint32_t)(ss * Tile::E) + c * 16) : 0x80000000u;
+        buffer_dma16(rs, off, 0, reinterpret_cast<float*>(lds + __builtin_amdgcn_readfirstlane((i * WAVES + wave) * 1024)));
+      }
+    } else {
+#pragma unroll 1
+      for (int i = 0; i < NI; ++i) {
+        int row, c;
+        place(i, wave, lane, row, c);
+        uint4 u = make_uint4(0, 0, 0, 0);
+        if (row < n) u = load_chunk_elems(base + (long long)row * ss, c * Tile::EC, D);
+        *reinterpret_cast<uint4*>(lds + ((i * WAVES + wave) * 64 + lane) * 16) = u;
+      }
+    }
+  }
+  // packed rows r0 .. of one key/value head's queries: row r is position r / G of head r % G
+  __device__ static __forceinline__ void packed(const T* head, long long ss, long long sh, int r0, int R, const FastDiv& gdiv,
+                                                int D, char* lds, int wave, int lane) {
+    const int i0 = (int)gdiv.div((uint32_t)r0);
+    const T* base = head + (long long)i0 * ss;
+    if constexpr (VEC) {
+      const auto rs = buffer_rsrc(base, 0x7fffffffu);
+#pragma unroll
+      for (int i = 0; i < NI; ++i) {
+        int row, c;
+        place(i, wave, lane, row, c);
+        const int r = r0 + row;
+        const int pi = (int)gdiv.div((uint32_t)r), g = r - pi * (int)gdiv.d;
+        const uint32_t off = c * Tile::EC < D && r < R
+                                 ? (uint32_t)((long long)(pi - i0) * ss * Tile::E + (long long)g * sh * Tile::E) + c * 16
+                                 : 0x80000000u;
+        buffer_dma16(rs, off, 0, reinterpret_cast<float*>(lds + __builtin_amdgcn_readfirstlane((i * WAVES + wave) * 1024)));
+      }
+    } else {
+#pragma unroll 1
+      for (int i = 0; i < NI; ++i) {
+        int row, c;
+        place(i, wave, lane, row, c);
+        const int r = r0 + row;
+        uint4 u = make_uint4(0, 0, 0, 0);
+        if (r < R) {
+          const int pi = (int)gdiv.div((uint32_t)r), g = r - pi * (int)gdiv.d;
+          u = load_chunk_elems(base + (long long)(pi - i0) * ss + (long long)g * sh, c * Tile::EC, D);
+        }
+        *reinterpret_cast<uint4*>(lds + ((i * WAVES + wave) * 64 + lane) * 16) = u;
+      }
+    }
+  }
+};
+
+// The B operand of a row (or key) that a lane owns: elements 16 t + 8 h + i of `row`, zeros past D or if !ok.
+template <class T, int DP, bool VEC>
+__device__ __forceinline__ void load_owned(const T* row, bool ok, int D, int lane, typename Num<T>::Frag (&f)[DP / 16]) {
+  using Frag = typename Num<T>::Frag;
+  const int h = lane >> 5;
+#pragma unroll
+  for (int t = 0; t < DP / 16; ++t) {
+    const int d0 = 16 * t + 8 * h;
+    uint4 u[sizeof(Frag) / 16];
+#pragma unroll
+    for (int w = 0; w < (int)(sizeof(Frag) / 16); ++w) {
+      const int d = d0 + w * (16 / (int)sizeof(T));
+      u[w] = make_uint4(0, 0, 0, 0);
+      if (ok && d < D) {
+        if constexpr (VEC)
+          u[w] = *reinterpret_cast<const uint4*>(row + d);
+        else
+          u[w] = load_chunk_elems(row, d, D);
+      }
+    }
+    __builtin_memcpy(&f[t], u, sizeof(Frag));
+  }
+}
+
+// acc[db][v] * f is element 32 db + 8 (v / 4) + 4 h + v % 4 of the lane's row.
+template <class T, int DP, bool VEC>
+__device__ __forceinline__ void store_owned(T* row, int D, int lane, const f32x16 (&acc)[DP / 32], float f) {
+  using Four = typename Num<T>::Four;
+  const int h = lane >> 5;
+#pragma unroll
+  for (int db = 0; db < DP / 32; ++db)
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const int d = 32 * db + 8 * q + 4 * h;
+      Four v;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v[i] = (T)(acc[db][4 * q + i] * f);
+      if constexpr (VEC) {
+        if (d < D) *reinterpret_cast<Four*>(row + d) = v;   // D is a multiple of 4
+      } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (d + i < D) row[d + i] = v[i];
+      }
+    }
+}
+
+// registers 8 u .. 8 u + 7 of a D block as the next product's B operand
+template <class T>
+__device__ __forceinline__ typename Num<T>::Frag to_frag(const f32x16& s, int u) {
+  typename Num<T>::Frag f;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) f[i] = (T)s[8 * u + i];
+  return f;
+}
+
+// The lanes l and l ^ 32 hold the two halves of a column.
+__device__ __forceinline__ float half_max(float x) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float half_sum(float x) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+
+__device__ __forceinline__ float exp2_hw(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// tanh(x) for y = 2 log2(e) x: 1 - 2 / (2^y + 1), absolute error a few 2^-24 (2^y = inf gives 1).  fp32
+// takes the library's tanhf, whose relative error holds near zero too.
+template <class T>
+__device__ __forceinline__ float tanh_of(float y) {
+  if constexpr (sizeof(T) == 4) return tanhf(y * (0.5f / kLog2e));
+  return 1.f - 2.f * __builtin_amdgcn_rcpf(exp2_hw(y) + 1.f);
+}
+
+// ---- operands that are not finite ------------------------------------------------------------------
+// A hidden (row, key) pair has weight 0, and 0 * inf is NaN: where a result comes out not finite, the tile is
+// computed again with this product.  It multiplies the finite elements and adds, as inf, -inf or NaN,
+// the others that a *visible* pair meets: `vis` holds 1 for such pairs, 0 for the hidden ones.
+template <class T>
+__device__ __forceinline__ f32x16 mma_visible(typename Num<T>::Frag a, typename Num<T>::Frag w, typename Num<T>::Frag vis,
+                                              f32x16 acc) {
+  using Frag = typename Num<T>::Frag;
+  __builtin_amdgcn_sched_barrier(0);   // rarely run: few registers before overlap
+  Frag fin, bad, sgn;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const float x = (float)a[i];
+    const bool ok = __builtin_isfinite(x);
+    fin[i] = ok ? a[i] : (T)0.f;
+    bad[i] = (T)(ok ? 0.f : 1.f);
+    sgn[i] = (T)(__builtin_isinf(x) ? (x > 0.f ? 1.f : -1.f) : 0.f);
+  }
+  acc = Num<T>::mma(fin, w, acc);
+  f32x16 z;
+#pragma unroll
+  for (int v = 0; v < 16; ++v) z[v] = 0.f;
+  const f32x16 n = Num<T>::mma(bad, vis, z), m = Num<T>::mma(sgn, vis, z);
+#pragma unroll
+  for (int v = 0; v < 16; ++v)
+    if (n[v] > 0.f)
+      acc[v] += n[v] == m[v] ? __builtin_inff() : n[v] == -m[v] ? -__builtin_inff() : __builtin_nanf("");
+  return acc;
+}
+
+template <int N>
+__device__ __forceinline__ bool not_finite(const f32x16 (&acc)[N]) {
+  // x * 0 is NaN for inf and NaN alone, and a NaN stays through the sum
+  float s = 0.f;
+#pragma unroll
+  for (int db = 0; db < N; ++db)
+#pragma unroll
+    for (int v = 0; v < 16; ++v) s = fmaf(acc[db][v], 0.f, s);
+  return !(s == 0.f);
+}
+
+// waits until at most N of this wave's global loads are outstanding (they complete in order)
+template <int N>
+__device__ __forceinline__ void wait_loads() {
+  static_assert(N >= 0 && N < 64, "six bits");
+  __builtin_amdgcn_s_waitcnt(0x0F70 | (N & 15) | ((N >> 4) << 14));
+}
+
+__device__ __forceinline__ void zero16(f32x16& a) {
+#pragma unroll
+  for (int v = 0; v < 16; ++v) a[v] = 0.f;
+}
+
+// Blocks are dealt out to the eight dies in turn; this gives each die a contiguous run of the work, so that
+// the tiles that read one head's keys share that die's L2.
+__device__ __forceinline__ int die_order(int id, int n) {
+  const int per = n >> 3, rest = n & 7, die = id & 7, k = id >> 3;
+  return die * per + min(die, rest) + k;
+}
+
+// Documents: which of the 64 tiles from `first` hold an id of [lo, hi]; id(t, lane) is the id of the
+// tile's lane-th row or -1.
+template <class F>
+__device__ __forceinline__ unsigned long long doc_tiles(int n, int lo, int hi, F id) {
+  unsigned long long m = 0;
+#pragma unroll 1
+  for (int t = 0; t < n; ++t) {
+    const int v = id(t);
+    const unsigned long long any = __ballot(v >= lo && v <= hi);
+    m |= (unsigned long long)(any != 0) << t;
+  }
+  return m;
+}
+
+// Where a tile's keys come from: the active tiles of [t0, t1), in order.
+struct KeyTiles {
+  int t1, lo, hi, len, base, bn;
+  unsigned long long mask;
+  const int* docs;   // of the batch entry, or null
+  __device__ __forceinline__ int from(int t, int lane) {
+    if (!docs) return t;
+    while (t < t1) {
+      if (base < 0 || t >= base + 64) {
+        base = t;
+        mask = doc_tiles(min(64, t1 - t), lo, hi, [&](int k) {
+          const int j = (t + k) * bn + lane;
+          return lane < bn && j < len ? docs[j] : -1;
+        });
+      }
+      const unsigned long long m = mask >> (t - base);
+      if (m) return t + __builtin_ctzll(m);
+      t = base + 64;
+    }
+    return t1;
+  }
+};
+
+// Smallest and largest document (>= 0) of the positions p0 .. p1 (at most 128 of them).
+__device__ __forceinline__ void doc_range(const int* docs, int p0, int p1, int lane, int& lo, int& hi) {
+  lo = 0x7fffffff;
+  hi = -1;
+  for (int p = max(p0, 0) + lane; p <= p1; p += 64) {
+    const int d = docs[p];
+    if (d >= 0) {
+      lo = min(lo, d);
+      hi = max(hi, d);
+    }
+  }
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    lo = min(lo, __shfl_xor(lo, o));
+    hi = max(hi, __shfl_xor(hi, o));
+  }
+}
+
+}  // namespace ntk

@@ -1,0 +1,305 @@
+// kernels_norm.hip -- root-mean-square norm with the residual's addition, its 8-bit output and its gradient.
+//
+//   h = x + residual,  r = (mean h^2 + eps)^(-1/2),  y = h r w;   8 bits: s = max|y| / 448, q = e4m3(y / s)
+//   g = dy w,  dx = r (g - h r^2 mean(g h)) + dh,  dw = sum_rows dy h r
+//
+// A row is held in registers between its two uses, so every array moves once.  Sums are fp32; y follows from the
+// unrounded h, and the gradient from the h that was stored.  A row takes 64, 256 or 1024 threads, each
+// with CH groups of 8 elements: short rows share a workgroup, long ones fill one.
+#include <hip/hip_runtime.h>
+
+#include "launch_seq.hpp"
+
+namespace ntk {
+namespace {
+
+constexpr int kE = 8;                       // elements a thread takes at once
+constexpr int kBlock = 256;
+constexpr float kMostE4m3 = 448.f;
+
+template <class T>
+struct Pack8 {
+  T v[kE];
+};
+
+// 8 elements from `at` on; those past n are zero
+template <class T, bool VEC>
+__device__ __forceinline__ void load8(const T* __restrict__ row, int at, int n, float (&f)[kE]) {
+  if constexpr (VEC) {
+    if (at < n) {
+      alignas(16) Pack8<T> p;
+      uint4* u = reinterpret_cast<uint4*>(&p);
+#pragma unroll
+      for (int i = 0; i < (int)sizeof(p) / 16; ++i) u[i] = reinterpret_cast<const uint4*>(row + at)[i];
+#pragma unroll
+      for (int i = 0; i < kE; ++i) f[i] = (float)p.v[i];
+      return;
+    }
+#pragma unroll
+    for (int i = 0; i < kE; ++i) f[i] = 0.f;
+  } else {
+#pragma unroll
+    for (int i = 0; i < kE; ++i) f[i] = at + i < n ? (float)row[at + i] : 0.f;
+  }
+}
+
+template <class T, bool VEC>
+__device__ __forceinline__ void store8(T* __restrict__ row, int at, int n, const float (&f)[kE]) {
+  if constexpr (VEC) {
+    if (at >= n) return;
+    alignas(16) Pack8<T> p;
+#pragma unroll
+    for (int i = 0; i < kE; ++i) p.v[i] = (T)f[i];
+    const uint4* u = reinterpret_cast<const uint4*>(&p);
+#pragma unroll
+    for (int i = 0; i < (int)sizeof(p) / 16; ++i) reinterpret_cast<uint4*>(row + at)[i] = u[i];
+  } else {
+#pragma unroll
+    for (int i = 0; i < kE; ++i)
+      if (at + i < n) row[at + i] = (T)f[i];
+  }
+}
+
+// sum (or maximum) over the TPR threads of a row; every thread gets it
+template <int TPR, bool MAX>
+__device__ __forceinline__ float row_all(float x, float* s) {
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const float y = __shfl_xor(x, o);
+    x = MAX ? fmaxf(x, y) : x + y;
+  }
+  if constexpr (TPR > 64) {
+    const int wave = threadIdx.x >> 6;
+    if ((threadIdx.x & 63) == 0) s[wave] = x;
+    __syncthreads();
+    x = s[0];
+#pragma unroll
+    for (int w = 1; w < TPR / 64; ++w) x = MAX ? fmaxf(x, s[w]) : x + s[w];
+    __syncthreads();
+  }
+  return x;
+}
+
+template <class T, class W, int TPR, int CH, bool VEC>
+__global__ void __launch_bounds__(TPR < kBlock ? kBlock : TPR) k_rms_norm(const NormArgs a) {
+  constexpr int RPB = TPR < kBlock ? kBlock / TPR : 1;
+  __shared__ float s[16];
+  const int t = threadIdx.x % TPR;
+  const long long row = (long long)blockIdx.x * RPB + threadIdx.x / TPR;
+  if (row >= a.rows) return;                // whole waves: with TPR > 64 the grid is exact
+  const T* x = (const T*)a.x + row * a.x_stride;
+  const T* res = a.residual ? (const T*)a.residual + row * a.residual_stride : nullptr;
+  const int n = a.width;
+  float h[CH][kE], w[CH][kE];
+#pragma unroll
+  for (int c = 0; c < CH; ++c) load8<T, VEC>(x, (c * TPR + t) * kE, n, h[c]);
+  if (res) {
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {
+      float e[kE];
+      load8<T, VEC>(res, (c * TPR + t) * kE, n, e);
+#pragma unroll
+      for (int i = 0; i < kE; ++i) h[c][i] += e[i];
+    }
+  }
+#pragma unroll
+  for (int c = 0; c < CH; ++c) load8<W, VEC>((const W*)a.weight, (c * TPR + t) * kE, n, w[c]);
+  float ss = 0.f;
+#pragma unroll
+  for (int c = 0; c < CH; ++c)
+#pragma unroll
+    for (int i = 0; i < kE; ++i) ss = fmaf(h[c][i], h[c][i], ss);
+  ss = row_all<TPR, false>(ss, s);
+  const float r = 1.f / sqrtf(ss / (float)n + a.eps);
+  if (a.h) {
+#pragma unroll
+    for (int c = 0; c < CH; ++c) store8<T, VEC>((T*)a.h + row * n, (c * TPR + t) * kE, n, h[c]);
+  }
+#pragma unroll
+  for (int c = 0; c < CH; ++c)
+#pragma unroll
+    for (int i = 0; i < kE; ++i) h[c][i] = h[c][i] * r * w[c][i];
+  if (!a.scale) {
+#pragma unroll
+    for (int c = 0; c < CH; ++c) store8<T, VEC>((T*)a.y + row * n, (c * TPR + t) * kE, n, h[c]);
+    return;
+  }
+  float most = 0.f;
+#pragma unroll
+  for (int c = 0; c < CH; ++c)
+#pragma unroll
+    for (int i = 0; i < kE; ++i) most = fmaxf(most, fabsf(h[c][i]));
+  most = row_all<TPR, true>(most, s);
+  const float scale = most > 0.f ? most / kMostE4m3 : 1.f;
+  if (t == 0) a.scale[row] = scale;
+  const float inv = 1.f / scale;
+  unsigned char* q = (unsigned char*)a.y + row * n;
+#pragma unroll
+  for (int c = 0; c < CH; ++c) {
+    unsigned u[2];
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      // the product with 1 / scale may round past 448, where the conversion has no finite value
+      float e[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float z = h[c][4 * k + i] * inv;
+        e[i] = z != z ? z : fminf(fmaxf(z, -kMostE4m3), kMostE4m3);
+      }
+      int p = __builtin_amdgcn_cvt_pk_fp8_f32(e[0], e[1], 0, false);
+      u[k] = (unsigned)__builtin_amdgcn_cvt_pk_fp8_f32(e[2], e[3], p, true);
+    }
+    const int at = (c * TPR + t) * kE;
+    if constexpr (VEC) {
+      if (at < n) *reinterpret_cast<uint2*>(q + at) = make_uint2(u[0], u[1]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < kE; ++i)
+        if (at + i < n) q[at + i] = (unsigned char)(u[i >> 2] >> (8 * (i & 3)));
+    }
+  }
+}
+
+// Workgroup g takes the rows g, g + G, ... (times RPB): dw is summed over them in registers and written as one
+// partial row a workgroup, which k_norm_columns adds in order.
+template <class T, class W, int TPR, int CH, bool VEC>
+__global__ void __launch_bounds__(TPR < kBlock ? kBlock : TPR) k_rms_norm_bwd(const NormBwdArgs a) {
+  constexpr int RPB = TPR < kBlock ? kBlock / TPR : 1;
+  __shared__ float s[16];
+  const int t = threadIdx.x % TPR, sub = threadIdx.x / TPR;
+  const int n = a.width;
+  float w[CH][kE], dw[CH][kE];
+#pragma unroll
+  for (int c = 0; c < CH; ++c) {
+    load8<W, VEC>((const W*)a.weight, (c * TPR + t) * kE, n, w[c]);
+#pragma unroll
+    for (int i = 0; i < kE; ++i) dw[c][i] = 0.f;
+  }
+  for (long long row = (long long)blockIdx.x * RPB + sub; row < a.rows; row += (long long)gridDim.x * RPB) {
+    float h[CH][kE], g[CH][kE];
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {
+      load8<T, VEC>((const T*)a.h + row * a.h_stride, (c * TPR + t) * kE, n, h[c]);
+      load8<T, VEC>((const T*)a.dy + row * a.dy_stride, (c * TPR + t) * kE, n, g[c]);
+    }
+    float ss = 0.f, sg = 0.f;
+#pragma unroll
+    for (int c = 0; c < CH; ++c)
+#pragma unroll
+      for (int i = 0; i < kE; ++i) {
+        ss = fmaf(h[c][i], h[c][i], ss);
+        sg = fmaf(g[c][i] * w[c][i], h[c][i], sg);
+      }
+    ss = row_all<TPR, false>(ss, s);
+    sg = row_all<TPR, false>(sg, s);
+    const float r = 1.f / sqrtf(ss / (float)n + a.eps);
+    const float f = r * r * (sg / (float)n);
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {
+      const int at = (c * TPR + t) * kE;
+      float e[kE];
+      if (a.dh) {
+        load8<T, VEC>((const T*)a.dh + row * a.dh_stride, at, n, e);
+      } else {
+#pragma unroll
+        for (int i = 0; i < kE; ++i) e[i] = 0.f;
+      }
+#pragma unroll
+      for (int i = 0; i < kE; ++i) {
+        dw[c][i] = fmaf(g[c][i], h[c][i] * r, dw[c][i]);
+        e[i] += r * (g[c][i] * w[c][i] - h[c][i] * f);
+      }
+      store8<T, VEC>((T*)a.dx + row * n, at, n, e);
+    }
+  }
+  float* part = a.part + ((long long)blockIdx.x * RPB + sub) * n;
+#pragma unroll
+  for (int c = 0; c < CH; ++c) store8<float, false>(part, (c * TPR + t) * kE, n, dw[c]);
+}
+
+// dw[c] = sum_p part[p][c], in a fixed order: 16 columns a workgroup, 16 threads a column.
+template <class W>
+__global__ void __launch_bounds__(256) k_norm_columns(const float* __restrict__ part, int parts, int n, W* __restrict__ dw) {
+  __shared__ float s[16][17];
+  const int c = threadIdx.x & 15, q = threadIdx.x >> 4, col = blockIdx.x * 16 + c;
+  float x = 0.f;
+  if (col < n)
+    for (int p = q; p < parts; p += 16) x += part[(long long)p * n + col];
+  s[q][c] = x;
+  __syncthreads();
+  if (q) return;
+#pragma unroll
+  for (int k = 1; k < 16; ++k) x += s[k][c];
+  if (col < n) dw[col] = (W)x;
+}
+
+// Threads a row and groups a thread.  Up to 1024 columns a wave holds the row: no barrier, four rows a workgroup.
+struct Shape {
+  int tpr, ch;
+};
+Shape shape_of(int n) {
+  if (n <= 512) return {64, 1};
+  if (n <= 1024) return {64, 2};
+  if (n <= 2048) return {256, 1};
+  if (n <= 4096) return {256, 2};
+  if (n <= 8192) return {256, 4};
+  if (n <= 16384) return {1024, 2};
+  return {1024, 4};
+}
+
+template <class T, class W, int TPR, int CH>
+hipError_t run(hipStream_t s, const NormArgs* f, const NormBwdArgs* b, bool vec) {
+  constexpr int threads = TPR < kBlock ? kBlock : TPR, rpb = TPR < kBlock ? kBlock / TPR : 1;
+  if (f) {
+    const dim3 grid((unsigned)((f->rows + rpb - 1) / rpb));
+    if (vec)
+      k_rms_norm<T, W, TPR, CH, true><<<grid, threads, 0, s>>>(*f);
+    else
+      k_rms_norm<T, W, TPR, CH, false><<<grid, threads, 0, s>>>(*f);
+    return hipGetLastError();
+  }
+  const int parts = norm_bwd_parts(b->rows, b->width);
+  const dim3 grid((unsigned)(parts / rpb));
+  if (vec)
+    k_rms_norm_bwd<T, W, TPR, CH, true><<<grid, threads, 0, s>>>(*b);
+  else
+    k_rms_norm_bwd<T, W, TPR, CH, false><<<grid, threads, 0, s>>>(*b);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  k_norm_columns<W><<<dim3((unsigned)((b->width + 15) / 16)), dim3(256), 0, s>>>(b->part, parts, b->width, (W*)b->dw);
+  return hipGetLastError();
+}
+
+template <class T, class W>
+hipError_t pick(hipStream_t s, const NormArgs* f, const NormBwdArgs* b, bool vec) {
+  const Shape h = shape_of(f ? f->width : b->width);
+  if (h.tpr == 64) return h.ch == 1 ? run<T, W, 64, 1>(s, f, b, vec) : run<T, W, 64, 2>(s, f, b, vec);
+  if (h.tpr == 256)
+    return h.ch == 1 ? run<T, W, 256, 1>(s, f, b, vec) : h.ch == 2 ? run<T, W, 256, 2>(s, f, b, vec) : run<T, W, 256, 4>(s, f, b, vec);
+  return h.ch == 2 ? run<T, W, 1024, 2>(s, f, b, vec) : run<T, W, 1024, 4>(s, f, b, vec);
+}
+
+hipError_t by_type(hipStream_t s, int dtype, int wtype, const NormArgs* f, const NormBwdArgs* b, bool vec) {
+  if (dtype == 1) return wtype == 0 ? pick<__bf16, float>(s, f, b, vec) : pick<__bf16, __bf16>(s, f, b, vec);
+  if (dtype == 2) return wtype == 0 ? pick<_Float16, float>(s, f, b, vec) : pick<_Float16, _Float16>(s, f, b, vec);
+  return pick<float, float>(s, f, b, vec);
+}
+
+}  // namespace
+
+int norm_bwd_parts(long long rows, int width) {
+  const Shape h = shape_of(width);
+  const int rpb = h.tpr < kBlock ? kBlock / h.tpr : 1;
+  const long long groups = (rows + rpb - 1) / rpb;
+  const long long most = h.tpr == 1024 ? 256 : 1024;    // workgroups: four (one of 1024 threads) a compute unit
+  return (int)(groups < most ? groups : most) * rpb;
+}
+
+hipError_t launch_rms_norm(hipStream_t s, int dtype, int wtype, const NormArgs& a, bool vec) {
+  return by_type(s, dtype, wtype, &a, nullptr, vec);
+}
+hipError_t launch_rms_norm_bwd(hipStream_t s, int dtype, int wtype, const NormBwdArgs& a, bool vec) {
+  return by_type(s, dtype, wtype, nullptr, &a, vec);
+}
+
+}  // namespace ntk

@@ -193,6 +193,18 @@ static int fail(ntk_handle* h, int code, const std::string& msg) {
   return code;
 }
 
+// The message of a failed call without a handle, for the entry points outside this file.
+namespace ntk {
+int call_error(int code, const char* what) noexcept;
+int call_error(int code, const char* what) noexcept {
+  try {
+    g_init_error = what;
+  } catch (...) {   // no memory for the message: the code alone
+  }
+  return code;
+}
+}  // namespace ntk
+
 static int hip_fail(ntk_handle* h, hipError_t e, const char* what) {
   return fail(h, NTK_E_HIP, std::string(what) + ": " + hipGetErrorString(e));
 }

@@ -1,0 +1,269 @@
+"""Operators of a sequence model's block: root-mean-square norm, rotary positions, attention.
+
+    h = seq.rms_norm(x, weight)                                    # or (y, h) with residual=
+    q, k = seq.rotary(q, table, positions, k=k)
+    o = seq.attention(q, k, v, causal=True)                        # or one token over a cache: k_lens=
+
+and their gradients (`rms_norm_backward`, `rotary(..., inverse=True)`, `attention_backward`).  Arrays are
+float32, bfloat16 or float16 torch tensors on the GPU; only the last dimension has to be contiguous.  Every
+call enqueues on the current stream, or on `stream`, and returns before the work is done.  As in `ntk`, PyTorch
+supplies device memory and streams only: every step runs in libntk.so (include/ntk_seq.h has the
+formulas, the limits and what each mask means).
+"""
+from __future__ import annotations
+
+import contextlib
+import ctypes
+import math
+
+import torch
+
+from . import _lib
+
+_DTYPES = {torch.float32: _lib.NTK_F32, torch.bfloat16: _lib.NTK_BF16, torch.float16: _lib.NTK_F16}
+_NO_CONTEXT = contextlib.nullcontext()
+
+
+def _check(t, name, dtype=None, ndim=None, device=None, shape=None):
+    if not isinstance(t, torch.Tensor) or not t.is_cuda or (t.dtype not in _DTYPES if dtype is None else t.dtype != dtype):
+        raise TypeError(f"{name} must be a GPU tensor of type {dtype or 'float32, bfloat16 or float16'}")
+    if device is not None and t.device != device:
+        raise ValueError(f"{name} is on {t.device}, expected {device}")
+    if (ndim is not None and t.dim() != ndim) or (shape is not None and tuple(t.shape) != tuple(shape)):
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape) if shape is not None else f'{ndim} dimensions'}")
+    if t.dim() and t.stride(-1) != 1 and t.shape[-1] > 1:
+        raise ValueError(f"{name} must be contiguous in its last dimension")
+
+
+class _Call:
+    """The device and stream of one call: outputs and workspaces are allocated for that stream, and tensors
+    that come from another one are kept from reuse until it has passed this call."""
+
+    def __init__(self, lead, stream, inputs):
+        self.device = lead.device
+        self.stream = torch.cuda.current_stream(lead.device) if stream is None else stream
+        self.handle = ctypes.c_void_p(self.stream.cuda_stream)
+        self._enter = []
+        if torch.cuda.current_device() != lead.device.index:
+            self._enter.append(torch.cuda.device(lead.device))
+        if stream is not None:
+            self._enter.append(torch.cuda.stream(stream))
+            for t in inputs:
+                if t is not None:
+                    t.record_stream(stream)
+
+    def __enter__(self):
+        for c in self._enter:
+            c.__enter__()
+        return self
+
+    def __exit__(self, *exc):
+        for c in reversed(self._enter):
+            c.__exit__(*exc)
+
+
+def _ptr(t):
+    return None if t is None else ctypes.c_void_p(t.data_ptr())
+
+
+def _view(t):
+    """ntk_view of [batch, position, head, dim]; the stride of a dimension of size 1 is never used."""
+    n, s = t.shape, t.stride()
+    return _lib.ntk_view(t.data_ptr(), s[0] if n[0] > 1 else 0, s[1] if n[1] > 1 else 0, s[2] if n[2] > 1 else 0)
+
+
+def _rows(t):
+    """A tensor's rows [rows, width] as (tensor, row stride), without a copy where the rows are evenly spaced."""
+    r = t.reshape(-1, t.shape[-1]) if t.dim() != 2 else t
+    return r, r.stride(0) if r.shape[0] > 1 else max(r.stride(0), r.shape[1])
+
+
+# ---- root-mean-square norm ----------------------------------------------------------------------------------
+
+def _rms_norm(x, weight, residual, eps, stream, e4m3):
+    lib = _lib.load()
+    _check(x, "x")
+    if x.dim() < 1:
+        raise ValueError("x needs a last dimension")
+    width = x.shape[-1]
+    if weight.dtype != torch.float32 and weight.dtype != x.dtype:
+        raise TypeError(f"weight must be float32 or {x.dtype}")
+    _check(weight, "weight", weight.dtype, device=x.device, shape=(width,))
+    if residual is not None:
+        _check(residual, "residual", x.dtype, device=x.device, shape=x.shape)
+    with _Call(x, stream, (x, weight, residual)) as call:
+        xr, xs = _rows(x)
+        rr, rs = (None, 0) if residual is None else _rows(residual)
+        y = torch.empty(x.shape, dtype=torch.float8_e4m3fn if e4m3 else x.dtype, device=x.device)
+        h = None if residual is None else torch.empty(x.shape, dtype=x.dtype, device=x.device)
+        scale = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device) if e4m3 else None
+        _lib.check(lib.ntk_rms_norm(_DTYPES[x.dtype], _DTYPES[weight.dtype], xr.shape[0], width, _ptr(xr), xs, _ptr(rr), rs,
+                                    _ptr(weight), eps, _ptr(y), _ptr(h), _ptr(scale), call.handle))
+    return y, h, scale
+
+
+def rms_norm(x, weight, residual=None, eps=1e-6, stream=None):
+    """y = h weight / sqrt(mean(h^2) + eps) over the last dimension, with h = x.  With `residual`, h = x + residual
+    and (y, h) is returned: h is what the next block adds to and what the backward pass reads."""
+    y, h, _ = _rms_norm(x, weight, residual, eps, stream, False)
+    return y if residual is None else (y, h)
+
+
+def rms_norm_e4m3(x, weight, residual=None, eps=1e-6, stream=None):
+    """The norm in 8 bits: (q, scale) or, with `residual`, (q, scale, h), where q (float8_e4m3fn) times its row's scale
+    is y, and scale = max|y| / 448."""
+    q, h, scale = _rms_norm(x, weight, residual, eps, stream, True)
+    return (q, scale) if residual is None else (q, scale, h)
+
+
+def rms_norm_backward(dy, h, weight, dh=None, eps=1e-6, stream=None):
+    """(dx, dweight) of `rms_norm`: dx is the gradient of x and of the residual alike.  `dh` is the gradient that
+    reaches h from elsewhere (the next block's residual)."""
+    lib = _lib.load()
+    _check(h, "h")
+    width = h.shape[-1]
+    _check(dy, "dy", h.dtype, device=h.device, shape=h.shape)
+    if dh is not None:
+        _check(dh, "dh", h.dtype, device=h.device, shape=h.shape)
+    if weight.dtype != torch.float32 and weight.dtype != h.dtype:
+        raise TypeError(f"weight must be float32 or {h.dtype}")
+    _check(weight, "weight", weight.dtype, device=h.device, shape=(width,))
+    with _Call(h, stream, (dy, h, weight, dh)) as call:
+        hr, hs = _rows(h)
+        yr, ys = _rows(dy)
+        dr, ds = (None, 0) if dh is None else _rows(dh)
+        dx, dweight = torch.empty(h.shape, dtype=h.dtype, device=h.device), torch.empty_like(weight)
+        rows = hr.shape[0]
+        if rows == 0:
+            return dx, dweight.zero_()
+        need = lib.ntk_rms_norm_workspace(rows, width)
+        if need < 0:
+            _lib.check(need)
+        work = torch.empty(need, dtype=torch.uint8, device=h.device)
+        _lib.check(lib.ntk_rms_norm_bwd(_DTYPES[h.dtype], _DTYPES[weight.dtype], rows, width, _ptr(yr), ys, _ptr(hr), hs, _ptr(weight),
+                                        _ptr(dr), ds, eps, _ptr(dx), _ptr(dweight), _ptr(work), need, call.handle))
+    return dx, dweight
+
+
+# ---- rotary positions ---------------------------------------------------------------------------------------
+
+def rotary_table(max_pos, rot, base=10000.0, scaling=None, factor=1.0, original=None, low=1.0, high=32.0, device=None,
+                 stream=None):
+    """[max_pos, rot / 2, 2] float32: the cosine and sine of every position and pair, angles in 64 bits.  For
+    contexts longer than the trained one `scaling` is "linear", "base" or "ramp" with their `factor` (the ramp also
+    with the trained length `original`, and the numbers of turns `low` and `high` between which it lies)."""
+    lib = _lib.load()
+    if not torch.cuda.is_available():
+        raise RuntimeError("no GPU visible: the NTK library runs on an MI355X only")
+    kinds = {None: _lib.NTK_ROTARY_PLAIN, "linear": _lib.NTK_ROTARY_LINEAR, "base": _lib.NTK_ROTARY_BASE, "ramp": _lib.NTK_ROTARY_RAMP}
+    if scaling not in kinds:
+        raise ValueError(f"scaling is one of {list(kinds)}")
+    if scaling == "ramp" and original is None:
+        raise ValueError('scaling="ramp" needs original')
+    dev = torch.device("cuda", torch.cuda.current_device() if device is None else torch.device(device).index or 0)
+    if max_pos < 1 or rot < 2 or rot % 2:
+        raise ValueError("rotary_table: max_pos < 1, or rot odd or < 2")
+    s = _lib.ntk_rotary_scaling(kinds[scaling], float(factor), float(original or 1), float(low), float(high))
+    with torch.cuda.device(dev), torch.cuda.stream(stream) if stream is not None else _NO_CONTEXT:
+        table = torch.empty((max_pos, rot // 2, 2), dtype=torch.float32, device=dev)
+        _lib.check(lib.ntk_rotary_table(max_pos, rot, float(base), ctypes.byref(s), _ptr(table),
+                                        ctypes.c_void_p(torch.cuda.current_stream(dev).cuda_stream)))
+    return table
+
+
+def rotary(q, table, positions=0, k=None, interleaved=False, inverse=False, inplace=False, stream=None):
+    """Turns the first 2 * table.shape[1] elements of every head of q [batch, length, heads, dim], and of k with head counts of
+    its own, by their positions: int32 [batch, length], or the first position of every sequence.  Returns q, or
+    (q, k).  `inverse` undoes it, which is also how the gradients pass."""
+    lib = _lib.load()
+    _check(q, "q", ndim=4)
+    _check(table, "table", torch.float32, ndim=3, device=q.device)
+    b, n, heads, dim = q.shape
+    if not table.is_contiguous() or table.shape[2] != 2:
+        raise ValueError("table must be a contiguous [max_pos, rot / 2, 2] tensor")
+    if k is not None:
+        _check(k, "k", q.dtype, device=q.device, shape=(b, n, k.shape[2] if k.dim() == 4 else -1, dim))
+    per_token = isinstance(positions, torch.Tensor)
+    if per_token:
+        _check(positions, "positions", torch.int32, device=q.device, shape=(b, n))
+        if not positions.is_contiguous():
+            raise ValueError("positions must be contiguous")
+    with _Call(q, stream, (q, table, k, positions if per_token else None)) as call:
+        qo = q if inplace else torch.empty((b, n, heads, dim), dtype=q.dtype, device=q.device)
+        ko = k if inplace or k is None else torch.empty(tuple(k.shape), dtype=k.dtype, device=k.device)
+        kv, kov = (None, None) if k is None else (ctypes.byref(_view(k)), ctypes.byref(_view(ko)))
+        _lib.check(lib.ntk_rotary(_DTYPES[q.dtype], b, n, heads, 0 if k is None else k.shape[2], dim, 2 * table.shape[1],
+                                  int(interleaved), int(inverse), ctypes.byref(_view(q)), kv, _ptr(table), table.shape[0],
+                                  _ptr(positions) if per_token else None, 0 if per_token else int(positions),
+                                  ctypes.byref(_view(qo)), kov, call.handle))
+    return qo if k is None else (qo, ko)
+
+
+# ---- attention ----------------------------------------------------------------------------------------------
+
+def _attention_desc(q, k, v, causal, softcap, scale, slopes, k_lens, prefix, docs):
+    _check(q, "q", ndim=4)
+    b, sq, heads, dim = q.shape
+    _check(k, "k", q.dtype, ndim=4, device=q.device)
+    sk, kv_heads = k.shape[1], k.shape[2]
+    if k.shape[0] != b or k.shape[3] != dim:
+        raise ValueError(f"k has shape {tuple(k.shape)}, expected ({b}, k_len, kv_heads, {dim})")
+    _check(v, "v", q.dtype, device=q.device, shape=k.shape)
+    for name, t, dtype, shape in (("k_lens", k_lens, torch.int32, (b,)), ("prefix", prefix, torch.int32, (b,)),
+                                  ("docs", docs, torch.int32, (b, sk)), ("slopes", slopes, torch.float32, (heads,))):
+        if t is not None:
+            _check(t, name, dtype, device=q.device, shape=shape)
+            if not t.is_contiguous():
+                raise ValueError(f"{name} must be contiguous")
+    p = ctypes.c_void_p
+    return _lib.ntk_attention_desc(_DTYPES[q.dtype], b, sq, sk, heads, kv_heads, dim, 1 if causal else 0,
+                                   1.0 / math.sqrt(max(dim, 1)) if scale is None else scale, softcap,
+                                   *(p(0 if t is None else t.data_ptr()) for t in (k_lens, prefix, docs, slopes)))
+
+
+def _workspace(lib, desc, backward, device):
+    need = lib.ntk_attention_workspace(ctypes.byref(desc), backward)
+    if need < 0:
+        _lib.check(need)
+    return (torch.empty(need, dtype=torch.uint8, device=device) if need else None), need
+
+
+def attention(q, k, v, causal=False, softcap=0.0, scale=None, slopes=None, k_lens=None, prefix=None, docs=None,
+              return_lse=False, out=None, stream=None):
+    """softmax(scores) v for q [batch, q_len, heads, dim], k and v [batch, k_len, kv_heads, dim] (heads a multiple of
+    kv_heads); returns o like q, or (o, lse) for the backward pass.  Scores are softcap tanh(scale q.k / softcap) - slope
+    |distance|; the queries are the last q_len of each sequence's k_lens positions.  See include/ntk_seq.h for
+    what `causal`, `prefix` and `docs` hide."""
+    lib = _lib.load()
+    desc = _attention_desc(q, k, v, causal, softcap, scale, slopes, k_lens, prefix, docs)
+    b, sq, heads, dim = q.shape
+    if out is not None:
+        _check(out, "out", q.dtype, device=q.device, shape=q.shape)
+    with _Call(q, stream, (q, k, v, slopes, k_lens, prefix, docs, out)) as call:
+        o = torch.empty((b, sq, heads, dim), dtype=q.dtype, device=q.device) if out is None else out
+        lse = torch.empty((b, heads, sq), dtype=torch.float32, device=q.device) if return_lse else None
+        work, need = _workspace(lib, desc, 0, q.device)
+        _lib.check(lib.ntk_attention(ctypes.byref(desc), ctypes.byref(_view(q)), ctypes.byref(_view(k)), ctypes.byref(_view(v)),
+                                     ctypes.byref(_view(o)), _ptr(lse), _ptr(work), need, call.handle))
+    return (o, lse) if return_lse else o
+
+
+def attention_backward(do, q, k, v, o, lse, causal=False, softcap=0.0, scale=None, slopes=None, k_lens=None, prefix=None,
+                       docs=None, stream=None):
+    """(dq, dk, dv) of `attention` from the gradient of o, with the o and lse that it returned and the same options."""
+    lib = _lib.load()
+    desc = _attention_desc(q, k, v, causal, softcap, scale, slopes, k_lens, prefix, docs)
+    b, sq, heads, dim = q.shape
+    _check(do, "do", q.dtype, device=q.device, shape=q.shape)
+    _check(o, "o", q.dtype, device=q.device, shape=q.shape)
+    _check(lse, "lse", torch.float32, device=q.device, shape=(b, heads, sq))
+    if not lse.is_contiguous():
+        raise ValueError("lse must be contiguous")
+    with _Call(q, stream, (do, q, k, v, o, lse, slopes, k_lens, prefix, docs)) as call:
+        dq = torch.empty((b, sq, heads, dim), dtype=q.dtype, device=q.device)
+        dk, dv = (torch.empty(tuple(k.shape), dtype=k.dtype, device=k.device) for _ in range(2))
+        work, need = _workspace(lib, desc, 1, q.device)
+        views = [ctypes.byref(_view(t)) for t in (do, q, k, v, o)]
+        grads = [ctypes.byref(_view(t)) for t in (dq, dk, dv)]
+        _lib.check(lib.ntk_attention_bwd(ctypes.byref(desc), *views, _ptr(lse), *grads, _ptr(work), need, call.handle))
+    return dq, dk, dv
