@@ -19,6 +19,9 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <type_traits>
+#include <utility>
+
 #include "gemm_core.hpp"
 #include "index_math.hpp"
 
@@ -135,29 +138,86 @@ struct AttnTile {
       return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
     }
   }
-  // the transpose: column 32 db + lane % 32 at the rows row + 8 (i / 4) + 4 h + i % 4
-  __device__ static __forceinline__ Frag cols(const char* s, int row, int db, int lane) {
-    const int h = lane >> 5;
-    if constexpr (E == 2) {
-      const int j = lane & 15, g = (lane >> 4) & 1;
-      const int r = row + 4 * h + (j >> 2);
-      const int c = 4 * db + 2 * g + ((j >> 1) & 1), b = (j & 1) * 8;
-      typedef __attribute__((address_space(3))) s16x4 L;
-      const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((L*)(s + at(r, c) + b));
-      const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((L*)(s + at(r + 8, c) + b));
-      typedef short s16x8 __attribute__((ext_vector_type(8)));
-      const s16x8 v = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-      return __builtin_bit_cast(Frag, v);
-    } else {
-      const int d = 32 * db + (lane & 31);
-      Frag f;
+  // the transpose: columns 32 db + lane % 32 (db < DB) at the rows row + 8 (i / 4) + 4 h + i % 4, `row` a multiple
+  // of 16 below ROWS.  16 bits: transposed LDS reads, four rows of 16 columns each.  They are written out with
+  // their wait, because the compiler has its own wait for every global load in flight, the next tile's included; a
+  // wave's MFMAs run on meanwhile.
+  struct Cols {
+    uint32_t a[E == 2 ? DP / 32 : 1][2];   // byte addresses of the two halves (rows, rows + 8) of each db
+    const char* s;
+    __device__ __forceinline__ void set(const char* tile, int lane) {
+      s = tile;
+      if constexpr (E == 2) {
+        const int j = lane & 15, r = 4 * (lane >> 5) + (j >> 2), c = 2 * ((lane >> 4) & 1) + ((j >> 1) & 1);
+        typedef __attribute__((address_space(3))) const char L;
+        const uint32_t base = (uint32_t)(uintptr_t)(L*)tile;
+        const uint32_t o = (uint32_t)at(r, c) + (j & 1) * 8;
 #pragma unroll
-      for (int i = 0; i < 8; ++i)
-        f[i] = *reinterpret_cast<const float*>(s + at(row + 8 * (i >> 2) + 4 * h + (i & 3), d >> 2) + (d & 3) * 4);
-      return f;
+        for (int db = 0; db < DP / 32; ++db) {
+          a[db][0] = base + (o ^ (db << 6));
+          a[db][1] = base + ((o ^ (db << 6) ^ 32) + 8 * RB);
+        }
+      }
     }
-  }
+    template <int ROW>
+    __device__ __forceinline__ void read(Frag (&f)[DP / 32], int lane) const {
+      if constexpr (E == 2) {
+        s16x4 v[DP / 32][2];
+        if constexpr (DP == 128)
+          asm volatile(
+              "ds_read_b64_tr_b16 %0, %8 offset:%16\n\t"
+              "ds_read_b64_tr_b16 %1, %9 offset:%16\n\t"
+              "ds_read_b64_tr_b16 %2, %10 offset:%16\n\t"
+              "ds_read_b64_tr_b16 %3, %11 offset:%16\n\t"
+              "ds_read_b64_tr_b16 %4, %12 offset:%16\n\t"
+              "ds_read_b64_tr_b16 %5, %13 offset:%16\n\t"
+              "ds_read_b64_tr_b16 %6, %14 offset:%16\n\t"
+              "ds_read_b64_tr_b16 %7, %15 offset:%16\n\t"
+              "s_waitcnt lgkmcnt(0)"
+              : "=&v"(v[0][0]), "=&v"(v[0][1]), "=&v"(v[1][0]), "=&v"(v[1][1]), "=&v"(v[2][0]), "=&v"(v[2][1]), "=&v"(v[3][0]),
+                "=&v"(v[3][1])
+              : "v"(a[0][0]), "v"(a[0][1]), "v"(a[1][0]), "v"(a[1][1]), "v"(a[2][0]), "v"(a[2][1]), "v"(a[3][0]), "v"(a[3][1]),
+                "i"(ROW * RB)
+              : "memory");
+        else
+          asm volatile(
+              "ds_read_b64_tr_b16 %0, %4 offset:%8\n\t"
+              "ds_read_b64_tr_b16 %1, %5 offset:%8\n\t"
+              "ds_read_b64_tr_b16 %2, %6 offset:%8\n\t"
+              "ds_read_b64_tr_b16 %3, %7 offset:%8\n\t"
+              "s_waitcnt lgkmcnt(0)"
+              : "=&v"(v[0][0]), "=&v"(v[0][1]), "=&v"(v[1][0]), "=&v"(v[1][1])
+              : "v"(a[0][0]), "v"(a[0][1]), "v"(a[1][0]), "v"(a[1][1]), "i"(ROW * RB)
+              : "memory");
+#pragma unroll
+        for (int db = 0; db < DP / 32; ++db) {
+          typedef short s16x8 __attribute__((ext_vector_type(8)));
+          const s16x8 w = __builtin_shufflevector(v[db][0], v[db][1], 0, 1, 2, 3, 4, 5, 6, 7);
+          f[db] = __builtin_bit_cast(Frag, w);
+        }
+      } else {
+        const int h = lane >> 5;
+#pragma unroll
+        for (int db = 0; db < DP / 32; ++db) {
+          const int d = 32 * db + (lane & 31);
+#pragma unroll
+          for (int i = 0; i < 8; ++i)
+            f[db][i] = *reinterpret_cast<const float*>(s + at(ROW + 8 * (i >> 2) + 4 * h + (i & 3), d >> 2) + (d & 3) * 4);
+        }
+      }
+    }
+  };
 };
+
+template <int... I, class F>
+__device__ __forceinline__ void unrolled_impl(std::integer_sequence<int, I...>, F&& f) {
+  (f(std::integral_constant<int, I>{}), ...);
+}
+// f(integral_constant<int, 0>), ... : a loop whose index is a constant expression
+template <int N, class F>
+__device__ __forceinline__ void unrolled(F&& f) {
+  unrolled_impl(std::make_integer_sequence<int, N>{}, f);
+}
 
 // 16 bytes of elements d0 .. of a row whose first `D` exist; element by element (any alignment).
 template <class T>

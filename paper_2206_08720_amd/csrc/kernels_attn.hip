@@ -102,22 +102,24 @@ struct FwdRows {
         sum += s[nb][v];
       }
     l += sum;
+    typename Tile::Cols vc;
+    vc.set(sv, lane);
+    unrolled<2 * NB>([&](auto step) {
+      constexpr int X = decltype(step)::value, nb = X / 2, u = X % 2;
+      const Frag p = to_frag<T>(s[nb], u);
+      Frag vt[DB];
+      vc.template read<16 * X>(vt, lane);
+      if constexpr (!Careful::value) {
 #pragma unroll
-    for (int nb = 0; nb < NB; ++nb)
+        for (int d = 0; d < DB; ++d) acc[d] = N::mma(vt[d], p, acc[d]);
+      } else {
+        Frag w;
 #pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        const Frag p = to_frag<T>(s[nb], u);
-        if constexpr (!Careful::value) {
+        for (int i = 0; i < 8; ++i) w[i] = (T)((vis[nb] >> (8 * u + i)) & 1 ? 1.f : 0.f);
 #pragma unroll
-          for (int d = 0; d < DB; ++d) acc[d] = N::mma(Tile::cols(sv, 32 * nb + 16 * u, d, lane), p, acc[d]);
-        } else {
-          Frag w;
-#pragma unroll
-          for (int i = 0; i < 8; ++i) w[i] = (T)((vis[nb] >> (8 * u + i)) & 1 ? 1.f : 0.f);
-#pragma unroll
-          for (int d = 0; d < DB; ++d) acc[d] = mma_visible<T>(Tile::cols(sv, 32 * nb + 16 * u, d, lane), p, w, acc[d]);
-        }
+        for (int d = 0; d < DB; ++d) acc[d] = mma_visible<T>(vt[d], p, w, acc[d]);
       }
+    });
   }
 };
 

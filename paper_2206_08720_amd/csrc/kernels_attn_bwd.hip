@@ -127,8 +127,10 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) k_attn_dq(const A
       if (tn < kt.t1) issue(tn, st ^ 1);
       const bool masked = docs || (t + 1) * BN > all;
       const char *k_ = sk + st * Load::BYTES, *v_ = sv + st * Load::BYTES;
-#pragma unroll
-      for (int nb = 0; nb < BN / 32; ++nb) {
+      typename Tile::Cols cols;
+      cols.set(k_, lane);
+      unrolled<BN / 32>([&](auto block) {
+        constexpr int nb = decltype(block)::value;
         f32x16 s, dp;
         zero16(s);
         zero16(dp);
@@ -151,24 +153,23 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) k_attn_dq(const A
         }
         weights<T>(a, s, dp, vis, [&](int) { return lse2; }, [&](int) { return delta; }, [&](int) { return slope2; },
                    [&](int v) { return (float)abs(pos - (base + 8 * (v >> 2) + (v & 3))); });
-#pragma unroll
-        for (int u = 0; u < 2; ++u) {
+        unrolled<2>([&](auto step) {
+          constexpr int u = decltype(step)::value;
           const Frag w = to_frag<T>(dp, u);
-          Frag on;
+          Frag kc[DB];
+          cols.template read<32 * nb + 16 * u>(kc, lane);
           if constexpr (decltype(careful)::value) {
+            Frag on;
 #pragma unroll
             for (int e = 0; e < 8; ++e) on[e] = (T)((vis >> (8 * u + e)) & 1 ? 1.f : 0.f);
-          }
 #pragma unroll
-          for (int d = 0; d < DB; ++d) {
-            const Frag kc = Tile::cols(k_, 32 * nb + 16 * u, d, lane);
-            if constexpr (decltype(careful)::value)
-              acc[d] = mma_visible<T>(kc, w, on, acc[d]);
-            else
-              acc[d] = N::mma(kc, w, acc[d]);
+            for (int d = 0; d < DB; ++d) acc[d] = mma_visible<T>(kc[d], w, on, acc[d]);
+          } else {
+#pragma unroll
+            for (int d = 0; d < DB; ++d) acc[d] = N::mma(kc[d], w, acc[d]);
           }
-        }
-      }
+        });
+      });
       if (docs && tn < kt.t1 && tid < BN) sids[(st ^ 1) * BN + tid] = nid;
       t = tn;
       st ^= 1;
@@ -296,8 +297,11 @@ __global__ void __launch_bounds__(256, 1) k_attn_dkv(const AttnArgs a) {
       const bool masked = docs || k0 + kBwdKeyTile > sc.klim(p_first);
       const char *q_ = sq + st * Load::BYTES, *g_ = sg + st * Load::BYTES;
       const RowStats<BR>& rs = stats[st];
-#pragma unroll
-      for (int rb = 0; rb < BR / 32; ++rb) {
+      typename Tile::Cols gcols, qcols;
+      gcols.set(g_, lane);
+      qcols.set(q_, lane);
+      unrolled<BR / 32>([&](auto block) {
+        constexpr int rb = decltype(block)::value;
         f32x16 s, dp;
         zero16(s);
         zero16(dp);
@@ -321,27 +325,29 @@ __global__ void __launch_bounds__(256, 1) k_attn_dkv(const AttnArgs a) {
         }
         weights<T>(a, s, dp, vis, [&](int v) { return rs.lse2[at(v)]; }, [&](int v) { return rs.delta[at(v)]; },
                    [&](int v) { return rs.slope2[at(v)]; }, [&](int v) { return (float)abs(rs.pos[at(v)] - j); });
-#pragma unroll
-        for (int u = 0; u < 2; ++u) {
+        unrolled<2>([&](auto step) {
+          constexpr int u = decltype(step)::value;
           const Frag p = to_frag<T>(s, u), w = to_frag<T>(dp, u);
-          Frag on;
+          Frag gc[DB], qc[DB];
+          gcols.template read<32 * rb + 16 * u>(gc, lane);
           if constexpr (decltype(careful)::value) {
+            Frag on;
 #pragma unroll
             for (int e = 0; e < 8; ++e) on[e] = (T)((vis >> (8 * u + e)) & 1 ? 1.f : 0.f);
-          }
 #pragma unroll
-          for (int d = 0; d < DB; ++d) {
-            const Frag gc = Tile::cols(g_, 32 * rb + 16 * u, d, lane), qc = Tile::cols(q_, 32 * rb + 16 * u, d, lane);
-            if constexpr (decltype(careful)::value) {
-              dv[d] = mma_visible<T>(gc, p, on, dv[d]);
-              dk[d] = mma_visible<T>(qc, w, on, dk[d]);
-            } else {
-              dv[d] = N::mma(gc, p, dv[d]);
-              dk[d] = N::mma(qc, w, dk[d]);
-            }
+            for (int d = 0; d < DB; ++d) dv[d] = mma_visible<T>(gc[d], p, on, dv[d]);
+            qcols.template read<32 * rb + 16 * u>(qc, lane);
+#pragma unroll
+            for (int d = 0; d < DB; ++d) dk[d] = mma_visible<T>(qc[d], w, on, dk[d]);
+          } else {
+#pragma unroll
+            for (int d = 0; d < DB; ++d) dv[d] = N::mma(gc[d], p, dv[d]);
+            qcols.template read<32 * rb + 16 * u>(qc, lane);
+#pragma unroll
+            for (int d = 0; d < DB; ++d) dk[d] = N::mma(qc[d], w, dk[d]);
           }
-        }
-      }
+        });
+      });
       if (tn < t_end) keep(st ^ 1);
       t = tn;
       st ^= 1;
