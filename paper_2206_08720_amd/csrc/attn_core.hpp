@@ -76,12 +76,13 @@ struct AttnArgs {
   AttnView q, k, v, o;             // backward: o is read
   AttnView dout, dq, dk, dv;       // backward
   float* lse;                      // [batch, heads, q_len]; may be null in the forward pass
-  const float* delta;              // backward: [batch, heads, q_len]
+  const float *lse2, *delta;       // backward: [batch, heads, q_len]
   const int* lens;                 // [batch] or null
   const int* prefix;               // [batch] or null
   const int* docs;                 // [batch, k_len] or null
   const float* slopes;             // [heads] or null
   float* part;                     // partial results of key (row) ranges
+  int* flags;                      // one a workgroup: its result has to be formed again
   int B, Sq, Sk, H, Hk, G, D;
   int R;                           // Sq * G rows a key/value head
   int tiles, splits;               // row (key) tiles a head, ranges the other axis is cut into
@@ -127,14 +128,26 @@ struct AttnTile {
   }
   __device__ static __forceinline__ int at(int r, int c) { return r * RB + ((c ^ swz(r)) << 4); }
 
-  // rows as the outer axis: elements 16 t + 8 h .. + 7 of row `row` (+ lane % 32)
-  __device__ static __forceinline__ Frag rows(const char* s, int row, int t, int lane) {
-    const int r = row + (lane & 31), h = lane >> 5;
+  // Where a lane's reads start: `r` for rows(), `c` for the transposed ones.  fresh() hides from the compiler that
+  // they stay the same, so that it forms the addresses of a loop's reads (an xor each) where they are used instead
+  // of holding all of them in registers that the accumulators need.
+  struct Lane {
+    uint32_t r, c;
+    __device__ __forceinline__ explicit Lane(int lane) {
+      const int h = lane >> 5, j = lane & 15;
+      r = (uint32_t)at(lane & 31, E == 2 ? h : 2 * h);
+      c = E == 2 ? (uint32_t)at(4 * h + (j >> 2), 2 * ((lane >> 4) & 1) + ((j >> 1) & 1)) + (j & 1) * 8 : (uint32_t)lane;
+    }
+    __device__ __forceinline__ void fresh() { asm volatile("" : "+v"(r), "+v"(c)); }
+  };
+
+  // rows as the outer axis: elements 16 t + 8 h .. + 7 of row `row` (a multiple of 32) + lane % 32
+  __device__ static __forceinline__ Frag rows(const char* s, int row, int t, const Lane& l) {
     if constexpr (E == 2) {
-      return *reinterpret_cast<const Frag*>(s + at(r, 2 * t + h));
+      return *reinterpret_cast<const Frag*>(s + (l.r ^ (uint32_t)(t << 5)) + row * RB);
     } else {
-      const f32x4 lo = *reinterpret_cast<const f32x4*>(s + at(r, 4 * t + 2 * h));
-      const f32x4 hi = *reinterpret_cast<const f32x4*>(s + at(r, 4 * t + 2 * h + 1));
+      const f32x4 lo = *reinterpret_cast<const f32x4*>(s + (l.r ^ (uint32_t)(t << 6)) + row * RB);
+      const f32x4 hi = *reinterpret_cast<const f32x4*>(s + (l.r ^ (uint32_t)((t << 6) | 16)) + row * RB);
       return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
     }
   }
@@ -145,22 +158,45 @@ struct AttnTile {
   struct Cols {
     uint32_t a[E == 2 ? DP / 32 : 1][2];   // byte addresses of the two halves (rows, rows + 8) of each db
     const char* s;
-    __device__ __forceinline__ void set(const char* tile, int lane) {
+    __device__ __forceinline__ void set(const char* tile, const Lane& l) {
       s = tile;
       if constexpr (E == 2) {
-        const int j = lane & 15, r = 4 * (lane >> 5) + (j >> 2), c = 2 * ((lane >> 4) & 1) + ((j >> 1) & 1);
         typedef __attribute__((address_space(3))) const char L;
         const uint32_t base = (uint32_t)(uintptr_t)(L*)tile;
-        const uint32_t o = (uint32_t)at(r, c) + (j & 1) * 8;
 #pragma unroll
         for (int db = 0; db < DP / 32; ++db) {
-          a[db][0] = base + (o ^ (db << 6));
-          a[db][1] = base + ((o ^ (db << 6) ^ 32) + 8 * RB);
+          a[db][0] = base + (l.c ^ (db << 6));
+          a[db][1] = base + ((l.c ^ (db << 6) ^ 32) + 8 * RB);
         }
       }
     }
-    template <int ROW>
-    __device__ __forceinline__ void read(Frag (&f)[DP / 32], int lane) const {
+    // one db
+    template <int ROW, int DBI, int EXTRA = 0>
+    __device__ __forceinline__ Frag read_one(const Lane& l) const {
+      if constexpr (E == 2) {
+        s16x4 lo, hi;
+        asm volatile(
+            "ds_read_b64_tr_b16 %0, %2 offset:%4\n\t"
+            "ds_read_b64_tr_b16 %1, %3 offset:%4\n\t"
+            "s_waitcnt lgkmcnt(0)"
+            : "=&v"(lo), "=&v"(hi)
+            : "v"(a[DBI][0]), "v"(a[DBI][1]), "i"(ROW * RB + EXTRA)
+            : "memory");
+        typedef short s16x8 __attribute__((ext_vector_type(8)));
+        const s16x8 w = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+        return __builtin_bit_cast(Frag, w);
+      } else {
+        const int lane = (int)l.c, h = lane >> 5, d = 32 * DBI + (lane & 31);
+        Frag f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          f[i] = *reinterpret_cast<const float*>(s + EXTRA + at(ROW + 8 * (i >> 2) + 4 * h + (i & 3), d >> 2) + (d & 3) * 4);
+        return f;
+      }
+    }
+    // all of them; EXTRA: bytes from the tile that set() was given
+    template <int ROW, int EXTRA = 0>
+    __device__ __forceinline__ void read(Frag (&f)[DP / 32], const Lane& l) const {
       if constexpr (E == 2) {
         s16x4 v[DP / 32][2];
         if constexpr (DP == 128)
@@ -177,7 +213,7 @@ struct AttnTile {
               : "=&v"(v[0][0]), "=&v"(v[0][1]), "=&v"(v[1][0]), "=&v"(v[1][1]), "=&v"(v[2][0]), "=&v"(v[2][1]), "=&v"(v[3][0]),
                 "=&v"(v[3][1])
               : "v"(a[0][0]), "v"(a[0][1]), "v"(a[1][0]), "v"(a[1][1]), "v"(a[2][0]), "v"(a[2][1]), "v"(a[3][0]), "v"(a[3][1]),
-                "i"(ROW * RB)
+                "i"(ROW * RB + EXTRA)
               : "memory");
         else
           asm volatile(
@@ -187,7 +223,7 @@ struct AttnTile {
               "ds_read_b64_tr_b16 %3, %7 offset:%8\n\t"
               "s_waitcnt lgkmcnt(0)"
               : "=&v"(v[0][0]), "=&v"(v[0][1]), "=&v"(v[1][0]), "=&v"(v[1][1])
-              : "v"(a[0][0]), "v"(a[0][1]), "v"(a[1][0]), "v"(a[1][1]), "i"(ROW * RB)
+              : "v"(a[0][0]), "v"(a[0][1]), "v"(a[1][0]), "v"(a[1][1]), "i"(ROW * RB + EXTRA)
               : "memory");
 #pragma unroll
         for (int db = 0; db < DP / 32; ++db) {
@@ -196,13 +232,13 @@ struct AttnTile {
           f[db] = __builtin_bit_cast(Frag, w);
         }
       } else {
-        const int h = lane >> 5;
+        const int lane = (int)l.c, h = lane >> 5;
 #pragma unroll
         for (int db = 0; db < DP / 32; ++db) {
           const int d = 32 * db + (lane & 31);
 #pragma unroll
           for (int i = 0; i < 8; ++i)
-            f[db][i] = *reinterpret_cast<const float*>(s + at(ROW + 8 * (i >> 2) + 4 * h + (i & 3), d >> 2) + (d & 3) * 4);
+            f[db][i] = *reinterpret_cast<const float*>(s + EXTRA + at(ROW + 8 * (i >> 2) + 4 * h + (i & 3), d >> 2) + (d & 3) * 4);
         }
       }
     }
@@ -229,6 +265,11 @@ __device__ __forceinline__ uint4 load_chunk_elems(const T* row, int d0, int D) {
   uint4 u;
   __builtin_memcpy(&u, e, 16);
   return u;
+}
+
+// One 4-byte load per lane into LDS: lane l's at lds[l].
+__device__ __forceinline__ void buffer_dma4(__amdgpu_buffer_rsrc_t r, uint32_t voff, float* lds) {
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void*)lds, 4, voff, 0, 0, 0);
 }
 
 // Rows into LDS by WAVES waves, 1 KB an instruction.  VEC: 16-byte chunks straight into LDS through a buffer
@@ -382,6 +423,11 @@ __device__ __forceinline__ float tanh_of(float y) {
   return 1.f - 2.f * __builtin_amdgcn_rcpf(exp2_hw(y) + 1.f);
 }
 
+__device__ __forceinline__ void zero16(f32x16& a) {
+#pragma unroll
+  for (int v = 0; v < 16; ++v) a[v] = 0.f;
+}
+
 // ---- operands that are not finite ------------------------------------------------------------------
 // A hidden (row, key) pair has weight 0, and 0 * inf is NaN: where a result comes out not finite, the tile is
 // computed again with this product.  It multiplies the finite elements and adds, as inf, -inf or NaN,
@@ -390,26 +436,46 @@ template <class T>
 __device__ __forceinline__ f32x16 mma_visible(typename Num<T>::Frag a, typename Num<T>::Frag w, typename Num<T>::Frag vis,
                                               f32x16 acc) {
   using Frag = typename Num<T>::Frag;
-  __builtin_amdgcn_sched_barrier(0);   // rarely run: few registers before overlap
-  Frag fin, bad, sgn;
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const float x = (float)a[i];
-    const bool ok = __builtin_isfinite(x);
-    fin[i] = ok ? a[i] : (T)0.f;
-    bad[i] = (T)(ok ? 0.f : 1.f);
-    sgn[i] = (T)(__builtin_isinf(x) ? (x > 0.f ? 1.f : -1.f) : 0.f);
-  }
-  acc = Num<T>::mma(fin, w, acc);
+  // rarely run: few registers before overlap
   f32x16 z;
+  zero16(z);
+  Frag f;
 #pragma unroll
-  for (int v = 0; v < 16; ++v) z[v] = 0.f;
-  const f32x16 n = Num<T>::mma(bad, vis, z), m = Num<T>::mma(sgn, vis, z);
+  for (int i = 0; i < 8; ++i) f[i] = (T)(__builtin_isfinite((float)a[i]) ? 0.f : 1.f);
+  __builtin_amdgcn_sched_barrier(0);
+  z = Num<T>::mma(f, vis, z);               // how many of them an element meets
+  unsigned n[4] = {0, 0, 0, 0};             // at most 16: a byte each
 #pragma unroll
-  for (int v = 0; v < 16; ++v)
-    if (n[v] > 0.f)
-      acc[v] += n[v] == m[v] ? __builtin_inff() : n[v] == -m[v] ? -__builtin_inff() : __builtin_nanf("");
+  for (int v = 0; v < 16; ++v) n[v >> 2] |= (unsigned)z[v] << (8 * (v & 3));
+  __builtin_amdgcn_sched_barrier(0);
+  zero16(z);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) f[i] = (T)(__builtin_isinf((float)a[i]) ? ((float)a[i] > 0.f ? 1.f : -1.f) : 0.f);
+  z = Num<T>::mma(f, vis, z);               // inf counted up, -inf down
+  __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) f[i] = __builtin_isfinite((float)a[i]) ? a[i] : (T)0.f;
+  acc = Num<T>::mma(f, w, acc);
+#pragma unroll
+  for (int v = 0; v < 16; ++v) {
+    const float c = (float)((n[v >> 2] >> (8 * (v & 3))) & 255u);
+    if (c > 0.f) acc[v] += c == z[v] ? __builtin_inff() : c == -z[v] ? -__builtin_inff() : __builtin_nanf("");
+  }
+  __builtin_amdgcn_sched_barrier(0);
   return acc;
+}
+
+// A kernel's body comes in two forms.  The ordinary one leaves a flag where its result has to be formed again; a second
+// launch, of the careful form with mma_visible, takes the flagged blocks.  Both in one kernel measured a third slower
+// with heads of 128: the careful form's registers make the compiler spill in the ordinary loop.
+constexpr int kAgainBlocks = 256;
+template <class Body>
+__device__ __forceinline__ void again(const int* flags, int blocks, Body body) {
+  for (int id = blockIdx.x; id < blocks; id += gridDim.x)
+    if (flags[id]) {
+      body(id);
+      __syncthreads();   // the next one fills the same LDS
+    }
 }
 
 template <int N>
@@ -430,10 +496,6 @@ __device__ __forceinline__ void wait_loads() {
   __builtin_amdgcn_s_waitcnt(0x0F70 | (N & 15) | ((N >> 4) << 14));
 }
 
-__device__ __forceinline__ void zero16(f32x16& a) {
-#pragma unroll
-  for (int v = 0; v < 16; ++v) a[v] = 0.f;
-}
 
 // Blocks are dealt out to the eight dies in turn; this gives each die a contiguous run of the work, so that
 // the tiles that read one head's keys share that die's L2.
@@ -442,38 +504,55 @@ __device__ __forceinline__ int die_order(int id, int n) {
   return die * per + min(die, rest) + k;
 }
 
-// Documents: which of the 64 tiles from `first` hold an id of [lo, hi]; id(t, lane) is the id of the
-// tile's lane-th row or -1.
+// ---- documents: the tiles that can matter ------------------------------------------------------------
+// A tile whose documents all lie outside the range of the owned rows' (keys') is passed over.  Which ones are
+// left is found before the products, 64 tiles a word, the words dealt out to the waves; tiles past the words that
+// LDS holds (2^14 of them) are taken as they come, and the masks decide.
+constexpr int kDocWords = 256;
+
+// One word: which of the n <= 64 tiles hold an id of [lo, hi]; id(t) is the id of this lane's row of tile t, or -1.
+// Sixteen tiles' loads are in flight at a time.
 template <class F>
-__device__ __forceinline__ unsigned long long doc_tiles(int n, int lo, int hi, F id) {
+__device__ __forceinline__ unsigned long long doc_word(int n, int lo, int hi, F id) {
   unsigned long long m = 0;
 #pragma unroll 1
-  for (int t = 0; t < n; ++t) {
-    const int v = id(t);
-    const unsigned long long any = __ballot(v >= lo && v <= hi);
-    m |= (unsigned long long)(any != 0) << t;
+  for (int t = 0; t < n; t += 16) {
+    int v[16];
+#pragma unroll
+    for (int u = 0; u < 16; ++u) v[u] = id(min(t + u, n - 1));
+#pragma unroll
+    for (int u = 0; u < 16; ++u) m |= (unsigned long long)(t + u < n && __ballot(v[u] >= lo && v[u] <= hi) != 0) << (t + u);
   }
   return m;
 }
 
-// Where a tile's keys come from: the active tiles of [t0, t1), in order.
-struct KeyTiles {
-  int t1, lo, hi, len, base, bn;
-  unsigned long long mask;
-  const int* docs;   // of the batch entry, or null
-  __device__ __forceinline__ int from(int t, int lane) {
-    if (!docs) return t;
+// The tiles [t0, t1) of a range, or those of them that hold documents in question.
+struct TileList {
+  int t0, t1;
+  const unsigned long long* words;   // LDS, or null: every tile
+  // fills the words; the caller puts a barrier behind it
+  template <class F>
+  __device__ __forceinline__ void find(unsigned long long* lds, int waves, int wave, int lane, int lo, int hi, F id) {
+    words = lds;
+    const int n = min((t1 - t0 + 63) / 64, kDocWords);
+    for (int w = wave; w < n; w += waves) {
+      const int base = t0 + 64 * w;
+      const unsigned long long m = doc_word(min(64, t1 - base), lo, hi, [&](int k) { return id(base + k); });
+      if (lane == 0) lds[w] = m;
+    }
+  }
+  // the first tile of the list from t on, or t1
+  __device__ __forceinline__ int from(int t) const {
+    if (!words) return t;
+    t = __builtin_amdgcn_readfirstlane(t);
     while (t < t1) {
-      if (base < 0 || t >= base + 64) {
-        base = t;
-        mask = doc_tiles(min(64, t1 - t), lo, hi, [&](int k) {
-          const int j = (t + k) * bn + lane;
-          return lane < bn && j < len ? docs[j] : -1;
-        });
-      }
-      const unsigned long long m = mask >> (t - base);
-      if (m) return t + __builtin_ctzll(m);
-      t = base + 64;
+      const int rel = t - t0, w = rel >> 6;
+      if (w >= kDocWords) return t;
+      const unsigned long long m = words[w] >> (rel & 63);
+      const unsigned lo = __builtin_amdgcn_readfirstlane((unsigned)m), hi = __builtin_amdgcn_readfirstlane((unsigned)(m >> 32));
+      if (lo) return t + __builtin_ctz(lo);
+      if (hi) return t + 32 + __builtin_ctz(hi);
+      t = t0 + 64 * (w + 1);
     }
     return t1;
   }

@@ -34,10 +34,10 @@ struct FwdRows {
   // Scores of a block of 32 keys from `key0` in log2 units (or, where neither a cap nor a slope applies, raw);
   // hidden ones are -inf.  `vis`: bit v for a visible pair.
   __device__ __forceinline__ void scores(const AttnArgs& a, const char* sk, int nb, int key0, const int* ids, bool masked,
-                                         int lane, f32x16& s, unsigned& vis) const {
+                                         int lane, const typename Tile::Lane& tl, f32x16& s, unsigned& vis) const {
     zero16(s);
 #pragma unroll
-    for (int t = 0; t < KT; ++t) s = N::mma(Tile::rows(sk, 32 * nb, t, lane), q[t], s);
+    for (int t = 0; t < KT; ++t) s = N::mma(Tile::rows(sk, 32 * nb, t, tl), q[t], s);
     const int h4 = 4 * (lane >> 5), base = key0 + 32 * nb + h4;
     if (a.cap_in != 0.f) {
 #pragma unroll
@@ -69,11 +69,12 @@ struct FwdRows {
   // A tile of 32 NB keys.  `careful`: with the product that keeps hidden operands out (mma_visible).
   template <int NB, class Careful>
   __device__ __forceinline__ void tile(const AttnArgs& a, const char* sk, const char* sv, const int* ids, int key0, bool masked,
-                                       Careful, int lane) {
+                                       Careful, int lane, typename Tile::Lane& tl) {
+    tl.fresh();
     f32x16 s[NB];
     unsigned vis[NB];
 #pragma unroll
-    for (int nb = 0; nb < NB; ++nb) scores(a, sk, nb, key0, ids, masked, lane, s[nb], vis[nb]);
+    for (int nb = 0; nb < NB; ++nb) scores(a, sk, nb, key0, ids, masked, lane, tl, s[nb], vis[nb]);
     float top = s[0][0];
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb)
@@ -103,21 +104,23 @@ struct FwdRows {
       }
     l += sum;
     typename Tile::Cols vc;
-    vc.set(sv, lane);
+    vc.set(sv, tl);
     unrolled<2 * NB>([&](auto step) {
       constexpr int X = decltype(step)::value, nb = X / 2, u = X % 2;
       const Frag p = to_frag<T>(s[nb], u);
-      Frag vt[DB];
-      vc.template read<16 * X>(vt, lane);
       if constexpr (!Careful::value) {
+        Frag vt[DB];
+        vc.template read<16 * X>(vt, tl);
 #pragma unroll
         for (int d = 0; d < DB; ++d) acc[d] = N::mma(vt[d], p, acc[d]);
       } else {
         Frag w;
 #pragma unroll
         for (int i = 0; i < 8; ++i) w[i] = (T)((vis[nb] >> (8 * u + i)) & 1 ? 1.f : 0.f);
-#pragma unroll
-        for (int d = 0; d < DB; ++d) acc[d] = mma_visible<T>(vt[d], p, w, acc[d]);
+        unrolled<DB>([&](auto block) {
+          constexpr int d = decltype(block)::value;
+          acc[d] = mma_visible<T>(vc.template read_one<16 * X, d>(tl), p, w, acc[d]);
+        });
       }
     });
   }
@@ -154,17 +157,16 @@ template <class T>
 constexpr int kFwdKeys = sizeof(T) == 2 ? 64 : 32;
 constexpr int kFwdRows = 128;
 
-template <class T, int DP, bool VEC>
-__global__ void __launch_bounds__(256, 2) k_attn_fwd(const AttnArgs a) {
+template <class T, int DP, bool VEC, bool CAREFUL>
+__device__ __forceinline__ bool fwd_body(const AttnArgs& a, char* smem, int block, int blocks) {
   constexpr int BN = kFwdKeys<T>;
   using Load = AttnLoad<T, DP, BN, 4, VEC>;
-  extern __shared__ __align__(1024) char smem[];
   char* sk = smem;                                  // [2][BN][DP]
   char* sv = smem + 2 * Load::BYTES;
   int* sids = reinterpret_cast<int*>(smem + 4 * Load::BYTES);   // [2][BN]
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
 
-  int id = die_order(blockIdx.x, gridDim.x);
+  int id = die_order(block, blocks);
   const int split = id % a.splits;
   id /= a.splits;
   const int mt = a.tiles - 1 - id % a.tiles;        // the rows that see most keys first
@@ -176,6 +178,7 @@ __global__ void __launch_bounds__(256, 2) k_attn_fwd(const AttnArgs a) {
   const int* docs = a.docs ? a.docs + (long long)b * a.Sk : nullptr;
 
   FwdRows<T, DP> w;
+  typename AttnTile<T, DP>::Lane tl(lane);
   w.pos = sc.off + i;
   w.klim = sc.klim(w.pos);
   w.doc = docs && w.pos >= 0 ? docs[w.pos] : 0;
@@ -186,21 +189,27 @@ __global__ void __launch_bounds__(256, 2) k_attn_fwd(const AttnArgs a) {
   const int p_lo = sc.off + (int)a.gdiv.div((uint32_t)r0);
   const int p_hi = sc.off + (int)a.gdiv.div((uint32_t)(min(r0 + kFwdRows, a.R) - 1));
   const int all = sc.klim(p_lo), any = sc.klim(p_hi);   // keys that every row sees, that some row sees
-  KeyTiles kt;
   const int nt = (any + BN - 1) / BN, per = (nt + a.splits - 1) / a.splits;
-  int t0 = split * per;
-  kt.t1 = min(nt, t0 + per);
-  kt.len = sc.len;
-  kt.base = -1;
-  kt.bn = BN;
-  kt.docs = docs;
-  if (docs) doc_range(docs, p_lo, p_hi, lane, kt.lo, kt.hi);
+  TileList kt;
+  kt.t0 = split * per;
+  kt.t1 = min(nt, kt.t0 + per);
+  kt.words = nullptr;
+  if (docs) {
+    __shared__ unsigned long long words[kDocWords];
+    int lo, hi;
+    doc_range(docs, p_lo, p_hi, lane, lo, hi);
+    kt.find(words, 4, wave, lane, lo, hi, [&](int t) {
+      const int j = t * BN + lane, d = docs[min(j, sc.len - 1)];
+      return lane < BN && j < sc.len ? d : -1;
+    });
+    __syncthreads();
+  }
   const T* kh = (const T*)a.k.p + b * a.k.sb + hk * a.k.sh;
   const T* vh = (const T*)a.v.p + b * a.v.sb + hk * a.v.sh;
 
   auto pass = [&](auto careful) {
     w.reset();
-    int t = kt.from(t0, lane), st = 0;
+    int t = kt.from(kt.t0), st = 0;
     int nid = -1;
     auto issue = [&](int t, int st) {
       if (docs && tid < BN) nid = t * BN + tid < sc.len ? docs[t * BN + tid] : -1;
@@ -214,20 +223,32 @@ __global__ void __launch_bounds__(256, 2) k_attn_fwd(const AttnArgs a) {
     while (t < kt.t1) {
       __builtin_amdgcn_s_waitcnt(0x0070);   // this wave's part of the tile has landed, and its LDS reads are done
       __syncthreads();
-      const int tn = kt.from(t + 1, lane);
+      const int tn = kt.from(t + 1);
       if (tn < kt.t1) issue(tn, st ^ 1);
       const bool masked = docs || (t + 1) * BN > all;
-      w.template tile<BN / 32>(a, sk + st * Load::BYTES, sv + st * Load::BYTES, sids + st * BN, t * BN, masked, careful, lane);
+      w.template tile<BN / 32>(a, sk + st * Load::BYTES, sv + st * Load::BYTES, sids + st * BN, t * BN, masked, careful, lane, tl);
       if (docs && tn < kt.t1 && tid < BN) sids[(st ^ 1) * BN + tid] = nid;
       t = tn;
       st ^= 1;
     }
   };
-  pass(std::false_type{});
+  pass(std::integral_constant<bool, CAREFUL>{});
   // 0 * inf of a hidden pair (or a visible one): once more, with the product that tells them apart
-  if (__syncthreads_or(not_finite(w.acc))) pass(std::true_type{});
+  if (!CAREFUL && __syncthreads_or(not_finite(w.acc))) return true;
   w.l = half_sum(w.l);
   finish_row<T, DP, VEC>(a, w, b, hk, r, split, lane);
+  return false;
+}
+template <class T, int DP, bool VEC>
+__global__ void __launch_bounds__(256, 2) k_attn_fwd(const AttnArgs a) {
+  extern __shared__ __align__(1024) char smem[];
+  const bool bad = fwd_body<T, DP, VEC, false>(a, smem, blockIdx.x, gridDim.x);
+  if (threadIdx.x == 0) a.flags[blockIdx.x] = bad;
+}
+template <class T, int DP, bool VEC>
+__global__ void __launch_bounds__(256, 1) k_attn_fwd_again(const AttnArgs a, int blocks) {
+  extern __shared__ __align__(1024) char smem[];
+  again(a.flags, blocks, [&](int id) { fwd_body<T, DP, VEC, true>(a, smem, id, blocks); });
 }
 
 // ---- few rows (at most 32 a key/value head: single tokens, short drafts) ---------------------------------
@@ -239,11 +260,10 @@ constexpr int kTokKeys = 32;
 template <class T, int DP>
 constexpr int kTokWaves = kTokKeys * DP * (int)sizeof(T) * 16 <= 128 * 1024 ? 4 : 2;
 
-template <class T, int DP, bool VEC>
-__global__ void __launch_bounds__((64 * kTokWaves<T, DP>), 1) k_attn_tokens(const AttnArgs a) {
+template <class T, int DP, bool VEC, bool CAREFUL>
+__device__ __forceinline__ bool tokens_body(const AttnArgs& a, char* smem) {
   constexpr int BN = kTokKeys, W = kTokWaves<T, DP>;
   using Load = AttnLoad<T, DP, BN, 1, VEC>;
-  extern __shared__ __align__(1024) char smem[];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   char* mine = smem + wave * 4 * Load::BYTES;          // [2][k, v]
   int* ids = reinterpret_cast<int*>(smem + 4 * W * Load::BYTES) + wave * BN;
@@ -258,6 +278,7 @@ __global__ void __launch_bounds__((64 * kTokWaves<T, DP>), 1) k_attn_tokens(cons
   const int* docs = a.docs ? a.docs + (long long)b * a.Sk : nullptr;
 
   FwdRows<T, DP> w;
+  typename AttnTile<T, DP>::Lane tl(lane);
   w.pos = sc.off + i;
   w.klim = sc.klim(w.pos);
   w.doc = docs && w.pos >= 0 ? docs[w.pos] : 0;
@@ -266,21 +287,27 @@ __global__ void __launch_bounds__((64 * kTokWaves<T, DP>), 1) k_attn_tokens(cons
   load_owned<T, DP, VEC>((const T*)a.q.p + b * a.q.sb + i * a.q.ss + (hk * a.G + g) * a.q.sh, r < a.R, a.D, lane, w.q);
 
   const int all = sc.klim(sc.off), any = sc.klim(sc.off + (a.R - 1) / a.G);
-  KeyTiles kt;
   const int nt = (any + BN - 1) / BN, per = (nt + a.splits - 1) / a.splits;
-  const int t0 = split * per;
-  kt.t1 = min(nt, t0 + per);
-  kt.len = sc.len;
-  kt.base = -1;
-  kt.bn = BN;
-  kt.docs = docs;
-  if (docs) doc_range(docs, sc.off, sc.off + (a.R - 1) / a.G, lane, kt.lo, kt.hi);
+  TileList kt;
+  kt.t0 = split * per;
+  kt.t1 = min(nt, kt.t0 + per);
+  kt.words = nullptr;
+  if (docs) {
+    __shared__ unsigned long long words[kDocWords];
+    int lo, hi;
+    doc_range(docs, sc.off, sc.off + (a.R - 1) / a.G, lane, lo, hi);
+    kt.find(words, W, wave, lane, lo, hi, [&](int t) {
+      const int j = t * BN + lane, d = docs[min(j, sc.len - 1)];
+      return lane < BN && j < sc.len ? d : -1;
+    });
+    __syncthreads();
+  }
   const T* kh = (const T*)a.k.p + b * a.k.sb + hk * a.k.sh;
   const T* vh = (const T*)a.v.p + b * a.v.sb + hk * a.v.sh;
 
   auto next = [&](int t) {       // the next of this wave's tiles: every W-th, documents skipped over
-    t = kt.from(t, lane);
-    while (t < kt.t1 && ((t - t0) & (W - 1)) != wave) t = kt.from(t + 1, lane);
+    t = kt.from(t);
+    while (t < kt.t1 && ((t - kt.t0) & (W - 1)) != wave) t = kt.from(t + 1);
     return t;
   };
   auto pass = [&](auto careful) {
@@ -290,7 +317,7 @@ __global__ void __launch_bounds__((64 * kTokWaves<T, DP>), 1) k_attn_tokens(cons
       Load::positions(kh, a.k.ss, t * BN, sc.len, a.D, s, 0, lane);
       Load::positions(vh, a.v.ss, t * BN, sc.len, a.D, s + Load::BYTES, 0, lane);
     };
-    int t = next(t0), st = 0;
+    int t = next(kt.t0), st = 0;
     if (t < kt.t1) issue(t, 0);
     while (t < kt.t1) {
       const int tn = next(t + 1);
@@ -305,7 +332,7 @@ __global__ void __launch_bounds__((64 * kTokWaves<T, DP>), 1) k_attn_tokens(cons
       __builtin_amdgcn_wave_barrier();
       __builtin_amdgcn_sched_barrier(0);
       const char* s = mine + st * 2 * Load::BYTES;
-      w.template tile<1>(a, s, s + Load::BYTES, ids, t * BN, masked, careful, lane);
+      w.template tile<1>(a, s, s + Load::BYTES, ids, t * BN, masked, careful, lane, tl);
       __builtin_amdgcn_s_waitcnt(0xC07F);   // this wave's LDS reads are done: the stage may be filled again
       __builtin_amdgcn_wave_barrier();
       __builtin_amdgcn_sched_barrier(0);
@@ -314,8 +341,8 @@ __global__ void __launch_bounds__((64 * kTokWaves<T, DP>), 1) k_attn_tokens(cons
       st ^= 1;
     }
   };
-  pass(std::false_type{});
-  if (__any(not_finite(w.acc))) pass(std::true_type{});
+  pass(std::integral_constant<bool, CAREFUL>{});
+  if (!CAREFUL && __syncthreads_or(not_finite(w.acc))) return true;
   w.l = half_sum(w.l);
 
   // the waves' states, one after the other, into the first one's
@@ -332,7 +359,7 @@ __global__ void __launch_bounds__((64 * kTokWaves<T, DP>), 1) k_attn_tokens(cons
     sml[(wave - 1) * 128 + 64 + lane] = w.l;
   }
   __syncthreads();
-  if (wave) return;
+  if (wave) return false;
   const float unit = a.cap_in != 0.f || a.slopes ? 1.f : a.c;
 #pragma unroll 1
   for (int o = 0; o < W - 1; ++o) {
@@ -348,6 +375,12 @@ __global__ void __launch_bounds__((64 * kTokWaves<T, DP>), 1) k_attn_tokens(cons
       for (int v = 0; v < 16; ++v) w.acc[db][v] = w.acc[db][v] * f0 + d[(db * 16 + v) * 64 + lane] * f1;
   }
   finish_row<T, DP, VEC>(a, w, b, hk, r, split, lane);
+  return false;
+}
+template <class T, int DP, bool VEC>
+__global__ void __launch_bounds__((64 * kTokWaves<T, DP>), 1) k_attn_tokens(const AttnArgs a) {
+  extern __shared__ __align__(1024) char smem[];
+  if (tokens_body<T, DP, VEC, false>(a, smem)) tokens_body<T, DP, VEC, true>(a, smem);
 }
 
 // ---- the ranges of a row, joined -----------------------------------------------------------------------
@@ -384,7 +417,13 @@ hipError_t run_fwd(hipStream_t s, const AttnArgs& a, bool tokens) {
     constexpr int bytes = 4 * AttnLoad<T, DP, kFwdKeys<T>, 4, VEC>::BYTES + 2 * kFwdKeys<T> * 4;
     const hipError_t e = hipFuncSetAttribute((const void*)k_attn_fwd<T, DP, VEC>, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
     if (e != hipSuccess) return e;
-    k_attn_fwd<T, DP, VEC><<<dim3(a.B * a.Hk * a.tiles * a.splits), dim3(256), bytes, s>>>(a);
+    const int blocks = a.B * a.Hk * a.tiles * a.splits;
+    k_attn_fwd<T, DP, VEC><<<dim3(blocks), dim3(256), bytes, s>>>(a);
+    const hipError_t e1 = hipGetLastError();
+    if (e1 != hipSuccess) return e1;
+    const hipError_t e2 = hipFuncSetAttribute((const void*)k_attn_fwd_again<T, DP, VEC>, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (e2 != hipSuccess) return e2;
+    k_attn_fwd_again<T, DP, VEC><<<dim3(std::min(blocks, kAgainBlocks)), dim3(256), bytes, s>>>(a, blocks);
   }
   hipError_t e = hipGetLastError();
   if (e == hipSuccess && a.splits > 1) {
@@ -413,6 +452,7 @@ AttnPlan attn_plan_fwd(int B, int Hk, int R, int Sk, int D) {
   if (!p.tokens && blocks >= 192) p.splits = 1;   // the join's traffic would cost more than idle units do
   const int dp = D <= 64 ? 64 : 128;
   p.part_floats = p.splits > 1 ? (long long)p.splits * B * Hk * R * (dp + 2) : 0;
+  p.flag_ints = p.tokens ? 0 : blocks * p.splits;
   return p;
 }
 

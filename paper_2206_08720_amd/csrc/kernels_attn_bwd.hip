@@ -12,34 +12,48 @@
 namespace ntk {
 namespace {
 
-// p and ds of 16 (row, key) pairs of a lane: `s` the raw products q k, `dp` the products dout v.  In: hidden pairs
-// as cleared bits of vis.  dist(v): |position - key| for the slope.
+// p and ds of 16 (row, key) pairs of a lane: `s` the raw products q k, `dp` the products dout v.  dist(v): |position -
+// key| for the slope.
 template <class T, class L, class Dl, class Sl, class Dist>
-__device__ __forceinline__ void weights(const AttnArgs& a, f32x16& s, f32x16& dp, unsigned vis, L lse2, Dl delta, Sl slope2,
-                                        Dist dist) {
+__device__ __forceinline__ void weights(const AttnArgs& a, f32x16& s, f32x16& dp, L lse2, Dl delta, Sl slope2, Dist dist) {
+  if (a.cap_in != 0.f || a.slopes) {
+#pragma unroll
+    for (int v = 0; v < 16; ++v) {
+      float x = s[v], fac = 1.f;
+      if (a.cap_in != 0.f) {
+        const float t = tanh_of<T>(x * a.cap_in);
+        fac = 1.f - t * t;
+        x = a.cap_out * t;
+      } else {
+        x *= a.c;
+      }
+      if (a.slopes) x -= slope2(v) * dist(v);
+      s[v] = exp2_hw(x - lse2(v));
+      dp[v] = s[v] * (dp[v] - delta(v)) * fac;
+      if (v % 4 == 3) __builtin_amdgcn_sched_barrier(0);   // the rows' numbers four at a time: registers are short
+    }
+    return;
+  }
 #pragma unroll
   for (int v = 0; v < 16; ++v) {
-    float x = s[v], fac = 1.f;
-    if (a.cap_in != 0.f) {
-      const float t = tanh_of<T>(x * a.cap_in);
-      fac = 1.f - t * t;
-      x = a.cap_out * t;
-    } else {
-      x *= a.c;
-    }
-    if (a.slopes) x -= slope2(v) * dist(v);
-    const float p = exp2_hw(x - lse2(v));
+    s[v] = exp2_hw(fmaf(s[v], a.c, -lse2(v)));
+    dp[v] = s[v] * (dp[v] - delta(v));
+  }
+}
+// the hidden ones (cleared bits of vis) are zero, whatever their operands held
+__device__ __forceinline__ void hide(f32x16& s, f32x16& dp, unsigned vis) {
+#pragma unroll
+  for (int v = 0; v < 16; ++v) {
     const bool on = (vis >> v) & 1;
-    s[v] = on ? p : 0.f;
-    dp[v] = on ? p * (dp[v] - delta(v)) * fac : 0.f;
+    s[v] = on ? s[v] : 0.f;
+    dp[v] = on ? dp[v] : 0.f;
   }
 }
 
-// delta of a row; rows that see nothing (lse = -inf) get weights 0 through lse2 = inf.
-__device__ __forceinline__ float lse_units(float lse) { return lse == -__builtin_inff() ? __builtin_inff() : lse * kLog2e; }
-
+// delta, and lse in units of log2; a row that sees nothing (lse = -inf) gets weights 0 through inf.
 template <class T>
-__global__ void __launch_bounds__(256) k_attn_delta(const AttnArgs a, float* __restrict__ delta, long long rows) {
+__global__ void __launch_bounds__(256) k_attn_delta(const AttnArgs a, float* __restrict__ lse2, float* __restrict__ delta,
+                                                    long long rows) {
   // 16 lanes a row (b, i, head)
   const int lane = threadIdx.x & 15;
   const long long id = (long long)blockIdx.x * 16 + (threadIdx.x >> 4);
@@ -53,7 +67,12 @@ __global__ void __launch_bounds__(256) k_attn_delta(const AttnArgs a, float* __r
   for (int d = lane; d < a.D; d += 16) s = fmaf((float)o[d], (float)g[d], s);
 #pragma unroll
   for (int w = 8; w; w >>= 1) s += __shfl_xor(s, w);
-  if (lane == 0) delta[((long long)b * a.H + head) * a.Sq + i] = s;
+  if (lane) return;
+  const long long at = ((long long)b * a.H + head) * a.Sq + i;
+  const float l = a.lse[at];
+  const bool empty = l == -__builtin_inff();
+  lse2[at] = empty ? __builtin_inff() : l * kLog2e;
+  delta[at] = empty ? 0.f : s;
 }
 
 // ---- dq: four waves of 32 rows over the key tiles -----------------------------------------------------
@@ -61,20 +80,21 @@ template <class T>
 constexpr int kBwdKeys = sizeof(T) == 2 ? 64 : 32;
 constexpr int kBwdRows = 128;
 
-template <class T, int DP, bool VEC>
-__global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) k_attn_dq(const AttnArgs a) {
+template <class T, int DP, bool VEC, bool CAREFUL>
+__device__ __forceinline__ bool dq_body(const AttnArgs& a, char* smem, int block, int blocks) {
   constexpr int BN = kBwdKeys<T>, KT = DP / 16, DB = DP / 32;
   using N = Num<T>;
   using Tile = AttnTile<T, DP>;
   using Frag = typename N::Frag;
   using Load = AttnLoad<T, DP, BN, 4, VEC>;
-  extern __shared__ __align__(1024) char smem[];
   char* sk = smem;
   char* sv = smem + 2 * Load::BYTES;
   int* sids = reinterpret_cast<int*>(smem + 4 * Load::BYTES);
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
 
-  int id = die_order(blockIdx.x, gridDim.x);
+  int id = die_order(block, blocks);
+  const int split = id % a.splits;
+  id /= a.splits;
   const int mt = a.tiles - 1 - id % a.tiles;
   id /= a.tiles;
   const int hk = id % a.Hk, b = id / a.Hk;
@@ -87,7 +107,7 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) k_attn_dq(const A
   const int klim = doc < 0 ? 0 : sc.klim(pos);
   const float slope2 = a.slopes ? a.slopes[head] * kLog2e : 0.f;
   const long long stat = ((long long)b * a.H + head) * a.Sq + i;
-  const float lse2 = r < a.R ? lse_units(a.lse[stat]) : __builtin_inff();
+  const float lse2 = a.lse2[stat];
   const float delta = a.delta[stat];
   Frag q[KT], g[KT];
   load_owned<T, DP, VEC>((const T*)a.q.p + b * a.q.sb + i * a.q.ss + head * a.q.sh, r < a.R, a.D, lane, q);
@@ -96,21 +116,30 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) k_attn_dq(const A
   const int p_lo = sc.off + (int)a.gdiv.div((uint32_t)r0);
   const int p_hi = sc.off + (int)a.gdiv.div((uint32_t)(min(r0 + kBwdRows, a.R) - 1));
   const int all = sc.klim(p_lo), any = sc.klim(p_hi);
-  KeyTiles kt;
-  kt.t1 = (any + BN - 1) / BN;
-  kt.len = sc.len;
-  kt.base = -1;
-  kt.bn = BN;
-  kt.docs = docs;
-  if (docs) doc_range(docs, p_lo, p_hi, lane, kt.lo, kt.hi);
+  const int nt = (any + BN - 1) / BN, per = (nt + a.splits - 1) / a.splits;
+  TileList kt;
+  kt.t0 = split * per;
+  kt.t1 = min(nt, kt.t0 + per);
+  kt.words = nullptr;
+  if (docs) {
+    __shared__ unsigned long long words[kDocWords];
+    int lo, hi;
+    doc_range(docs, p_lo, p_hi, lane, lo, hi);
+    kt.find(words, 4, wave, lane, lo, hi, [&](int t) {
+      const int j = t * BN + lane, d = docs[min(j, sc.len - 1)];
+      return lane < BN && j < sc.len ? d : -1;
+    });
+    __syncthreads();
+  }
   const T* kh = (const T*)a.k.p + b * a.k.sb + hk * a.k.sh;
   const T* vh = (const T*)a.v.p + b * a.v.sb + hk * a.v.sh;
 
+  typename Tile::Lane tl(lane);
   f32x16 acc[DB];
   auto pass = [&](auto careful) {
 #pragma unroll
     for (int d = 0; d < DB; ++d) zero16(acc[d]);
-    int t = kt.from(0, lane), st = 0, nid = -1;
+    int t = kt.from(kt.t0), st = 0, nid = -1;
     auto issue = [&](int t, int st) {
       if (docs && tid < BN) nid = t * BN + tid < sc.len ? docs[t * BN + tid] : -1;
       Load::positions(kh, a.k.ss, t * BN, sc.len, a.D, sk + st * Load::BYTES, wave, lane);
@@ -123,12 +152,13 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) k_attn_dq(const A
     while (t < kt.t1) {
       __builtin_amdgcn_s_waitcnt(0x0070);
       __syncthreads();
-      const int tn = kt.from(t + 1, lane);
+      const int tn = kt.from(t + 1);
       if (tn < kt.t1) issue(tn, st ^ 1);
       const bool masked = docs || (t + 1) * BN > all;
+      tl.fresh();
       const char *k_ = sk + st * Load::BYTES, *v_ = sv + st * Load::BYTES;
       typename Tile::Cols cols;
-      cols.set(k_, lane);
+      cols.set(k_, tl);
       unrolled<BN / 32>([&](auto block) {
         constexpr int nb = decltype(block)::value;
         f32x16 s, dp;
@@ -136,8 +166,9 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) k_attn_dq(const A
         zero16(dp);
 #pragma unroll
         for (int x = 0; x < KT; ++x) {
-          s = N::mma(Tile::rows(k_, 32 * nb, x, lane), q[x], s);
-          dp = N::mma(Tile::rows(v_, 32 * nb, x, lane), g[x], dp);
+          s = N::mma(Tile::rows(k_, 32 * nb, x, tl), q[x], s);
+          dp = N::mma(Tile::rows(v_, 32 * nb, x, tl), g[x], dp);
+          if (x % 2) __builtin_amdgcn_sched_barrier(0);
         }
         const int h4 = 4 * (lane >> 5), base = t * BN + 32 * nb + h4;
         unsigned vis = 0xffffu;
@@ -151,20 +182,23 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) k_attn_dq(const A
               if (sids[st * BN + 32 * nb + h4 + 8 * (v >> 2) + (v & 3)] != doc) vis &= ~(1u << v);
           }
         }
-        weights<T>(a, s, dp, vis, [&](int) { return lse2; }, [&](int) { return delta; }, [&](int) { return slope2; },
+        weights<T>(a, s, dp, [&](int) { return lse2; }, [&](int) { return delta; }, [&](int) { return slope2; },
                    [&](int v) { return (float)abs(pos - (base + 8 * (v >> 2) + (v & 3))); });
+        if (masked) hide(s, dp, vis);
         unrolled<2>([&](auto step) {
           constexpr int u = decltype(step)::value;
           const Frag w = to_frag<T>(dp, u);
-          Frag kc[DB];
-          cols.template read<32 * nb + 16 * u>(kc, lane);
           if constexpr (decltype(careful)::value) {
             Frag on;
 #pragma unroll
             for (int e = 0; e < 8; ++e) on[e] = (T)((vis >> (8 * u + e)) & 1 ? 1.f : 0.f);
-#pragma unroll
-            for (int d = 0; d < DB; ++d) acc[d] = mma_visible<T>(kc[d], w, on, acc[d]);
+            unrolled<DB>([&](auto db) {
+              constexpr int d = decltype(db)::value;
+              acc[d] = mma_visible<T>(cols.template read_one<32 * nb + 16 * u, d>(tl), w, on, acc[d]);
+            });
           } else {
+            Frag kc[DB];
+            cols.template read<32 * nb + 16 * u>(kc, tl);
 #pragma unroll
             for (int d = 0; d < DB; ++d) acc[d] = N::mma(kc[d], w, acc[d]);
           }
@@ -175,80 +209,93 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) k_attn_dq(const A
       st ^= 1;
     }
   };
-  pass(std::false_type{});
-  if (__syncthreads_or(not_finite(acc))) pass(std::true_type{});
-  if (r < a.R)
+  pass(std::integral_constant<bool, CAREFUL>{});
+  if (!CAREFUL && __syncthreads_or(not_finite(acc))) return true;
+  if (r >= a.R) return false;
+  if (a.splits > 1)
+    store_owned<float, DP, true>(a.part + (((long long)split * a.B * a.Hk + (long long)b * a.Hk + hk) * a.R + r) * DP, DP, lane, acc, 1.f);
+  else
     store_owned<T, DP, VEC>((T*)a.dq.p + b * a.dq.sb + i * a.dq.ss + head * a.dq.sh, a.D, lane, acc, a.scale);
+  return false;
+}
+template <class T, int DP, bool VEC>
+__global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) k_attn_dq(const AttnArgs a) {
+  extern __shared__ __align__(1024) char smem[];
+  const bool bad = dq_body<T, DP, VEC, false>(a, smem, blockIdx.x, gridDim.x);
+  if (threadIdx.x == 0) a.flags[blockIdx.x] = bad;
 }
 
 // ---- dk, dv: four waves of 32 keys over the row tiles -----------------------------------------------------
-template <class T>
-constexpr int kBwdRowTile = sizeof(T) == 2 ? 64 : 32;
+// A wave's keys stay in registers and its values in LDS: with both in registers (and dk, dv in 128 more) only one
+// wave a SIMD would fit, and nothing would run beside its MFMAs.
+constexpr int kBwdRowTile = 32;
 constexpr int kBwdKeyTile = 128;
 
 // What a tile of rows brings along, in LDS.
-template <int BR>
 struct RowStats {
-  float lse2[BR], delta[BR], slope2[BR];
-  int klim[BR], pos[BR], doc[BR];
+  float lse2[64], delta[64];         // a wave's worth: loaded straight into LDS, the first kBwdRowTile count
+  float slope2[kBwdRowTile];
+  int klim[kBwdRowTile], pos[kBwdRowTile], doc[kBwdRowTile];
 };
 
-template <class T, int DP, bool VEC>
-__global__ void __launch_bounds__(256, 1) k_attn_dkv(const AttnArgs a) {
-  constexpr int BR = kBwdRowTile<T>, KT = DP / 16, DB = DP / 32;
+template <class T, int DP, bool VEC, bool CAREFUL>
+__device__ __forceinline__ bool dkv_body(const AttnArgs& a, char* smem, int block, int blocks) {
+  constexpr int BR = kBwdRowTile, KT = DP / 16, DB = DP / 32;
   using N = Num<T>;
   using Tile = AttnTile<T, DP>;
   using Frag = typename N::Frag;
   using Load = AttnLoad<T, DP, BR, 4, VEC>;
-  extern __shared__ __align__(1024) char smem[];
-  char* sq = smem;
+  using LoadV = AttnLoad<T, DP, kBwdKeyTile, 4, VEC>;
+  char* sq = smem;                                   // [2][BR][DP]
   char* sg = smem + 2 * Load::BYTES;
-  RowStats<BR>* stats = reinterpret_cast<RowStats<BR>*>(smem + 4 * Load::BYTES);   // [2]
+  char* sv = smem + 4 * Load::BYTES;                 // [128][DP]
+  RowStats* stats = reinterpret_cast<RowStats*>(sv + LoadV::BYTES);   // [2]
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
 
-  int id = die_order(blockIdx.x, gridDim.x);
-  const int k0 = (id % a.tiles) * kBwdKeyTile;       // the keys that most rows see first
-  id /= a.tiles;
-  const int hk = id % a.Hk, b = id / a.Hk;
+  int id = die_order(block, blocks);
+  const int split = id % a.splits;
+  id /= a.splits;
+  // A causal tile's work falls with its place.  Neighbouring heads run through the tiles in opposite directions, so
+  // that the two workgroups of a compute unit come to the same sum.
+  const int tile = id % a.tiles, bh = id / a.tiles;
+  const int k0 = (bh & 1 ? a.tiles - 1 - tile : tile) * kBwdKeyTile;
+  const int hk = bh % a.Hk, b = bh / a.Hk;
   const AttnScope sc(a, b);
   const int j = k0 + wave * 32 + (lane & 31), jc = min(j, a.Sk - 1);
   const int* docs = a.docs ? a.docs + (long long)b * a.Sk : nullptr;
   const bool live = j < sc.len;
   const int doc = docs ? (live ? docs[jc] : -1) : 0;
-  Frag k[KT], vv[KT];
+  Frag k[KT];
   load_owned<T, DP, VEC>((const T*)a.k.p + b * a.k.sb + jc * a.k.ss + hk * a.k.sh, live, a.D, lane, k);
-  load_owned<T, DP, VEC>((const T*)a.v.p + b * a.v.sb + jc * a.v.ss + hk * a.v.sh, live, a.D, lane, vv);
+  if (k0 < sc.len)
+    LoadV::positions((const T*)a.v.p + b * a.v.sb + hk * a.v.sh, a.v.ss, k0, sc.len, a.D, sv, wave, lane);
 
   // the first query that sees one of the keys: positions below 0 do not exist
   int i0 = max(0, -sc.off);
   if (sc.causal && sc.prefix <= k0) i0 = max(i0, k0 - sc.off);
-  const int nr = (a.R + BR - 1) / BR;
-  const int t_end = k0 < sc.len && i0 < a.Sq ? nr : 0;
-  int lo = 0x7fffffff, hi = -1;                       // the keys' documents
-  if (docs) doc_range(docs, k0, min(k0 + kBwdKeyTile, sc.len) - 1, lane, lo, hi);
-  int base = -1;
-  unsigned long long mask = 0;
-  auto from = [&](int t) {                            // the next row tile with one of them
-    if (!docs) return t;
-    while (t < t_end) {
-      if (base < 0 || t >= base + 64) {
-        base = t;
-        mask = doc_tiles(min(64, t_end - t), lo, hi, [&](int x) {
-          const int r = (t + x) * BR + lane;
-          if (lane >= BR || r >= a.R) return -1;
-          const int p = sc.off + (int)a.gdiv.div((uint32_t)r);
-          return p >= 0 ? docs[p] : -1;
-        });
-      }
-      const unsigned long long m = mask >> (t - base);
-      if (m) return t + (int)__builtin_ctzll(m);
-      t = base + 64;
-    }
-    return t_end;
-  };
+  const int all_t = k0 < sc.len && i0 < a.Sq ? (a.R + BR - 1) / BR : 0;
+  const int first = min((int)((long long)i0 * a.G / BR), all_t), per = (all_t - first + a.splits - 1) / a.splits;
+  TileList rt;
+  rt.t0 = __builtin_amdgcn_readfirstlane(first + split * per);
+  rt.t1 = __builtin_amdgcn_readfirstlane(min(all_t, first + split * per + per));
+  rt.words = nullptr;
+  if (docs) {
+    __shared__ unsigned long long words[kDocWords];
+    int lo, hi;                                       // the keys' documents
+    doc_range(docs, k0, min(k0 + kBwdKeyTile, sc.len) - 1, lane, lo, hi);
+    rt.find(words, 4, wave, lane, lo, hi, [&](int t) {
+      const int r = t * BR + lane, p = sc.off + (int)a.gdiv.div((uint32_t)min(r, a.R - 1)), d = docs[max(p, 0)];
+      return lane < BR && r < a.R && p >= 0 ? d : -1;
+    });
+    __syncthreads();
+  }
   const T* qh = (const T*)a.q.p + b * a.q.sb + (long long)hk * a.G * a.q.sh;
   const T* gh = (const T*)a.dout.p + b * a.dout.sb + (long long)hk * a.G * a.dout.sh;
 
+  const long long stat = ((long long)b * a.H + (long long)hk * a.G) * a.Sq;   // [group][q_len] of this head
+  const auto lse_rs = buffer_rsrc(a.lse2 + stat, (uint32_t)a.R * 4u), delta_rs = buffer_rsrc(a.delta + stat, (uint32_t)a.R * 4u);
+
+  typename Tile::Lane tl(lane);
   f32x16 dk[DB], dv[DB];
   auto pass = [&](auto careful) {
 #pragma unroll
@@ -256,148 +303,256 @@ __global__ void __launch_bounds__(256, 1) k_attn_dkv(const AttnArgs a) {
       zero16(dk[d]);
       zero16(dv[d]);
     }
-    float n_lse = 0.f, n_delta = 0.f, n_slope = 0.f;
-    int n_klim = 0, n_pos = 0, n_doc = 0;
     auto issue = [&](int t, int st) {
-      if (tid < BR) {
-        const int r = t * BR + tid, rc = min(r, a.R - 1);
-        const int i = (int)a.gdiv.div((uint32_t)rc), head = hk * a.G + rc - i * a.G;
-        const long long stat = ((long long)b * a.H + head) * a.Sq + i;
-        n_pos = sc.off + i;
-        n_doc = docs && n_pos >= 0 ? docs[n_pos] : 0;
-        n_klim = r < a.R && n_doc >= 0 ? sc.klim(n_pos) : 0;
-        n_lse = a.lse[stat];
-        n_delta = a.delta[stat];
-        if (a.slopes) n_slope = a.slopes[head];
-      }
+      int lane = tid & 63;
+      asm volatile("" : "+v"(lane));   // the places are formed here, not held over the products
       Load::packed(qh, a.q.ss, a.q.sh, t * BR, a.R, a.gdiv, a.D, sq + st * Load::BYTES, wave, lane);
       Load::packed(gh, a.dout.ss, a.dout.sh, t * BR, a.R, a.gdiv, a.D, sg + st * Load::BYTES, wave, lane);
-    };
-    auto keep = [&](int st) {
-      if (tid < BR) {
-        stats[st].lse2[tid] = n_klim > 0 ? lse_units(n_lse) : __builtin_inff();   // rows past the last: weight 0
-        stats[st].delta[tid] = n_klim > 0 ? n_delta : 0.f;
-        stats[st].slope2[tid] = n_slope * kLog2e;
-        stats[st].klim[tid] = n_klim;
-        stats[st].pos[tid] = n_pos;
-        stats[st].doc[tid] = n_doc;
+      if (wave == 0) {   // rows past the last read zeros: their operands are zero too
+        const int r = t * BR + lane, i = (int)a.gdiv.div((uint32_t)r), g = r - i * a.G;
+        const uint32_t off = lane < BR && r < a.R ? (uint32_t)((g * a.Sq + i) * 4) : 0x80000000u;
+        buffer_dma4(lse_rs, off, stats[st].lse2);
+        buffer_dma4(delta_rs, off, stats[st].delta);
       }
     };
-    int t = from((int)((long long)i0 * a.G / BR)), st = 0;
-    if (t < t_end) {
+    // what only masks and slopes ask for, formed after the tile before
+    auto keep = [&](int t, int st) {
+      if (tid < BR) {
+        const int rc = min(t * BR + tid, a.R - 1), i = (int)a.gdiv.div((uint32_t)rc), pos = sc.off + i;
+        const int d = docs && pos >= 0 ? docs[pos] : 0;
+        stats[st].slope2[tid] = a.slopes ? a.slopes[hk * a.G + rc - i * a.G] * kLog2e : 0.f;
+        stats[st].klim[tid] = d >= 0 ? sc.klim(pos) : 0;
+        stats[st].pos[tid] = pos;
+        stats[st].doc[tid] = d;
+      }
+    };
+    int t = rt.from(rt.t0), st = 0;
+    if (t < rt.t1) {
       issue(t, 0);
-      keep(0);
+      keep(t, 0);
     }
-    while (t < t_end) {
+    while (t < rt.t1) {
       __builtin_amdgcn_s_waitcnt(0x0070);
       __syncthreads();
-      const int tn = from(t + 1);
-      if (tn < t_end) issue(tn, st ^ 1);
+      const int tn = rt.from(t + 1);
+      if (tn < rt.t1) issue(tn, st ^ 1);
       const int p_first = sc.off + (int)a.gdiv.div((uint32_t)(t * BR));
       const bool masked = docs || k0 + kBwdKeyTile > sc.klim(p_first);
+      tl.fresh();
       const char *q_ = sq + st * Load::BYTES, *g_ = sg + st * Load::BYTES;
-      const RowStats<BR>& rs = stats[st];
-      typename Tile::Cols gcols, qcols;
-      gcols.set(g_, lane);
-      qcols.set(q_, lane);
-      unrolled<BR / 32>([&](auto block) {
-        constexpr int rb = decltype(block)::value;
-        f32x16 s, dp;
-        zero16(s);
-        zero16(dp);
+      const RowStats& rs = stats[st];
+      f32x16 s, dp;
+      zero16(s);
+      zero16(dp);
 #pragma unroll
-        for (int x = 0; x < KT; ++x) {
-          s = N::mma(Tile::rows(q_, 32 * rb, x, lane), k[x], s);
-          dp = N::mma(Tile::rows(g_, 32 * rb, x, lane), vv[x], dp);
+      for (int x = 0; x < KT; ++x) {
+        s = N::mma(Tile::rows(q_, 0, x, tl), k[x], s);
+        dp = N::mma(Tile::rows(g_, 0, x, tl), Tile::rows(sv, 32 * wave, x, tl), dp);
+        if (x % 2) __builtin_amdgcn_sched_barrier(0);   // no more fragments in flight than the accumulators leave room for
+      }
+      const int rr = 4 * (lane >> 5);
+      auto at = [&](int v) { return rr + 8 * (v >> 2) + (v & 3); };
+      weights<T>(a, s, dp, [&](int v) { return rs.lse2[at(v)]; }, [&](int v) { return rs.delta[at(v)]; },
+                 [&](int v) { return rs.slope2[at(v)]; }, [&](int v) { return (float)abs(rs.pos[at(v)] - j); });
+      unsigned vis = 0xffffu;
+      if (masked) {
+#pragma unroll
+        for (int v = 0; v < 16; ++v) {
+          if (j >= rs.klim[at(v)]) vis &= ~(1u << v);
+          if (v % 4 == 3) __builtin_amdgcn_sched_barrier(0);
         }
-        const int rr = 32 * rb + 4 * (lane >> 5);
-        auto at = [&](int v) { return rr + 8 * (v >> 2) + (v & 3); };
-        unsigned vis = 0xffffu;
-        if (masked) {
+        if (docs) {
 #pragma unroll
-          for (int v = 0; v < 16; ++v)
-            if (j >= rs.klim[at(v)]) vis &= ~(1u << v);
-          if (docs) {
-#pragma unroll
-            for (int v = 0; v < 16; ++v)
-              if (rs.doc[at(v)] != doc) vis &= ~(1u << v);
+          for (int v = 0; v < 16; ++v) {
+            if (rs.doc[at(v)] != doc) vis &= ~(1u << v);
+            if (v % 4 == 3) __builtin_amdgcn_sched_barrier(0);
           }
         }
-        weights<T>(a, s, dp, vis, [&](int v) { return rs.lse2[at(v)]; }, [&](int v) { return rs.delta[at(v)]; },
-                   [&](int v) { return rs.slope2[at(v)]; }, [&](int v) { return (float)abs(rs.pos[at(v)] - j); });
-        unrolled<2>([&](auto step) {
-          constexpr int u = decltype(step)::value;
-          const Frag p = to_frag<T>(s, u), w = to_frag<T>(dp, u);
+        hide(s, dp, vis);
+      }
+      constexpr int GQ = 2 * Load::BYTES;                // from the tile of q to that of dout
+      typename Tile::Cols qcols;
+      qcols.set(q_, tl);
+      const Frag pf[2] = {to_frag<T>(s, 0), to_frag<T>(s, 1)}, wf[2] = {to_frag<T>(dp, 0), to_frag<T>(dp, 1)};
+      __builtin_amdgcn_sched_barrier(0);
+      unrolled<2>([&](auto step) {
+        constexpr int u = decltype(step)::value;
+        const Frag p = pf[u], w = wf[u];
+        if constexpr (decltype(careful)::value) {
+          Frag on;
+#pragma unroll
+          for (int e = 0; e < 8; ++e) on[e] = (T)((vis >> (8 * u + e)) & 1 ? 1.f : 0.f);
+          unrolled<DB>([&](auto db) {
+            constexpr int d = decltype(db)::value;
+            dv[d] = mma_visible<T>(qcols.template read_one<16 * u, d, GQ>(tl), p, on, dv[d]);
+            dk[d] = mma_visible<T>(qcols.template read_one<16 * u, d>(tl), w, on, dk[d]);
+          });
+        } else {
           Frag gc[DB], qc[DB];
-          gcols.template read<32 * rb + 16 * u>(gc, lane);
-          if constexpr (decltype(careful)::value) {
-            Frag on;
+          qcols.template read<16 * u, GQ>(gc, tl);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) on[e] = (T)((vis >> (8 * u + e)) & 1 ? 1.f : 0.f);
+          for (int d = 0; d < DB; ++d) dv[d] = N::mma(gc[d], p, dv[d]);
+          __builtin_amdgcn_sched_barrier(0);   // these products run while the next fragments are read
+          qcols.template read<16 * u>(qc, tl);
 #pragma unroll
-            for (int d = 0; d < DB; ++d) dv[d] = mma_visible<T>(gc[d], p, on, dv[d]);
-            qcols.template read<32 * rb + 16 * u>(qc, lane);
-#pragma unroll
-            for (int d = 0; d < DB; ++d) dk[d] = mma_visible<T>(qc[d], w, on, dk[d]);
-          } else {
-#pragma unroll
-            for (int d = 0; d < DB; ++d) dv[d] = N::mma(gc[d], p, dv[d]);
-            qcols.template read<32 * rb + 16 * u>(qc, lane);
-#pragma unroll
-            for (int d = 0; d < DB; ++d) dk[d] = N::mma(qc[d], w, dk[d]);
-          }
-        });
+          for (int d = 0; d < DB; ++d) dk[d] = N::mma(qc[d], w, dk[d]);
+          __builtin_amdgcn_sched_barrier(0);
+        }
       });
-      if (tn < t_end) keep(st ^ 1);
+      if (tn < rt.t1) keep(tn, st ^ 1);
       t = tn;
       st ^= 1;
     }
   };
-  pass(std::false_type{});
-  if (__syncthreads_or(not_finite(dk) || not_finite(dv))) pass(std::true_type{});
-  if (j < a.Sk) {   // keys past the batch entry's length get zeros
-    store_owned<T, DP, VEC>((T*)a.dk.p + b * a.dk.sb + j * a.dk.ss + hk * a.dk.sh, a.D, lane, dk, a.scale);
-    store_owned<T, DP, VEC>((T*)a.dv.p + b * a.dv.sb + j * a.dv.ss + hk * a.dv.sh, a.D, lane, dv, 1.f);
+  pass(std::integral_constant<bool, CAREFUL>{});
+  if (!CAREFUL && __syncthreads_or(not_finite(dk) || not_finite(dv))) return true;
+  if (j >= a.Sk) return false;
+  if (a.splits > 1) {
+    const long long keys = (long long)a.B * a.Hk * a.Sk, row = (long long)bh * a.Sk + j;
+    store_owned<float, DP, true>(a.part + ((long long)split * keys + row) * DP, DP, lane, dk, 1.f);
+    store_owned<float, DP, true>(a.part + ((long long)(a.splits + split) * keys + row) * DP, DP, lane, dv, 1.f);
+    return false;
   }
+  // keys past the batch entry's length get zeros
+  store_owned<T, DP, VEC>((T*)a.dk.p + b * a.dk.sb + j * a.dk.ss + hk * a.dk.sh, a.D, lane, dk, a.scale);
+  store_owned<T, DP, VEC>((T*)a.dv.p + b * a.dv.sb + j * a.dv.ss + hk * a.dv.sh, a.D, lane, dv, 1.f);
+  return false;
+}
+template <class T, int DP, bool VEC>
+__global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) k_attn_dkv(const AttnArgs a) {
+  extern __shared__ __align__(1024) char smem[];
+  const bool bad = dkv_body<T, DP, VEC, false>(a, smem, blockIdx.x, gridDim.x);
+  if (threadIdx.x == 0) a.flags[blockIdx.x] = bad;
 }
 
 template <class T, int DP, bool VEC>
-hipError_t run_bwd(hipStream_t s, AttnArgs& a) {
-  {
-    constexpr int bytes = 4 * AttnLoad<T, DP, kBwdKeys<T>, 4, VEC>::BYTES + 2 * kBwdKeys<T> * 4;
-    a.tiles = (a.R + kBwdRows - 1) / kBwdRows;
-    const hipError_t e = hipFuncSetAttribute((const void*)k_attn_dq<T, DP, VEC>, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
-    if (e != hipSuccess) return e;
-    if (a.tiles) k_attn_dq<T, DP, VEC><<<dim3(a.B * a.Hk * a.tiles), dim3(256), bytes, s>>>(a);
+__global__ void __launch_bounds__(256, 1) k_attn_dq_again(const AttnArgs a, int blocks) {
+  extern __shared__ __align__(1024) char smem[];
+  again(a.flags, blocks, [&](int id) { dq_body<T, DP, VEC, true>(a, smem, id, blocks); });
+}
+template <class T, int DP, bool VEC>
+__global__ void __launch_bounds__(256, 1) k_attn_dkv_again(const AttnArgs a, int blocks) {
+  extern __shared__ __align__(1024) char smem[];
+  again(a.flags, blocks, [&](int id) { dkv_body<T, DP, VEC, true>(a, smem, id, blocks); });
+}
+
+// ---- the ranges' partial sums, added in order -------------------------------------------------------------
+// y[row] = f sum_s part[s][row]; a row is a position of a key/value head (gdiv.d = 1), or a packed query row.
+template <class T, int DP>
+__global__ void __launch_bounds__(256) k_attn_sum(const float* __restrict__ part, AttnView y, FastDiv gdiv, int heads, int per_head,
+                                                  long long rows, int D, int splits, float f) {
+  constexpr int TPR = DP / 4;
+  const long long row = (long long)blockIdx.x * (256 / TPR) + threadIdx.x / TPR;
+  if (row >= rows) return;
+  const int d = (threadIdx.x % TPR) * 4;
+  f32x4 x = *reinterpret_cast<const f32x4*>(part + row * DP + d);
+#pragma unroll 4
+  for (int s = 1; s < splits; ++s) {
+    const f32x4 z = *reinterpret_cast<const f32x4*>(part + ((long long)s * rows + row) * DP + d);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] += z[i];
   }
-  {
-    constexpr int BR = kBwdRowTile<T>;
-    constexpr int bytes = 4 * AttnLoad<T, DP, BR, 4, VEC>::BYTES + 2 * (int)sizeof(RowStats<BR>);
-    a.tiles = (a.Sk + kBwdKeyTile - 1) / kBwdKeyTile;
-    const hipError_t e = hipFuncSetAttribute((const void*)k_attn_dkv<T, DP, VEC>, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
-    if (e != hipSuccess) return e;
-    if (a.tiles) k_attn_dkv<T, DP, VEC><<<dim3(a.B * a.Hk * a.tiles), dim3(256), bytes, s>>>(a);
-  }
+  const long long bh = row / per_head;
+  const int r = (int)(row - bh * per_head), hk = (int)(bh % heads), b = (int)(bh / heads);
+  const int i = (int)gdiv.div((uint32_t)r), head = hk * (int)gdiv.d + r - i * (int)gdiv.d;
+  T* o = (T*)y.p + b * y.sb + i * y.ss + head * y.sh;
+#pragma unroll
+  for (int e = 0; e < 4; ++e)
+    if (d + e < D) o[d + e] = (T)(x[e] * f);
+}
+
+template <class T, int DP>
+hipError_t run_sum(hipStream_t s, const AttnArgs& a, const float* part, const AttnView& y, const FastDiv& g, int per_head, int splits,
+                   float f) {
+  const long long rows = (long long)a.B * a.Hk * per_head;
+  constexpr int rpb = 256 / (DP / 4);
+  k_attn_sum<T, DP><<<dim3((unsigned)((rows + rpb - 1) / rpb)), dim3(256), 0, s>>>(part, y, g, a.Hk, per_head, rows, a.D, splits, f);
   return hipGetLastError();
 }
 
+// `k` on `blocks` workgroups, then `k_again` on those it flagged
+template <class K, class A>
+hipError_t run_twice(hipStream_t s, const AttnArgs& a, K k, A k_again, int bytes) {
+  const int blocks = a.B * a.Hk * a.tiles * a.splits;
+  hipError_t e = hipFuncSetAttribute((const void*)k, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+  if (e == hipSuccess) e = hipFuncSetAttribute((const void*)k_again, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+  if (e != hipSuccess) return e;
+  k<<<dim3(blocks), dim3(256), bytes, s>>>(a);
+  if ((e = hipGetLastError()) != hipSuccess) return e;
+  k_again<<<dim3(std::min(blocks, kAgainBlocks)), dim3(256), bytes, s>>>(a, blocks);
+  return hipGetLastError();
+}
+
+template <class T, int DP, bool VEC>
+hipError_t run_bwd(hipStream_t s, AttnArgs& a, const AttnBwdPlan& plan) {
+  if (plan.dq_tiles) {
+    constexpr int bytes = 4 * AttnLoad<T, DP, kBwdKeys<T>, 4, VEC>::BYTES + 2 * kBwdKeys<T> * 4;
+    a.tiles = plan.dq_tiles;
+    a.splits = plan.dq_splits;
+    hipError_t e = run_twice(s, a, k_attn_dq<T, DP, VEC>, k_attn_dq_again<T, DP, VEC>, bytes);
+    if (e == hipSuccess && a.splits > 1) e = run_sum<T, DP>(s, a, a.part, a.dq, a.gdiv, a.R, a.splits, a.scale);
+    if (e != hipSuccess) return e;
+  }
+  if (plan.dkv_tiles) {
+    constexpr int bytes = 4 * AttnLoad<T, DP, kBwdRowTile, 4, VEC>::BYTES + AttnLoad<T, DP, kBwdKeyTile, 4, VEC>::BYTES + 2 * (int)sizeof(RowStats);
+    a.tiles = plan.dkv_tiles;
+    a.splits = plan.dkv_splits;
+    hipError_t e = run_twice(s, a, k_attn_dkv<T, DP, VEC>, k_attn_dkv_again<T, DP, VEC>, bytes);
+    if (e == hipSuccess && a.splits > 1) {
+      const FastDiv one(1);
+      e = run_sum<T, DP>(s, a, a.part, a.dk, one, a.Sk, a.splits, a.scale);
+      if (e == hipSuccess) e = run_sum<T, DP>(s, a, a.part + (long long)a.splits * a.B * a.Hk * a.Sk * DP, a.dv, one, a.Sk, a.splits, 1.f);
+    }
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
+}
+
 template <class T>
-hipError_t run_bwd_dim(hipStream_t s, AttnArgs& a, float* delta, bool vec) {
+hipError_t run_bwd_dim(hipStream_t s, AttnArgs& a, const AttnBwdPlan& plan, float* work, bool vec) {
   const long long rows = (long long)a.B * a.Sq * a.H;
-  if (rows) k_attn_delta<T><<<dim3((unsigned)((rows + 15) / 16)), dim3(256), 0, s>>>(a, delta, rows);
+  float* lse2 = work + plan.part_floats;
+  float* delta = lse2 + rows;
+  if (rows) k_attn_delta<T><<<dim3((unsigned)((rows + 15) / 16)), dim3(256), 0, s>>>(a, lse2, delta, rows);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
+  a.lse2 = lse2;
   a.delta = delta;
-  if (a.D <= 64) return vec ? run_bwd<T, 64, true>(s, a) : run_bwd<T, 64, false>(s, a);
-  return vec ? run_bwd<T, 128, true>(s, a) : run_bwd<T, 128, false>(s, a);
+  a.part = work;
+  a.flags = reinterpret_cast<int*>(delta + rows);   // one after the other on the stream
+  if (a.D <= 64) return vec ? run_bwd<T, 64, true>(s, a, plan) : run_bwd<T, 64, false>(s, a, plan);
+  return vec ? run_bwd<T, 128, true>(s, a, plan) : run_bwd<T, 128, false>(s, a, plan);
+}
+
+// Ranges of the summed axis: where the tiles are too few for two workgroups on each of 256 compute units, the
+// axis is cut so that there are, into ranges of at least 256 keys or rows.
+int ranges(long long blocks, long long axis) {
+  if (blocks >= 256) return 1;   // the partial sums' traffic would cost more than it gains
+  return (int)std::max(1LL, std::min((512 + blocks - 1) / blocks, axis / 256));
 }
 
 }  // namespace
 
-hipError_t launch_attn_bwd(hipStream_t s, int dtype, AttnArgs& a, float* delta, bool vec) {
-  if (dtype == 1) return run_bwd_dim<__bf16>(s, a, delta, vec);
-  if (dtype == 2) return run_bwd_dim<_Float16>(s, a, delta, vec);
-  return run_bwd_dim<float>(s, a, delta, vec);
+AttnBwdPlan attn_plan_bwd(int B, int Hk, int R, int Sk, int D) {
+  AttnBwdPlan p{};
+  const int dp = D <= 64 ? 64 : 128;
+  const long long bh = (long long)B * Hk;
+  p.dq_splits = p.dkv_splits = 1;
+  if (bh == 0) return p;
+  p.dq_tiles = (R + kBwdRows - 1) / kBwdRows;
+  p.dkv_tiles = (Sk + kBwdKeyTile - 1) / kBwdKeyTile;
+  if (p.dq_tiles) p.dq_splits = ranges(bh * p.dq_tiles, Sk);
+  if (p.dkv_tiles) p.dkv_splits = ranges(bh * p.dkv_tiles, R);
+  const long long dq = p.dq_splits > 1 ? p.dq_splits * bh * R * dp : 0, dkv = p.dkv_splits > 1 ? 2 * p.dkv_splits * bh * Sk * dp : 0;
+  p.flag_ints = bh * std::max(p.dq_tiles * p.dq_splits, p.dkv_tiles * p.dkv_splits);
+  p.part_floats = std::max(dq, dkv);   // one after the other on the stream
+  return p;
+}
+
+hipError_t launch_attn_bwd(hipStream_t s, int dtype, AttnArgs& a, const AttnBwdPlan& plan, float* work, bool vec) {
+  if (dtype == 1) return run_bwd_dim<__bf16>(s, a, plan, work, vec);
+  if (dtype == 2) return run_bwd_dim<_Float16>(s, a, plan, work, vec);
+  return run_bwd_dim<float>(s, a, plan, work, vec);
 }
 
 }  // namespace ntk

@@ -62,18 +62,24 @@ int attn_args(const ntk_attention_desc* d, AttnPlan* plan) {
   if (d->prefix && !d->causal) return bad(NTK_E_ARG, "attention: a prefix needs causal");
   // rows and grids are 32-bit; a margin for the last tile
   const long long G = d->heads / d->kv_heads, R = (long long)d->q_len * G, bh = (long long)d->batch * d->kv_heads;
-  if (R >= (1LL << 31) - 1024 || d->k_len >= (1LL << 31) - 1024 || bh >= (1LL << 31))
-    return bad(NTK_E_UNSUPPORTED, "attention: q_len * group or k_len reaches 2^31");
+  if (R >= (1LL << 29) - 1024 || d->k_len >= (1LL << 31) - 1024 || bh >= (1LL << 31))
+    return bad(NTK_E_UNSUPPORTED, "attention: q_len * group reaches 2^29 or k_len 2^31");
   if (R > 0 && bh > 0) {
     *plan = attn_plan_fwd(d->batch, d->kv_heads, (int)R, d->k_len, d->head_dim);
-    const long long tiles = plan->tokens ? 1 : plan->tiles, k_tiles = (d->k_len + 127) / 128;
-    if (!grid_ok(bh * tiles * plan->splits, 256) || !grid_ok(bh * ((R + 127) / 128), 256) || !grid_ok(bh * k_tiles, 256) ||
-        !grid_ok((bh * R + 15) / 16, 256) || (plan->splits > 1 && !grid_ok(bh * R, 128)))
+    const long long tiles = plan->tokens ? 1 : plan->tiles;
+    const AttnBwdPlan back = attn_plan_bwd(d->batch, d->kv_heads, (int)R, d->k_len, d->head_dim);
+    if (!grid_ok(bh * tiles * plan->splits, 256) || !grid_ok(bh * back.dq_tiles * back.dq_splits, 256) ||
+        !grid_ok(bh * back.dkv_tiles * back.dkv_splits, 256) || !grid_ok((bh * R + 3) / 4, 256) || !grid_ok((bh * d->k_len + 3) / 4, 256) ||
+        (plan->splits > 1 && !grid_ok(bh * R, 128)))
       return bad(NTK_E_UNSUPPORTED, "attention: too many rows for one launch");
   } else {
     *plan = AttnPlan{};
   }
   return NTK_OK;
+}
+
+AttnBwdPlan bwd_plan(const ntk_attention_desc* d) {
+  return attn_plan_bwd(d->batch, d->kv_heads, d->q_len * (d->heads / d->kv_heads), d->k_len, d->head_dim);
 }
 
 void set_view(AttnView& to, const ntk_view* v) {
@@ -233,8 +239,9 @@ extern "C" int ntk_rotary(int dtype, int batch, int length, int q_heads, int k_h
 extern "C" long long ntk_attention_workspace(const ntk_attention_desc* desc, int backward) {
   AttnPlan plan;
   if (int rc = attn_args(desc, &plan)) return rc;
-  if (backward) return (long long)desc->batch * desc->heads * desc->q_len * 4;
-  return plan.part_floats * 4;
+  if (!backward) return (plan.part_floats + plan.flag_ints) * 4;
+  const AttnBwdPlan back = bwd_plan(desc);
+  return (back.part_floats + back.flag_ints + 2 * (long long)desc->batch * desc->heads * desc->q_len) * 4;
 }
 
 extern "C" int ntk_attention(const ntk_attention_desc* desc, const ntk_view* q, const ntk_view* k, const ntk_view* v,
@@ -247,7 +254,8 @@ extern "C" int ntk_attention(const ntk_attention_desc* desc, const ntk_view* q, 
     return bad(NTK_E_ARG, "attention: a view is missing, unaligned or has a negative stride");
   if (!aligned(lse, 4) || !aligned(desc->k_lens, 4) || !aligned(desc->prefix, 4) || !aligned(desc->docs, 4) || !aligned(desc->slopes, 4))
     return bad(NTK_E_ARG, "attention: a pointer is not aligned to its type");
-  if (plan.part_floats && (!workspace || !whole16(workspace) || workspace_bytes < plan.part_floats * 4))
+  const long long need = (plan.part_floats + plan.flag_ints) * 4;
+  if (need && (!workspace || !whole16(workspace) || workspace_bytes < need))
     return bad(NTK_E_ARG, "attention: the workspace is missing, unaligned or too small");
   AttnArgs a{};
   set_desc(a, desc);
@@ -261,6 +269,7 @@ extern "C" int ntk_attention(const ntk_attention_desc* desc, const ntk_view* q, 
   }
   a.lse = lse;
   a.part = (float*)workspace;
+  a.flags = (int*)workspace + plan.part_floats;
   a.tiles = plan.tiles;
   a.splits = plan.splits;
   const hipError_t err = launch_attn_fwd((hipStream_t)hip_stream, desc->dtype, a, plan.tokens, vec);
@@ -301,6 +310,6 @@ extern "C" int ntk_attention_bwd(const ntk_attention_desc* desc, const ntk_view*
     set_view(a.dv, dv);
   }
   a.lse = const_cast<float*>(lse);
-  const hipError_t err = launch_attn_bwd((hipStream_t)hip_stream, desc->dtype, a, (float*)workspace, vec);
+  const hipError_t err = launch_attn_bwd((hipStream_t)hip_stream, desc->dtype, a, bwd_plan(desc), (float*)workspace, vec);
   return err == hipSuccess ? NTK_OK : hip_bad(err);
 }
