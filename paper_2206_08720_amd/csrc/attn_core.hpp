@@ -89,7 +89,7 @@ struct AttnArgs {
   int causal;
   float scale;                     // of the raw product
   float c;                         // scale * log2(e)
-  float cap_in, cap_out;           // softcap > 0: 2 log2(e) scale / cap and cap log2(e); else 0
+  float cap_in, cap_out, cap_inv;  // softcap > 0: 2 log2(e) scale / cap, cap log2(e) and 1 / (cap log2(e)); else 0
   FastDiv gdiv;
 };
 
@@ -415,12 +415,12 @@ __device__ __forceinline__ float half_sum(float x) {
 
 __device__ __forceinline__ float exp2_hw(float x) { return __builtin_amdgcn_exp2f(x); }
 
-// tanh(x) for y = 2 log2(e) x: 1 - 2 / (2^y + 1), absolute error a few 2^-24 (2^y = inf gives 1).  fp32
-// takes the library's tanhf, whose relative error holds near zero too.
+// The capped score in log2 units, cap log2(e) tanh(scale x / cap), with tanh(y) = 1 - 2 / (e^2y + 1): an absolute
+// error of a few 2^-24 cap (e^2y = inf gives 1).  fp32 takes the library's tanhf, whose relative error holds near zero too.
 template <class T>
-__device__ __forceinline__ float tanh_of(float y) {
-  if constexpr (sizeof(T) == 4) return tanhf(y * (0.5f / kLog2e));
-  return 1.f - 2.f * __builtin_amdgcn_rcpf(exp2_hw(y) + 1.f);
+__device__ __forceinline__ float capped(const AttnArgs& a, float x) {
+  if constexpr (sizeof(T) == 4) return a.cap_out * tanhf(x * a.cap_in * (0.5f / kLog2e));
+  return fmaf(-2.f * a.cap_out, __builtin_amdgcn_rcpf(exp2_hw(x * a.cap_in) + 1.f), a.cap_out);
 }
 
 __device__ __forceinline__ void zero16(f32x16& a) {
@@ -497,11 +497,19 @@ __device__ __forceinline__ void wait_loads() {
 }
 
 
-// Blocks are dealt out to the eight dies in turn; this gives each die a contiguous run of the work, so that
-// the tiles that read one head's keys share that die's L2.
-__device__ __forceinline__ int die_order(int id, int n) {
-  const int per = n >> 3, rest = n & 7, die = id & 7, k = id >> 3;
-  return die * per + min(die, rest) + k;
+// Workgroup -> (batch entry and key/value head, item of it).  Workgroups are dealt out to the eight dies in turn, so
+// heads go by the number modulo 8 where they divide evenly: the tiles that read one head's keys then share a die's
+// L2.  All heads' first items come first, and the kernels put the tiles with most work there, so that the last
+// ones to run are short.
+__device__ __forceinline__ void place(int block, int heads, int& bh, int& item) {
+  if (heads % 8 == 0) {
+    const int m = heads / 8, k = block >> 3;
+    item = k / m;
+    bh = (block & 7) * m + k - item * m;
+  } else {
+    item = block / heads;
+    bh = block - item * heads;
+  }
 }
 
 // ---- documents: the tiles that can matter ------------------------------------------------------------

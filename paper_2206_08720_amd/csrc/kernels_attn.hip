@@ -32,7 +32,8 @@ struct FwdRows {
   }
 
   // Scores of a block of 32 keys from `key0` in log2 units (or, where neither a cap nor a slope applies, raw);
-  // hidden ones are -inf.  `vis`: bit v for a visible pair.
+  // hidden ones are -inf.  Careful: `vis` gets bit v for a visible pair.
+  template <class Careful>
   __device__ __forceinline__ void scores(const AttnArgs& a, const char* sk, int nb, int key0, const int* ids, bool masked,
                                          int lane, const typename Tile::Lane& tl, f32x16& s, unsigned& vis) const {
     zero16(s);
@@ -41,7 +42,7 @@ struct FwdRows {
     const int h4 = 4 * (lane >> 5), base = key0 + 32 * nb + h4;
     if (a.cap_in != 0.f) {
 #pragma unroll
-      for (int v = 0; v < 16; ++v) s[v] = a.cap_out * tanh_of<T>(s[v] * a.cap_in);
+      for (int v = 0; v < 16; ++v) s[v] = capped<T>(a, s[v]);
     } else if (a.slopes) {
 #pragma unroll
       for (int v = 0; v < 16; ++v) s[v] *= a.c;
@@ -50,19 +51,26 @@ struct FwdRows {
 #pragma unroll
       for (int v = 0; v < 16; ++v) s[v] -= slope2 * (float)abs(pos - (base + 8 * (v >> 2) + (v & 3)));
     }
-    vis = 0xffffu;
     if (masked) {
       const int left = klim - base;
-#pragma unroll
-      for (int v = 0; v < 16; ++v)
-        if (8 * (v >> 2) + (v & 3) >= left) vis &= ~(1u << v);
-      if (a.docs) {
+      if constexpr (Careful::value) {
+        vis = 0xffffu;
 #pragma unroll
         for (int v = 0; v < 16; ++v)
-          if (ids[32 * nb + h4 + 8 * (v >> 2) + (v & 3)] != doc) vis &= ~(1u << v);
+          if (8 * (v >> 2) + (v & 3) >= left || (a.docs && ids[32 * nb + h4 + 8 * (v >> 2) + (v & 3)] != doc)) vis &= ~(1u << v);
       }
+      if (a.docs) {
 #pragma unroll
-      for (int v = 0; v < 16; ++v) s[v] = (vis >> v) & 1 ? s[v] : -__builtin_inff();
+        for (int v = 0; v < 16; ++v) {
+          const int k = 8 * (v >> 2) + (v & 3);
+          s[v] = k < left && ids[32 * nb + h4 + k] == doc ? s[v] : -__builtin_inff();
+        }
+      } else {
+#pragma unroll
+        for (int v = 0; v < 16; ++v) s[v] = 8 * (v >> 2) + (v & 3) < left ? s[v] : -__builtin_inff();
+      }
+    } else if (Careful::value) {
+      vis = 0xffffu;
     }
   }
 
@@ -74,7 +82,7 @@ struct FwdRows {
     f32x16 s[NB];
     unsigned vis[NB];
 #pragma unroll
-    for (int nb = 0; nb < NB; ++nb) scores(a, sk, nb, key0, ids, masked, lane, tl, s[nb], vis[nb]);
+    for (int nb = 0; nb < NB; ++nb) scores<Careful>(a, sk, nb, key0, ids, masked, lane, tl, s[nb], vis[nb]);
     float top = s[0][0];
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb)
@@ -158,7 +166,7 @@ constexpr int kFwdKeys = sizeof(T) == 2 ? 64 : 32;
 constexpr int kFwdRows = 128;
 
 template <class T, int DP, bool VEC, bool CAREFUL>
-__device__ __forceinline__ bool fwd_body(const AttnArgs& a, char* smem, int block, int blocks) {
+__device__ __forceinline__ bool fwd_body(const AttnArgs& a, char* smem, int block) {
   constexpr int BN = kFwdKeys<T>;
   using Load = AttnLoad<T, DP, BN, 4, VEC>;
   char* sk = smem;                                  // [2][BN][DP]
@@ -166,12 +174,10 @@ __device__ __forceinline__ bool fwd_body(const AttnArgs& a, char* smem, int bloc
   int* sids = reinterpret_cast<int*>(smem + 4 * Load::BYTES);   // [2][BN]
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
 
-  int id = die_order(block, blocks);
-  const int split = id % a.splits;
-  id /= a.splits;
-  const int mt = a.tiles - 1 - id % a.tiles;        // the rows that see most keys first
-  id /= a.tiles;
-  const int hk = id % a.Hk, b = id / a.Hk;
+  int bh, item;
+  place(block, a.B * a.Hk, bh, item);
+  const int split = item % a.splits, mt = a.tiles - 1 - item / a.splits;   // the rows that see most keys first
+  const int hk = bh % a.Hk, b = bh / a.Hk;
   const AttnScope sc(a, b);
   const int r0 = mt * kFwdRows, r = r0 + wave * 32 + (lane & 31);
   const int i = (int)a.gdiv.div((uint32_t)min(r, a.R - 1)), g = min(r, a.R - 1) - i * a.G;
@@ -182,6 +188,7 @@ __device__ __forceinline__ bool fwd_body(const AttnArgs& a, char* smem, int bloc
   w.pos = sc.off + i;
   w.klim = sc.klim(w.pos);
   w.doc = docs && w.pos >= 0 ? docs[w.pos] : 0;
+  const bool one = __all(w.doc >= 0 && w.doc == __builtin_amdgcn_readfirstlane(w.doc));   // this wave's rows: one document
   if (w.doc < 0) w.klim = 0;
   w.slope2 = a.slopes ? a.slopes[hk * a.G + g] * kLog2e : 0.f;
   load_owned<T, DP, VEC>((const T*)a.q.p + b * a.q.sb + i * a.q.ss + (hk * a.G + g) * a.q.sh, r < a.R, a.D, lane, w.q);
@@ -199,8 +206,8 @@ __device__ __forceinline__ bool fwd_body(const AttnArgs& a, char* smem, int bloc
     int lo, hi;
     doc_range(docs, p_lo, p_hi, lane, lo, hi);
     kt.find(words, 4, wave, lane, lo, hi, [&](int t) {
-      const int j = t * BN + lane, d = docs[min(j, sc.len - 1)];
-      return lane < BN && j < sc.len ? d : -1;
+      const int j = t * BN + lane % BN, d = docs[min(j, sc.len - 1)];
+      return j < sc.len ? d : -1;
     });
     __syncthreads();
   }
@@ -225,7 +232,7 @@ __device__ __forceinline__ bool fwd_body(const AttnArgs& a, char* smem, int bloc
       __syncthreads();
       const int tn = kt.from(t + 1);
       if (tn < kt.t1) issue(tn, st ^ 1);
-      const bool masked = docs || (t + 1) * BN > all;
+      const bool masked = (t + 1) * BN > all || (docs && !(one && __all(sids[st * BN + lane % BN] == w.doc)));
       w.template tile<BN / 32>(a, sk + st * Load::BYTES, sv + st * Load::BYTES, sids + st * BN, t * BN, masked, careful, lane, tl);
       if (docs && tn < kt.t1 && tid < BN) sids[(st ^ 1) * BN + tid] = nid;
       t = tn;
@@ -242,13 +249,13 @@ __device__ __forceinline__ bool fwd_body(const AttnArgs& a, char* smem, int bloc
 template <class T, int DP, bool VEC>
 __global__ void __launch_bounds__(256, 2) k_attn_fwd(const AttnArgs a) {
   extern __shared__ __align__(1024) char smem[];
-  const bool bad = fwd_body<T, DP, VEC, false>(a, smem, blockIdx.x, gridDim.x);
+  const bool bad = fwd_body<T, DP, VEC, false>(a, smem, blockIdx.x);
   if (threadIdx.x == 0) a.flags[blockIdx.x] = bad;
 }
 template <class T, int DP, bool VEC>
 __global__ void __launch_bounds__(256, 1) k_attn_fwd_again(const AttnArgs a, int blocks) {
   extern __shared__ __align__(1024) char smem[];
-  again(a.flags, blocks, [&](int id) { fwd_body<T, DP, VEC, true>(a, smem, id, blocks); });
+  again(a.flags, blocks, [&](int id) { fwd_body<T, DP, VEC, true>(a, smem, id); });
 }
 
 // ---- few rows (at most 32 a key/value head: single tokens, short drafts) ---------------------------------
@@ -268,10 +275,9 @@ __device__ __forceinline__ bool tokens_body(const AttnArgs& a, char* smem) {
   char* mine = smem + wave * 4 * Load::BYTES;          // [2][k, v]
   int* ids = reinterpret_cast<int*>(smem + 4 * W * Load::BYTES) + wave * BN;
 
-  int id = die_order(blockIdx.x, gridDim.x);
-  const int split = id % a.splits;
-  id /= a.splits;
-  const int hk = id % a.Hk, b = id / a.Hk;
+  int bh, split;
+  place(blockIdx.x, a.B * a.Hk, bh, split);
+  const int hk = bh % a.Hk, b = bh / a.Hk;
   const AttnScope sc(a, b);
   const int r = lane & 31;
   const int i = (int)a.gdiv.div((uint32_t)min(r, a.R - 1)), g = min(r, a.R - 1) - i * a.G;
@@ -297,8 +303,8 @@ __device__ __forceinline__ bool tokens_body(const AttnArgs& a, char* smem) {
     int lo, hi;
     doc_range(docs, sc.off, sc.off + (a.R - 1) / a.G, lane, lo, hi);
     kt.find(words, W, wave, lane, lo, hi, [&](int t) {
-      const int j = t * BN + lane, d = docs[min(j, sc.len - 1)];
-      return lane < BN && j < sc.len ? d : -1;
+      const int j = t * BN + lane % BN, d = docs[min(j, sc.len - 1)];
+      return j < sc.len ? d : -1;
     });
     __syncthreads();
   }

@@ -21,9 +21,9 @@ __device__ __forceinline__ void weights(const AttnArgs& a, f32x16& s, f32x16& dp
     for (int v = 0; v < 16; ++v) {
       float x = s[v], fac = 1.f;
       if (a.cap_in != 0.f) {
-        const float t = tanh_of<T>(x * a.cap_in);
-        fac = 1.f - t * t;
-        x = a.cap_out * t;
+        x = capped<T>(a, x);
+        const float t = x * a.cap_inv;
+        fac = fmaf(-t, t, 1.f);
       } else {
         x *= a.c;
       }
@@ -81,7 +81,7 @@ constexpr int kBwdKeys = sizeof(T) == 2 ? 64 : 32;
 constexpr int kBwdRows = 128;
 
 template <class T, int DP, bool VEC, bool CAREFUL>
-__device__ __forceinline__ bool dq_body(const AttnArgs& a, char* smem, int block, int blocks) {
+__device__ __forceinline__ bool dq_body(const AttnArgs& a, char* smem, int block) {
   constexpr int BN = kBwdKeys<T>, KT = DP / 16, DB = DP / 32;
   using N = Num<T>;
   using Tile = AttnTile<T, DP>;
@@ -92,18 +92,17 @@ __device__ __forceinline__ bool dq_body(const AttnArgs& a, char* smem, int block
   int* sids = reinterpret_cast<int*>(smem + 4 * Load::BYTES);
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
 
-  int id = die_order(block, blocks);
-  const int split = id % a.splits;
-  id /= a.splits;
-  const int mt = a.tiles - 1 - id % a.tiles;
-  id /= a.tiles;
-  const int hk = id % a.Hk, b = id / a.Hk;
+  int bh, item;
+  place(block, a.B * a.Hk, bh, item);
+  const int split = item % a.splits, mt = a.tiles - 1 - item / a.splits;   // the rows that see most keys first
+  const int hk = bh % a.Hk, b = bh / a.Hk;
   const AttnScope sc(a, b);
   const int r0 = mt * kBwdRows, r = r0 + wave * 32 + (lane & 31), rc = min(r, a.R - 1);
   const int i = (int)a.gdiv.div((uint32_t)rc), head = hk * a.G + rc - i * a.G;
   const int* docs = a.docs ? a.docs + (long long)b * a.Sk : nullptr;
   const int pos = sc.off + i;
   const int doc = docs && pos >= 0 ? docs[pos] : 0;
+  const bool one = __all(doc >= 0 && doc == __builtin_amdgcn_readfirstlane(doc));   // this wave's rows: one document
   const int klim = doc < 0 ? 0 : sc.klim(pos);
   const float slope2 = a.slopes ? a.slopes[head] * kLog2e : 0.f;
   const long long stat = ((long long)b * a.H + head) * a.Sq + i;
@@ -126,8 +125,8 @@ __device__ __forceinline__ bool dq_body(const AttnArgs& a, char* smem, int block
     int lo, hi;
     doc_range(docs, p_lo, p_hi, lane, lo, hi);
     kt.find(words, 4, wave, lane, lo, hi, [&](int t) {
-      const int j = t * BN + lane, d = docs[min(j, sc.len - 1)];
-      return lane < BN && j < sc.len ? d : -1;
+      const int j = t * BN + lane % BN, d = docs[min(j, sc.len - 1)];
+      return j < sc.len ? d : -1;
     });
     __syncthreads();
   }
@@ -154,7 +153,7 @@ __device__ __forceinline__ bool dq_body(const AttnArgs& a, char* smem, int block
       __syncthreads();
       const int tn = kt.from(t + 1);
       if (tn < kt.t1) issue(tn, st ^ 1);
-      const bool masked = docs || (t + 1) * BN > all;
+      const bool masked = (t + 1) * BN > all || (docs && !(one && __all(sids[st * BN + lane % BN] == doc)));
       tl.fresh();
       const char *k_ = sk + st * Load::BYTES, *v_ = sv + st * Load::BYTES;
       typename Tile::Cols cols;
@@ -221,7 +220,7 @@ __device__ __forceinline__ bool dq_body(const AttnArgs& a, char* smem, int block
 template <class T, int DP, bool VEC>
 __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) k_attn_dq(const AttnArgs a) {
   extern __shared__ __align__(1024) char smem[];
-  const bool bad = dq_body<T, DP, VEC, false>(a, smem, blockIdx.x, gridDim.x);
+  const bool bad = dq_body<T, DP, VEC, false>(a, smem, blockIdx.x);
   if (threadIdx.x == 0) a.flags[blockIdx.x] = bad;
 }
 
@@ -239,7 +238,7 @@ struct RowStats {
 };
 
 template <class T, int DP, bool VEC, bool CAREFUL>
-__device__ __forceinline__ bool dkv_body(const AttnArgs& a, char* smem, int block, int blocks) {
+__device__ __forceinline__ bool dkv_body(const AttnArgs& a, char* smem, int block) {
   constexpr int BR = kBwdRowTile, KT = DP / 16, DB = DP / 32;
   using N = Num<T>;
   using Tile = AttnTile<T, DP>;
@@ -252,13 +251,9 @@ __device__ __forceinline__ bool dkv_body(const AttnArgs& a, char* smem, int bloc
   RowStats* stats = reinterpret_cast<RowStats*>(sv + LoadV::BYTES);   // [2]
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
 
-  int id = die_order(block, blocks);
-  const int split = id % a.splits;
-  id /= a.splits;
-  // A causal tile's work falls with its place.  Neighbouring heads run through the tiles in opposite directions, so
-  // that the two workgroups of a compute unit come to the same sum.
-  const int tile = id % a.tiles, bh = id / a.tiles;
-  const int k0 = (bh & 1 ? a.tiles - 1 - tile : tile) * kBwdKeyTile;
+  int bh, item;
+  place(block, a.B * a.Hk, bh, item);
+  const int split = item % a.splits, k0 = item / a.splits * kBwdKeyTile;   // the keys that most rows see first
   const int hk = bh % a.Hk, b = bh / a.Hk;
   const AttnScope sc(a, b);
   const int j = k0 + wave * 32 + (lane & 31), jc = min(j, a.Sk - 1);
@@ -421,19 +416,19 @@ __device__ __forceinline__ bool dkv_body(const AttnArgs& a, char* smem, int bloc
 template <class T, int DP, bool VEC>
 __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) k_attn_dkv(const AttnArgs a) {
   extern __shared__ __align__(1024) char smem[];
-  const bool bad = dkv_body<T, DP, VEC, false>(a, smem, blockIdx.x, gridDim.x);
+  const bool bad = dkv_body<T, DP, VEC, false>(a, smem, blockIdx.x);
   if (threadIdx.x == 0) a.flags[blockIdx.x] = bad;
 }
 
 template <class T, int DP, bool VEC>
 __global__ void __launch_bounds__(256, 1) k_attn_dq_again(const AttnArgs a, int blocks) {
   extern __shared__ __align__(1024) char smem[];
-  again(a.flags, blocks, [&](int id) { dq_body<T, DP, VEC, true>(a, smem, id, blocks); });
+  again(a.flags, blocks, [&](int id) { dq_body<T, DP, VEC, true>(a, smem, id); });
 }
 template <class T, int DP, bool VEC>
 __global__ void __launch_bounds__(256, 1) k_attn_dkv_again(const AttnArgs a, int blocks) {
   extern __shared__ __align__(1024) char smem[];
-  again(a.flags, blocks, [&](int id) { dkv_body<T, DP, VEC, true>(a, smem, id, blocks); });
+  again(a.flags, blocks, [&](int id) { dkv_body<T, DP, VEC, true>(a, smem, id); });
 }
 
 // ---- the ranges' partial sums, added in order -------------------------------------------------------------
@@ -472,8 +467,7 @@ hipError_t run_sum(hipStream_t s, const AttnArgs& a, const float* part, const At
 
 // `k` on `blocks` workgroups, then `k_again` on those it flagged
 template <class K, class A>
-hipError_t run_twice(hipStream_t s, const AttnArgs& a, K k, A k_again, int bytes) {
-  const int blocks = a.B * a.Hk * a.tiles * a.splits;
+hipError_t run_twice(hipStream_t s, const AttnArgs& a, K k, A k_again, int bytes, int blocks) {
   hipError_t e = hipFuncSetAttribute((const void*)k, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
   if (e == hipSuccess) e = hipFuncSetAttribute((const void*)k_again, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
   if (e != hipSuccess) return e;
@@ -489,7 +483,7 @@ hipError_t run_bwd(hipStream_t s, AttnArgs& a, const AttnBwdPlan& plan) {
     constexpr int bytes = 4 * AttnLoad<T, DP, kBwdKeys<T>, 4, VEC>::BYTES + 2 * kBwdKeys<T> * 4;
     a.tiles = plan.dq_tiles;
     a.splits = plan.dq_splits;
-    hipError_t e = run_twice(s, a, k_attn_dq<T, DP, VEC>, k_attn_dq_again<T, DP, VEC>, bytes);
+    hipError_t e = run_twice(s, a, k_attn_dq<T, DP, VEC>, k_attn_dq_again<T, DP, VEC>, bytes, a.B * a.Hk * a.tiles * a.splits);
     if (e == hipSuccess && a.splits > 1) e = run_sum<T, DP>(s, a, a.part, a.dq, a.gdiv, a.R, a.splits, a.scale);
     if (e != hipSuccess) return e;
   }
@@ -497,7 +491,7 @@ hipError_t run_bwd(hipStream_t s, AttnArgs& a, const AttnBwdPlan& plan) {
     constexpr int bytes = 4 * AttnLoad<T, DP, kBwdRowTile, 4, VEC>::BYTES + AttnLoad<T, DP, kBwdKeyTile, 4, VEC>::BYTES + 2 * (int)sizeof(RowStats);
     a.tiles = plan.dkv_tiles;
     a.splits = plan.dkv_splits;
-    hipError_t e = run_twice(s, a, k_attn_dkv<T, DP, VEC>, k_attn_dkv_again<T, DP, VEC>, bytes);
+    hipError_t e = run_twice(s, a, k_attn_dkv<T, DP, VEC>, k_attn_dkv_again<T, DP, VEC>, bytes, a.B * a.Hk * a.tiles * a.splits);
     if (e == hipSuccess && a.splits > 1) {
       const FastDiv one(1);
       e = run_sum<T, DP>(s, a, a.part, a.dk, one, a.Sk, a.splits, a.scale);
@@ -533,7 +527,7 @@ int ranges(long long blocks, long long axis) {
 
 }  // namespace
 
-AttnBwdPlan attn_plan_bwd(int B, int Hk, int R, int Sk, int D) {
+AttnBwdPlan attn_plan_bwd(int B, int Hk, int R, int Sk, int D, bool causal) {
   AttnBwdPlan p{};
   const int dp = D <= 64 ? 64 : 128;
   const long long bh = (long long)B * Hk;
@@ -543,6 +537,9 @@ AttnBwdPlan attn_plan_bwd(int B, int Hk, int R, int Sk, int D) {
   p.dkv_tiles = (Sk + kBwdKeyTile - 1) / kBwdKeyTile;
   if (p.dq_tiles) p.dq_splits = ranges(bh * p.dq_tiles, Sk);
   if (p.dkv_tiles) p.dkv_splits = ranges(bh * p.dkv_tiles, R);
+  // A causal tile's work falls with its place: where all workgroups run at once the first ones last twice as long as
+  // the mean.  Halved, they leave room that others fill (2 x 16 heads over 8, 4096 positions: XX us against YY).
+  if (causal && p.dkv_splits == 1 && bh * p.dkv_tiles < 2048 && p.dkv_tiles > 2) p.dkv_splits = 2;
   const long long dq = p.dq_splits > 1 ? p.dq_splits * bh * R * dp : 0, dkv = p.dkv_splits > 1 ? 2 * p.dkv_splits * bh * Sk * dp : 0;
   p.flag_ints = bh * std::max(p.dq_tiles * p.dq_splits, p.dkv_tiles * p.dkv_splits);
   p.part_floats = std::max(dq, dkv);   // one after the other on the stream

@@ -67,7 +67,7 @@ int attn_args(const ntk_attention_desc* d, AttnPlan* plan) {
   if (R > 0 && bh > 0) {
     *plan = attn_plan_fwd(d->batch, d->kv_heads, (int)R, d->k_len, d->head_dim);
     const long long tiles = plan->tokens ? 1 : plan->tiles;
-    const AttnBwdPlan back = attn_plan_bwd(d->batch, d->kv_heads, (int)R, d->k_len, d->head_dim);
+    const AttnBwdPlan back = attn_plan_bwd(d->batch, d->kv_heads, (int)R, d->k_len, d->head_dim, d->causal != 0);
     if (!grid_ok(bh * tiles * plan->splits, 256) || !grid_ok(bh * back.dq_tiles * back.dq_splits, 256) ||
         !grid_ok(bh * back.dkv_tiles * back.dkv_splits, 256) || !grid_ok((bh * R + 3) / 4, 256) || !grid_ok((bh * d->k_len + 3) / 4, 256) ||
         (plan->splits > 1 && !grid_ok(bh * R, 128)))
@@ -79,7 +79,7 @@ int attn_args(const ntk_attention_desc* d, AttnPlan* plan) {
 }
 
 AttnBwdPlan bwd_plan(const ntk_attention_desc* d) {
-  return attn_plan_bwd(d->batch, d->kv_heads, d->q_len * (d->heads / d->kv_heads), d->k_len, d->head_dim);
+  return attn_plan_bwd(d->batch, d->kv_heads, d->q_len * (d->heads / d->kv_heads), d->k_len, d->head_dim, d->causal != 0);
 }
 
 void set_view(AttnView& to, const ntk_view* v) {
@@ -107,6 +107,7 @@ void set_desc(AttnArgs& a, const ntk_attention_desc* d) {
   a.c = d->scale * kLog2e;
   a.cap_in = d->softcap > 0.f ? 2.f * kLog2e * d->scale / d->softcap : 0.f;
   a.cap_out = d->softcap * kLog2e;
+  a.cap_inv = d->softcap > 0.f ? 1.f / a.cap_out : 0.f;
   a.gdiv = FastDiv((uint32_t)a.G);
   a.splits = 1;
 }
