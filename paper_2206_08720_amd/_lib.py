@@ -122,7 +122,7 @@ def load():
     lib.ntk_mfma_peak.argtypes = [ctypes.c_int, ctypes.POINTER(ctypes.c_double)]
     lib.ntk_mfma_peak.restype = ctypes.c_int
     I, L, F = ctypes.c_int, ctypes.c_longlong, ctypes.c_float
-    V, D = ctypes.POINTER(ntk_view), ctypes.POINTER(ntk_attention_desc)
+    V, D = P, ctypes.POINTER(ntk_attention_desc)   # views: byref() of an ntk_view, or of its four numbers in an array
     for name, args, res in (
             ("ntk_rms_norm", [I, I, L, I, P, L, P, L, P, F, P, P, P, P], I),
             ("ntk_rms_norm_workspace", [L, I], L),

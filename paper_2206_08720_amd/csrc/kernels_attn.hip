@@ -395,14 +395,26 @@ __global__ void __launch_bounds__(DP) k_attn_join(const AttnArgs a) {
   const int d = threadIdx.x, r = blockIdx.x % a.R, bh = blockIdx.x / a.R, hk = bh % a.Hk, b = bh / a.Hk;
   const long long rows = (long long)a.B * a.Hk * a.R, row = (long long)bh * a.R + r;
   const float* ml = a.part + (long long)a.splits * rows * DP;
-  float m = -__builtin_inff();
-  for (int s = 0; s < a.splits; ++s) m = fmaxf(m, ml[(s * rows + row) * 2]);
-  float l = 0.f, o = 0.f;
-  for (int s = 0; s < a.splits; ++s) {
-    const float ms = ml[(s * rows + row) * 2];
-    const float f = ms == m ? 1.f : exp2_hw(ms - m);
-    l += ml[(s * rows + row) * 2 + 1] * f;
-    o += a.part[(s * rows + row) * DP + d] * f;
+  // online, eight ranges' numbers in flight at a time
+  float m = -__builtin_inff(), l = 0.f, o = 0.f;
+  for (int s0 = 0; s0 < a.splits; s0 += 8) {
+    float ms[8], ls[8], os[8];
+#pragma unroll
+    for (int u = 0; u < 8; ++u) {
+      const long long at = (long long)min(s0 + u, a.splits - 1) * rows + row;
+      ms[u] = s0 + u < a.splits ? ml[at * 2] : -__builtin_inff();
+      ls[u] = ml[at * 2 + 1];
+      os[u] = a.part[at * DP + d];
+    }
+#pragma unroll
+    for (int u = 0; u < 8; ++u) {
+      if (s0 + u >= a.splits) break;
+      const float mn = fmaxf(m, ms[u]);
+      const float f = m == mn ? 1.f : exp2_hw(m - mn), g = ms[u] == mn ? 1.f : exp2_hw(ms[u] - mn);
+      l = l * f + ls[u] * g;
+      o = o * f + os[u] * g;
+      m = mn;
+    }
   }
   const int i = (int)a.gdiv.div((uint32_t)r), head = hk * a.G + r - i * a.G;
   if (d < a.D) ((T*)a.o.p)[b * a.o.sb + i * a.o.ss + head * a.o.sh + d] = (T)(l == 0.f ? 0.f : o / l);
@@ -447,13 +459,15 @@ hipError_t run_fwd_dim(hipStream_t s, const AttnArgs& a, bool tokens, bool vec) 
 
 }  // namespace
 
-AttnPlan attn_plan_fwd(int B, int Hk, int R, int Sk, int D) {
+AttnPlan attn_plan_fwd(int dtype, int B, int Hk, int R, int Sk, int D) {
   AttnPlan p;
   p.tokens = R <= 32;
   p.tiles = (R + kFwdRows - 1) / kFwdRows;
   const long long blocks = (long long)B * Hk * (p.tokens ? 1 : p.tiles);
-  // ranges: enough workgroups for two on each of 256 compute units, none of fewer than 256 keys
-  const long long want = (512 + blocks - 1) / blocks, most = std::max(1, (Sk + 255) / 256);
+  // ranges: enough workgroups for two on each of 256 compute units, none of fewer than 256 keys (64 for many rows in fp32,
+  // whose products take 16 times as long)
+  const int least = dtype == 0 && !p.tokens ? 64 : 256;
+  const long long want = (512 + blocks - 1) / blocks, most = std::max(1, (Sk + least - 1) / least);
   p.splits = (int)std::max(1LL, std::min(want, most));
   if (!p.tokens && blocks >= 192) p.splits = 1;   // the join's traffic would cost more than idle units do
   const int dp = D <= 64 ? 64 : 128;

@@ -51,7 +51,7 @@ __device__ __forceinline__ void hide(f32x16& s, f32x16& dp, unsigned vis) {
 }
 
 // delta, and lse in units of log2; a row that sees nothing (lse = -inf) gets weights 0 through inf.
-template <class T>
+template <class T, bool VEC>
 __global__ void __launch_bounds__(256) k_attn_delta(const AttnArgs a, float* __restrict__ lse2, float* __restrict__ delta,
                                                     long long rows) {
   // 16 lanes a row (b, i, head)
@@ -64,7 +64,19 @@ __global__ void __launch_bounds__(256) k_attn_delta(const AttnArgs a, float* __r
   const T* o = (const T*)a.o.p + b * a.o.sb + i * a.o.ss + head * a.o.sh;
   const T* g = (const T*)a.dout.p + b * a.dout.sb + i * a.dout.ss + head * a.dout.sh;
   float s = 0.f;
-  for (int d = lane; d < a.D; d += 16) s = fmaf((float)o[d], (float)g[d], s);
+  if constexpr (VEC) {
+    constexpr int EC = 16 / (int)sizeof(T);
+    for (int d = lane * EC; d < a.D; d += 16 * EC) {
+      const uint4 uo = *reinterpret_cast<const uint4*>(o + d), ug = *reinterpret_cast<const uint4*>(g + d);
+      T x[EC], y[EC];
+      __builtin_memcpy(x, &uo, 16);
+      __builtin_memcpy(y, &ug, 16);
+#pragma unroll
+      for (int i = 0; i < EC; ++i) s = fmaf((float)x[i], (float)y[i], s);
+    }
+  } else {
+    for (int d = lane; d < a.D; d += 16) s = fmaf((float)o[d], (float)g[d], s);
+  }
 #pragma unroll
   for (int w = 8; w; w >>= 1) s += __shfl_xor(s, w);
   if (lane) return;
@@ -507,7 +519,9 @@ hipError_t run_bwd_dim(hipStream_t s, AttnArgs& a, const AttnBwdPlan& plan, floa
   const long long rows = (long long)a.B * a.Sq * a.H;
   float* lse2 = work + plan.part_floats;
   float* delta = lse2 + rows;
-  if (rows) k_attn_delta<T><<<dim3((unsigned)((rows + 15) / 16)), dim3(256), 0, s>>>(a, lse2, delta, rows);
+  const dim3 grid((unsigned)((rows + 15) / 16));
+  if (rows && vec) k_attn_delta<T, true><<<grid, dim3(256), 0, s>>>(a, lse2, delta, rows);
+  if (rows && !vec) k_attn_delta<T, false><<<grid, dim3(256), 0, s>>>(a, lse2, delta, rows);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   a.lse2 = lse2;
@@ -519,15 +533,16 @@ hipError_t run_bwd_dim(hipStream_t s, AttnArgs& a, const AttnBwdPlan& plan, floa
 }
 
 // Ranges of the summed axis: where the tiles are too few for two workgroups on each of 256 compute units, the
-// axis is cut so that there are, into ranges of at least 256 keys or rows.
-int ranges(long long blocks, long long axis) {
+// axis is cut so that there are, into ranges of at least 256 keys or rows (64 in fp32, whose products take 16 times
+// as long).
+int ranges(long long blocks, long long axis, int dtype) {
   if (blocks >= 256) return 1;   // the partial sums' traffic would cost more than it gains
-  return (int)std::max(1LL, std::min((512 + blocks - 1) / blocks, axis / 256));
+  return (int)std::max(1LL, std::min((512 + blocks - 1) / blocks, axis / (dtype == 0 ? 64 : 256)));
 }
 
 }  // namespace
 
-AttnBwdPlan attn_plan_bwd(int B, int Hk, int R, int Sk, int D, bool causal) {
+AttnBwdPlan attn_plan_bwd(int dtype, int B, int Hk, int R, int Sk, int D, bool causal) {
   AttnBwdPlan p{};
   const int dp = D <= 64 ? 64 : 128;
   const long long bh = (long long)B * Hk;
@@ -535,10 +550,10 @@ AttnBwdPlan attn_plan_bwd(int B, int Hk, int R, int Sk, int D, bool causal) {
   if (bh == 0) return p;
   p.dq_tiles = (R + kBwdRows - 1) / kBwdRows;
   p.dkv_tiles = (Sk + kBwdKeyTile - 1) / kBwdKeyTile;
-  if (p.dq_tiles) p.dq_splits = ranges(bh * p.dq_tiles, Sk);
-  if (p.dkv_tiles) p.dkv_splits = ranges(bh * p.dkv_tiles, R);
+  if (p.dq_tiles) p.dq_splits = ranges(bh * p.dq_tiles, Sk, dtype);
+  if (p.dkv_tiles) p.dkv_splits = ranges(bh * p.dkv_tiles, R, dtype);
   // A causal tile's work falls with its place: where all workgroups run at once the first ones last twice as long as
-  // the mean.  Halved, they leave room that others fill (2 x 16 heads over 8, 4096 positions: XX us against YY).
+  // the mean.  Halved, they leave room that others fill (2 x 16 heads over 8, 4096 positions of 128: 474 us with the sums' addition against 604).
   if (causal && p.dkv_splits == 1 && bh * p.dkv_tiles < 2048 && p.dkv_tiles > 2) p.dkv_splits = 2;
   const long long dq = p.dq_splits > 1 ? p.dq_splits * bh * R * dp : 0, dkv = p.dkv_splits > 1 ? 2 * p.dkv_splits * bh * Sk * dp : 0;
   p.flag_ints = bh * std::max(p.dq_tiles * p.dq_splits, p.dkv_tiles * p.dkv_splits);

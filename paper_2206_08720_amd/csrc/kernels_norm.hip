@@ -22,9 +22,11 @@ struct Pack8 {
   T v[kE];
 };
 
-// 8 elements from `at` on; those past n are zero
-template <class T, bool VEC>
-__device__ __forceinline__ void load8(const T* __restrict__ row, int at, int n, float (&f)[kE]) {
+// The 8 elements of group `c` of thread t: neighbours (VEC), or one from each of 8 runs of TPR, so that the threads of
+// a row read neighbours.  Those past n are zero.
+template <class T, bool VEC, int TPR>
+__device__ __forceinline__ void load8(const T* __restrict__ row, int c, int t, int n, float (&f)[kE]) {
+  const int at = VEC ? (c * TPR + t) * kE : c * TPR * kE + t;
   if constexpr (VEC) {
     if (at < n) {
       alignas(16) Pack8<T> p;
@@ -39,12 +41,13 @@ __device__ __forceinline__ void load8(const T* __restrict__ row, int at, int n, 
     for (int i = 0; i < kE; ++i) f[i] = 0.f;
   } else {
 #pragma unroll
-    for (int i = 0; i < kE; ++i) f[i] = at + i < n ? (float)row[at + i] : 0.f;
+    for (int i = 0; i < kE; ++i) f[i] = at + i * TPR < n ? (float)row[at + i * TPR] : 0.f;
   }
 }
 
-template <class T, bool VEC>
-__device__ __forceinline__ void store8(T* __restrict__ row, int at, int n, const float (&f)[kE]) {
+template <class T, bool VEC, int TPR>
+__device__ __forceinline__ void store8(T* __restrict__ row, int c, int t, int n, const float (&f)[kE]) {
+  const int at = VEC ? (c * TPR + t) * kE : c * TPR * kE + t;
   if constexpr (VEC) {
     if (at >= n) return;
     alignas(16) Pack8<T> p;
@@ -56,7 +59,7 @@ __device__ __forceinline__ void store8(T* __restrict__ row, int at, int n, const
   } else {
 #pragma unroll
     for (int i = 0; i < kE; ++i)
-      if (at + i < n) row[at + i] = (T)f[i];
+      if (at + i * TPR < n) row[at + i * TPR] = (T)f[i];
   }
 }
 
@@ -92,18 +95,18 @@ __global__ void __launch_bounds__(TPR < kBlock ? kBlock : TPR) k_rms_norm(const 
   const int n = a.width;
   float h[CH][kE], w[CH][kE];
 #pragma unroll
-  for (int c = 0; c < CH; ++c) load8<T, VEC>(x, (c * TPR + t) * kE, n, h[c]);
+  for (int c = 0; c < CH; ++c) load8<T, VEC, TPR>(x, c, t, n, h[c]);
   if (res) {
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
       float e[kE];
-      load8<T, VEC>(res, (c * TPR + t) * kE, n, e);
+      load8<T, VEC, TPR>(res, c, t, n, e);
 #pragma unroll
       for (int i = 0; i < kE; ++i) h[c][i] += e[i];
     }
   }
 #pragma unroll
-  for (int c = 0; c < CH; ++c) load8<W, VEC>((const W*)a.weight, (c * TPR + t) * kE, n, w[c]);
+  for (int c = 0; c < CH; ++c) load8<W, VEC, TPR>((const W*)a.weight, c, t, n, w[c]);
   float ss = 0.f;
 #pragma unroll
   for (int c = 0; c < CH; ++c)
@@ -113,7 +116,7 @@ __global__ void __launch_bounds__(TPR < kBlock ? kBlock : TPR) k_rms_norm(const 
   const float r = 1.f / sqrtf(ss / (float)n + a.eps);
   if (a.h) {
 #pragma unroll
-    for (int c = 0; c < CH; ++c) store8<T, VEC>((T*)a.h + row * n, (c * TPR + t) * kE, n, h[c]);
+    for (int c = 0; c < CH; ++c) store8<T, VEC, TPR>((T*)a.h + row * n, c, t, n, h[c]);
   }
 #pragma unroll
   for (int c = 0; c < CH; ++c)
@@ -121,7 +124,7 @@ __global__ void __launch_bounds__(TPR < kBlock ? kBlock : TPR) k_rms_norm(const 
     for (int i = 0; i < kE; ++i) h[c][i] = h[c][i] * r * w[c][i];
   if (!a.scale) {
 #pragma unroll
-    for (int c = 0; c < CH; ++c) store8<T, VEC>((T*)a.y + row * n, (c * TPR + t) * kE, n, h[c]);
+    for (int c = 0; c < CH; ++c) store8<T, VEC, TPR>((T*)a.y + row * n, c, t, n, h[c]);
     return;
   }
   float most = 0.f;
@@ -149,13 +152,13 @@ __global__ void __launch_bounds__(TPR < kBlock ? kBlock : TPR) k_rms_norm(const 
       int p = __builtin_amdgcn_cvt_pk_fp8_f32(e[0], e[1], 0, false);
       u[k] = (unsigned)__builtin_amdgcn_cvt_pk_fp8_f32(e[2], e[3], p, true);
     }
-    const int at = (c * TPR + t) * kE;
+    const int at = VEC ? (c * TPR + t) * kE : c * TPR * kE + t;
     if constexpr (VEC) {
       if (at < n) *reinterpret_cast<uint2*>(q + at) = make_uint2(u[0], u[1]);
     } else {
 #pragma unroll
       for (int i = 0; i < kE; ++i)
-        if (at + i < n) q[at + i] = (unsigned char)(u[i >> 2] >> (8 * (i & 3)));
+        if (at + i * TPR < n) q[at + i * TPR] = (unsigned char)(u[i >> 2] >> (8 * (i & 3)));
     }
   }
 }
@@ -171,7 +174,7 @@ __global__ void __launch_bounds__(TPR < kBlock ? kBlock : TPR) k_rms_norm_bwd(co
   float w[CH][kE], dw[CH][kE];
 #pragma unroll
   for (int c = 0; c < CH; ++c) {
-    load8<W, VEC>((const W*)a.weight, (c * TPR + t) * kE, n, w[c]);
+    load8<W, VEC, TPR>((const W*)a.weight, c, t, n, w[c]);
 #pragma unroll
     for (int i = 0; i < kE; ++i) dw[c][i] = 0.f;
   }
@@ -179,8 +182,8 @@ __global__ void __launch_bounds__(TPR < kBlock ? kBlock : TPR) k_rms_norm_bwd(co
     float h[CH][kE], g[CH][kE];
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
-      load8<T, VEC>((const T*)a.h + row * a.h_stride, (c * TPR + t) * kE, n, h[c]);
-      load8<T, VEC>((const T*)a.dy + row * a.dy_stride, (c * TPR + t) * kE, n, g[c]);
+      load8<T, VEC, TPR>((const T*)a.h + row * a.h_stride, c, t, n, h[c]);
+      load8<T, VEC, TPR>((const T*)a.dy + row * a.dy_stride, c, t, n, g[c]);
     }
     float ss = 0.f, sg = 0.f;
 #pragma unroll
@@ -196,10 +199,9 @@ __global__ void __launch_bounds__(TPR < kBlock ? kBlock : TPR) k_rms_norm_bwd(co
     const float f = r * r * (sg / (float)n);
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
-      const int at = (c * TPR + t) * kE;
       float e[kE];
       if (a.dh) {
-        load8<T, VEC>((const T*)a.dh + row * a.dh_stride, at, n, e);
+        load8<T, VEC, TPR>((const T*)a.dh + row * a.dh_stride, c, t, n, e);
       } else {
 #pragma unroll
         for (int i = 0; i < kE; ++i) e[i] = 0.f;
@@ -209,27 +211,32 @@ __global__ void __launch_bounds__(TPR < kBlock ? kBlock : TPR) k_rms_norm_bwd(co
         dw[c][i] = fmaf(g[c][i], h[c][i] * r, dw[c][i]);
         e[i] += r * (g[c][i] * w[c][i] - h[c][i] * f);
       }
-      store8<T, VEC>((T*)a.dx + row * n, at, n, e);
+      store8<T, VEC, TPR>((T*)a.dx + row * n, c, t, n, e);
     }
   }
   float* part = a.part + ((long long)blockIdx.x * RPB + sub) * n;
 #pragma unroll
-  for (int c = 0; c < CH; ++c) store8<float, false>(part, (c * TPR + t) * kE, n, dw[c]);
+  for (int c = 0; c < CH; ++c) store8<float, VEC, TPR>(part, c, t, n, dw[c]);
 }
 
-// dw[c] = sum_p part[p][c], in a fixed order: 16 columns a workgroup, 16 threads a column.
+// dw[c] = sum_p part[p][c], in a fixed order: 16 columns a workgroup, 64 threads a column, eight loads in flight each.
 template <class W>
-__global__ void __launch_bounds__(256) k_norm_columns(const float* __restrict__ part, int parts, int n, W* __restrict__ dw) {
-  __shared__ float s[16][17];
+__global__ void __launch_bounds__(1024) k_norm_columns(const float* __restrict__ part, int parts, int n, W* __restrict__ dw) {
+  __shared__ float s[64][17];
   const int c = threadIdx.x & 15, q = threadIdx.x >> 4, col = blockIdx.x * 16 + c;
   float x = 0.f;
-  if (col < n)
-    for (int p = q; p < parts; p += 16) x += part[(long long)p * n + col];
+  for (int p0 = q; p0 < parts; p0 += 64 * 8) {
+    float v[8];
+#pragma unroll
+    for (int u = 0; u < 8; ++u) v[u] = col < n && p0 + 64 * u < parts ? part[(long long)(p0 + 64 * u) * n + col] : 0.f;
+#pragma unroll
+    for (int u = 0; u < 8; ++u) x += v[u];
+  }
   s[q][c] = x;
   __syncthreads();
   if (q) return;
 #pragma unroll
-  for (int k = 1; k < 16; ++k) x += s[k][c];
+  for (int k = 1; k < 64; ++k) x += s[k][c];
   if (col < n) dw[col] = (W)x;
 }
 
@@ -266,7 +273,7 @@ hipError_t run(hipStream_t s, const NormArgs* f, const NormBwdArgs* b, bool vec)
     k_rms_norm_bwd<T, W, TPR, CH, false><<<grid, threads, 0, s>>>(*b);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  k_norm_columns<W><<<dim3((unsigned)((b->width + 15) / 16)), dim3(256), 0, s>>>(b->part, parts, b->width, (W*)b->dw);
+  k_norm_columns<W><<<dim3((unsigned)((b->width + 15) / 16)), dim3(1024), 0, s>>>(b->part, parts, b->width, (W*)b->dw);
   return hipGetLastError();
 }
 

@@ -16,7 +16,7 @@ struct AttnPlan {
   int tiles, splits;
   long long part_floats, flag_ints;
 };
-AttnPlan attn_plan_fwd(int B, int Hk, int R, int Sk, int D);
+AttnPlan attn_plan_fwd(int dtype, int B, int Hk, int R, int Sk, int D);
 // dtype: 0 fp32, 1 bf16, 2 fp16; vec: every operand's rows take 16-byte loads.
 hipError_t launch_attn_fwd(hipStream_t s, int dtype, const AttnArgs& a, bool tokens, bool vec);
 
@@ -26,7 +26,7 @@ struct AttnBwdPlan {
   int dq_tiles, dq_splits, dkv_tiles, dkv_splits;
   long long part_floats, flag_ints;
 };
-AttnBwdPlan attn_plan_bwd(int B, int Hk, int R, int Sk, int D, bool causal);
+AttnBwdPlan attn_plan_bwd(int dtype, int B, int Hk, int R, int Sk, int D, bool causal);
 // delta[b, h, i] = sum_d dout o, then dq, dk and dv.  work: part_floats, then 2 * batch * heads * q_len floats, then flag_ints.
 hipError_t launch_attn_bwd(hipStream_t s, int dtype, AttnArgs& a, const AttnBwdPlan& plan, float* work, bool vec);
 

@@ -65,9 +65,9 @@ int attn_args(const ntk_attention_desc* d, AttnPlan* plan) {
   if (R >= (1LL << 29) - 1024 || d->k_len >= (1LL << 31) - 1024 || bh >= (1LL << 31))
     return bad(NTK_E_UNSUPPORTED, "attention: q_len * group reaches 2^29 or k_len 2^31");
   if (R > 0 && bh > 0) {
-    *plan = attn_plan_fwd(d->batch, d->kv_heads, (int)R, d->k_len, d->head_dim);
+    *plan = attn_plan_fwd(d->dtype, d->batch, d->kv_heads, (int)R, d->k_len, d->head_dim);
     const long long tiles = plan->tokens ? 1 : plan->tiles;
-    const AttnBwdPlan back = attn_plan_bwd(d->batch, d->kv_heads, (int)R, d->k_len, d->head_dim, d->causal != 0);
+    const AttnBwdPlan back = attn_plan_bwd(d->dtype, d->batch, d->kv_heads, (int)R, d->k_len, d->head_dim, d->causal != 0);
     if (!grid_ok(bh * tiles * plan->splits, 256) || !grid_ok(bh * back.dq_tiles * back.dq_splits, 256) ||
         !grid_ok(bh * back.dkv_tiles * back.dkv_splits, 256) || !grid_ok((bh * R + 3) / 4, 256) || !grid_ok((bh * d->k_len + 3) / 4, 256) ||
         (plan->splits > 1 && !grid_ok(bh * R, 128)))
@@ -79,7 +79,7 @@ int attn_args(const ntk_attention_desc* d, AttnPlan* plan) {
 }
 
 AttnBwdPlan bwd_plan(const ntk_attention_desc* d) {
-  return attn_plan_bwd(d->batch, d->kv_heads, d->q_len * (d->heads / d->kv_heads), d->k_len, d->head_dim, d->causal != 0);
+  return attn_plan_bwd(d->dtype, d->batch, d->kv_heads, d->q_len * (d->heads / d->kv_heads), d->k_len, d->head_dim, d->causal != 0);
 }
 
 void set_view(AttnView& to, const ntk_view* v) {

@@ -29,25 +29,31 @@ def _check(t, name, dtype=None, ndim=None, device=None, shape=None):
         raise TypeError(f"{name} must be a GPU tensor of type {dtype or 'float32, bfloat16 or float16'}")
     if device is not None and t.device != device:
         raise ValueError(f"{name} is on {t.device}, expected {device}")
-    if (ndim is not None and t.dim() != ndim) or (shape is not None and tuple(t.shape) != tuple(shape)):
+    if (ndim is not None and t.dim() != ndim) or (shape is not None and t.shape != shape):
         raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape) if shape is not None else f'{ndim} dimensions'}")
-    if t.dim() and t.stride(-1) != 1 and t.shape[-1] > 1:
+    if not t.is_contiguous() and t.stride(-1) != 1 and t.shape[-1] > 1:
         raise ValueError(f"{name} must be contiguous in its last dimension")
+
+
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda i: torch.cuda.current_stream(i).cuda_stream)
 
 
 class _Call:
     """The device and stream of one call: outputs and workspaces are allocated for that stream, and tensors
     that come from another one are kept from reuse until it has passed this call."""
 
+    __slots__ = ("handle", "_enter")
+
     def __init__(self, lead, stream, inputs):
-        self.device = lead.device
-        self.stream = torch.cuda.current_stream(lead.device) if stream is None else stream
-        self.handle = ctypes.c_void_p(self.stream.cuda_stream)
-        self._enter = []
-        if torch.cuda.current_device() != lead.device.index:
-            self._enter.append(torch.cuda.device(lead.device))
-        if stream is not None:
-            self._enter.append(torch.cuda.stream(stream))
+        index = lead.device.index
+        self._enter = ()
+        if stream is None:
+            self.handle = _raw_stream(index)
+            if torch.cuda.current_device() != index:
+                self._enter = (torch.cuda.device(index),)
+        else:
+            self.handle = stream.cuda_stream
+            self._enter = (torch.cuda.device(index), torch.cuda.stream(stream))
             for t in inputs:
                 if t is not None:
                     t.record_stream(stream)
@@ -63,19 +69,29 @@ class _Call:
 
 
 def _ptr(t):
-    return None if t is None else ctypes.c_void_p(t.data_ptr())
+    return None if t is None else t.data_ptr()
 
 
-def _view(t):
-    """ntk_view of [batch, position, head, dim]; the stride of a dimension of size 1 is never used."""
-    n, s = t.shape, t.stride()
-    return _lib.ntk_view(t.data_ptr(), s[0] if n[0] > 1 else 0, s[1] if n[1] > 1 else 0, s[2] if n[2] > 1 else 0)
+def _views(*tensors):
+    """The tensors' [batch, position, head, dim] as ntk_view structs in one array, and a reference to each (None for None); the
+    stride of a dimension of size 1 is never used and counts as 0."""
+    values = []
+    for t in tensors:
+        if t is None:
+            values += (0, 0, 0, 0)
+        else:
+            (b, n, h, _), (sb, sn, sh, _) = t.shape, t.stride()
+            values += (t.data_ptr(), sb if b > 1 else 0, sn if n > 1 else 0, sh if h > 1 else 0)
+    array = (ctypes.c_longlong * len(values))(*values)
+    return [None if t is None else ctypes.byref(array, 32 * i) for i, t in enumerate(tensors)]
 
 
 def _rows(t):
     """A tensor's rows [rows, width] as (tensor, row stride), without a copy where the rows are evenly spaced."""
-    r = t.reshape(-1, t.shape[-1]) if t.dim() != 2 else t
-    return r, r.stride(0) if r.shape[0] > 1 else max(r.stride(0), r.shape[1])
+    if t.dim() != 2:
+        t = t.reshape(-1, t.shape[-1])
+    rows, width = t.shape
+    return t, t.stride(0) if rows > 1 else width
 
 
 # ---- root-mean-square norm ----------------------------------------------------------------------------------
@@ -88,7 +104,7 @@ def _rms_norm(x, weight, residual, eps, stream, e4m3):
     width = x.shape[-1]
     if weight.dtype != torch.float32 and weight.dtype != x.dtype:
         raise TypeError(f"weight must be float32 or {x.dtype}")
-    _check(weight, "weight", weight.dtype, device=x.device, shape=(width,))
+    _check(weight, "weight", weight.dtype, device=x.device, shape=x.shape[-1:])
     if residual is not None:
         _check(residual, "residual", x.dtype, device=x.device, shape=x.shape)
     with _Call(x, stream, (x, weight, residual)) as call:
@@ -127,7 +143,7 @@ def rms_norm_backward(dy, h, weight, dh=None, eps=1e-6, stream=None):
         _check(dh, "dh", h.dtype, device=h.device, shape=h.shape)
     if weight.dtype != torch.float32 and weight.dtype != h.dtype:
         raise TypeError(f"weight must be float32 or {h.dtype}")
-    _check(weight, "weight", weight.dtype, device=h.device, shape=(width,))
+    _check(weight, "weight", weight.dtype, device=h.device, shape=h.shape[-1:])
     with _Call(h, stream, (dy, h, weight, dh)) as call:
         hr, hs = _rows(h)
         yr, ys = _rows(dy)
@@ -190,12 +206,12 @@ def rotary(q, table, positions=0, k=None, interleaved=False, inverse=False, inpl
             raise ValueError("positions must be contiguous")
     with _Call(q, stream, (q, table, k, positions if per_token else None)) as call:
         qo = q if inplace else torch.empty((b, n, heads, dim), dtype=q.dtype, device=q.device)
-        ko = k if inplace or k is None else torch.empty(tuple(k.shape), dtype=k.dtype, device=k.device)
-        kv, kov = (None, None) if k is None else (ctypes.byref(_view(k)), ctypes.byref(_view(ko)))
+        ko = k if inplace or k is None else torch.empty(k.shape, dtype=k.dtype, device=k.device)
+        qv, kv, qov, kov = _views(q, k, qo, ko)
         _lib.check(lib.ntk_rotary(_DTYPES[q.dtype], b, n, heads, 0 if k is None else k.shape[2], dim, 2 * table.shape[1],
-                                  int(interleaved), int(inverse), ctypes.byref(_view(q)), kv, _ptr(table), table.shape[0],
+                                  int(interleaved), int(inverse), qv, kv, _ptr(table), table.shape[0],
                                   _ptr(positions) if per_token else None, 0 if per_token else int(positions),
-                                  ctypes.byref(_view(qo)), kov, call.handle))
+                                  qov, kov, call.handle))
     return qo if k is None else (qo, ko)
 
 
@@ -215,10 +231,9 @@ def _attention_desc(q, k, v, causal, softcap, scale, slopes, k_lens, prefix, doc
             _check(t, name, dtype, device=q.device, shape=shape)
             if not t.is_contiguous():
                 raise ValueError(f"{name} must be contiguous")
-    p = ctypes.c_void_p
     return _lib.ntk_attention_desc(_DTYPES[q.dtype], b, sq, sk, heads, kv_heads, dim, 1 if causal else 0,
                                    1.0 / math.sqrt(max(dim, 1)) if scale is None else scale, softcap,
-                                   *(p(0 if t is None else t.data_ptr()) for t in (k_lens, prefix, docs, slopes)))
+                                   _ptr(k_lens), _ptr(prefix), _ptr(docs), _ptr(slopes))
 
 
 def _workspace(lib, desc, backward, device):
@@ -243,8 +258,7 @@ def attention(q, k, v, causal=False, softcap=0.0, scale=None, slopes=None, k_len
         o = torch.empty((b, sq, heads, dim), dtype=q.dtype, device=q.device) if out is None else out
         lse = torch.empty((b, heads, sq), dtype=torch.float32, device=q.device) if return_lse else None
         work, need = _workspace(lib, desc, 0, q.device)
-        _lib.check(lib.ntk_attention(ctypes.byref(desc), ctypes.byref(_view(q)), ctypes.byref(_view(k)), ctypes.byref(_view(v)),
-                                     ctypes.byref(_view(o)), _ptr(lse), _ptr(work), need, call.handle))
+        _lib.check(lib.ntk_attention(ctypes.byref(desc), *_views(q, k, v, o), _ptr(lse), _ptr(work), need, call.handle))
     return (o, lse) if return_lse else o
 
 
@@ -261,9 +275,8 @@ def attention_backward(do, q, k, v, o, lse, causal=False, softcap=0.0, scale=Non
         raise ValueError("lse must be contiguous")
     with _Call(q, stream, (do, q, k, v, o, lse, slopes, k_lens, prefix, docs)) as call:
         dq = torch.empty((b, sq, heads, dim), dtype=q.dtype, device=q.device)
-        dk, dv = (torch.empty(tuple(k.shape), dtype=k.dtype, device=k.device) for _ in range(2))
+        dk, dv = (torch.empty(k.shape, dtype=k.dtype, device=k.device) for _ in range(2))
         work, need = _workspace(lib, desc, 1, q.device)
-        views = [ctypes.byref(_view(t)) for t in (do, q, k, v, o)]
-        grads = [ctypes.byref(_view(t)) for t in (dq, dk, dv)]
-        _lib.check(lib.ntk_attention_bwd(ctypes.byref(desc), *views, _ptr(lse), *grads, _ptr(work), need, call.handle))
+        views = _views(do, q, k, v, o, dq, dk, dv)
+        _lib.check(lib.ntk_attention_bwd(ctypes.byref(desc), *views[:5], _ptr(lse), *views[5:], _ptr(work), need, call.handle))
     return dq, dk, dv
