@@ -51,6 +51,42 @@ __device__ __forceinline__ void hide(f32x16& s, f32x16& dp, unsigned vis) {
 }
 
 // delta, and lse in units of log2; a row that sees nothing (lse = -inf) gets weights 0 through inf.
+// fp16 keeps 11 bits only above 2^-14, and p and ds of long rows lie below.  p is formed times 2^10 (its offset is in
+// lse2).  ds, whose size is that of the gradient, is multiplied by a power of two that follows the lane's
+// largest so far, as the running maximum of a softmax does; the sums of the lane change with it.
+template <class T>
+constexpr bool kIsF16 = std::is_same_v<T, _Float16>;
+template <class T>
+constexpr float kPScale = kIsF16<T> ? 1024.f : 1.f;
+constexpr float kDsTop = 16384.f;         // a quarter of the largest fp16
+
+template <class T, int N>
+struct DsScale {
+  float mul = kIsF16<T> ? 0x1p100f : 1.f;
+  __device__ __forceinline__ void apply(f32x16& ds, f32x16 (&acc)[N]) {
+    if constexpr (kIsF16<T>) {
+      float top = 0.f;
+#pragma unroll
+      for (int v = 0; v < 16; ++v) top = fmaxf(top, fabsf(ds[v]));
+      top = half_max(top);
+      if (__any(top * mul > kDsTop)) {
+        // 2^14 over the power of two above top (inf counts as 2^127)
+        const int e = min((int)(__float_as_uint(top) >> 23) - 127 + 1, 127);
+        const float to = top * mul > kDsTop ? __uint_as_float((uint32_t)(14 - e + 127) << 23) : mul, f = to / mul;
+        mul = to;
+#pragma unroll
+        for (int d = 0; d < N; ++d)
+#pragma unroll
+          for (int v = 0; v < 16; ++v) acc[d][v] *= f;
+      }
+#pragma unroll
+      for (int v = 0; v < 16; ++v) ds[v] *= mul;
+    }
+  }
+  // what the sums are multiplied by at the end
+  __device__ __forceinline__ float undo() const { return 1.f / (mul * kPScale<T>); }
+};
+
 template <class T, bool VEC>
 __global__ void __launch_bounds__(256) k_attn_delta(const AttnArgs a, float* __restrict__ lse2, float* __restrict__ delta,
                                                     long long rows) {
@@ -83,7 +119,7 @@ __global__ void __launch_bounds__(256) k_attn_delta(const AttnArgs a, float* __r
   const long long at = ((long long)b * a.H + head) * a.Sq + i;
   const float l = a.lse[at];
   const bool empty = l == -__builtin_inff();
-  lse2[at] = empty ? __builtin_inff() : l * kLog2e;
+  lse2[at] = empty ? __builtin_inff() : l * kLog2e - (kIsF16<T> ? 10.f : 0.f);
   delta[at] = empty ? 0.f : s;
 }
 
@@ -147,9 +183,11 @@ __device__ __forceinline__ bool dq_body(const AttnArgs& a, char* smem, int block
 
   typename Tile::Lane tl(lane);
   f32x16 acc[DB];
+  DsScale<T, DB> dscale;
   auto pass = [&](auto careful) {
 #pragma unroll
     for (int d = 0; d < DB; ++d) zero16(acc[d]);
+    dscale = {};
     int t = kt.from(kt.t0), st = 0, nid = -1;
     auto issue = [&](int t, int st) {
       if (docs && tid < BN) nid = t * BN + tid < sc.len ? docs[t * BN + tid] : -1;
@@ -196,6 +234,7 @@ __device__ __forceinline__ bool dq_body(const AttnArgs& a, char* smem, int block
         weights<T>(a, s, dp, [&](int) { return lse2; }, [&](int) { return delta; }, [&](int) { return slope2; },
                    [&](int v) { return (float)abs(pos - (base + 8 * (v >> 2) + (v & 3))); });
         if (masked) hide(s, dp, vis);
+        dscale.apply(dp, acc);
         unrolled<2>([&](auto step) {
           constexpr int u = decltype(step)::value;
           const Frag w = to_frag<T>(dp, u);
@@ -224,9 +263,9 @@ __device__ __forceinline__ bool dq_body(const AttnArgs& a, char* smem, int block
   if (!CAREFUL && __syncthreads_or(not_finite(acc))) return true;
   if (r >= a.R) return false;
   if (a.splits > 1)
-    store_owned<float, DP, true>(a.part + (((long long)split * a.B * a.Hk + (long long)b * a.Hk + hk) * a.R + r) * DP, DP, lane, acc, 1.f);
+    store_owned<float, DP, true>(a.part + (((long long)split * a.B * a.Hk + (long long)b * a.Hk + hk) * a.R + r) * DP, DP, lane, acc, dscale.undo());
   else
-    store_owned<T, DP, VEC>((T*)a.dq.p + b * a.dq.sb + i * a.dq.ss + head * a.dq.sh, a.D, lane, acc, a.scale);
+    store_owned<T, DP, VEC>((T*)a.dq.p + b * a.dq.sb + i * a.dq.ss + head * a.dq.sh, a.D, lane, acc, a.scale * dscale.undo());
   return false;
 }
 template <class T, int DP, bool VEC>
@@ -304,12 +343,14 @@ __device__ __forceinline__ bool dkv_body(const AttnArgs& a, char* smem, int bloc
 
   typename Tile::Lane tl(lane);
   f32x16 dk[DB], dv[DB];
+  DsScale<T, DB> dscale;
   auto pass = [&](auto careful) {
 #pragma unroll
     for (int d = 0; d < DB; ++d) {
       zero16(dk[d]);
       zero16(dv[d]);
     }
+    dscale = {};
     auto issue = [&](int t, int st) {
       int lane = tid & 63;
       asm volatile("" : "+v"(lane));   // the places are formed here, not held over the products
@@ -380,6 +421,7 @@ __device__ __forceinline__ bool dkv_body(const AttnArgs& a, char* smem, int bloc
       constexpr int GQ = 2 * Load::BYTES;                // from the tile of q to that of dout
       typename Tile::Cols qcols;
       qcols.set(q_, tl);
+      dscale.apply(dp, dk);
       const Frag pf[2] = {to_frag<T>(s, 0), to_frag<T>(s, 1)}, wf[2] = {to_frag<T>(dp, 0), to_frag<T>(dp, 1)};
       __builtin_amdgcn_sched_barrier(0);
       unrolled<2>([&](auto step) {
@@ -416,13 +458,13 @@ __device__ __forceinline__ bool dkv_body(const AttnArgs& a, char* smem, int bloc
   if (j >= a.Sk) return false;
   if (a.splits > 1) {
     const long long keys = (long long)a.B * a.Hk * a.Sk, row = (long long)bh * a.Sk + j;
-    store_owned<float, DP, true>(a.part + ((long long)split * keys + row) * DP, DP, lane, dk, 1.f);
-    store_owned<float, DP, true>(a.part + ((long long)(a.splits + split) * keys + row) * DP, DP, lane, dv, 1.f);
+    store_owned<float, DP, true>(a.part + ((long long)split * keys + row) * DP, DP, lane, dk, dscale.undo());
+    store_owned<float, DP, true>(a.part + ((long long)(a.splits + split) * keys + row) * DP, DP, lane, dv, 1.f / kPScale<T>);
     return false;
   }
   // keys past the batch entry's length get zeros
-  store_owned<T, DP, VEC>((T*)a.dk.p + b * a.dk.sb + j * a.dk.ss + hk * a.dk.sh, a.D, lane, dk, a.scale);
-  store_owned<T, DP, VEC>((T*)a.dv.p + b * a.dv.sb + j * a.dv.ss + hk * a.dv.sh, a.D, lane, dv, 1.f);
+  store_owned<T, DP, VEC>((T*)a.dk.p + b * a.dk.sb + j * a.dk.ss + hk * a.dk.sh, a.D, lane, dk, a.scale * dscale.undo());
+  store_owned<T, DP, VEC>((T*)a.dv.p + b * a.dv.sb + j * a.dv.ss + hk * a.dv.sh, a.D, lane, dv, 1.f / kPScale<T>);
   return false;
 }
 template <class T, int DP, bool VEC>

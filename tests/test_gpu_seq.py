@@ -43,10 +43,12 @@ def _close(name, got, ref, tol):
 
 # ---- attention ------------------------------------------------------------------------------------------------------
 
-def _oracle(q, k, v, type, do=None, causal=False, softcap=0.0, scale=None, slopes=None, k_lens=None, prefix=None, docs=None):
-    """{name: (value, tolerance)} in 64 bits on the CPU; a hidden pair enters no sum."""
+def _oracle(q, k, v, type, do=None, causal=False, softcap=0.0, scale=None, slopes=None, k_lens=None, prefix=None, docs=None, inner=None):
+    """{name: (value, tolerance)} in 64 bits on the CPU; a hidden pair enters no sum.  inner: the smallest step of p and
+    ds in their products (the type's own, where the kernels do not scale them)."""
     import torch
     u, tiny = U[type], TINY[type]
+    inner = tiny if inner is None else inner
     B, Sq, H, D = q.shape
     Sk, Hk = k.shape[1], k.shape[2]
     scale = 1 / math.sqrt(D) if scale is None else scale
@@ -91,7 +93,7 @@ def _oracle(q, k, v, type, do=None, causal=False, softcap=0.0, scale=None, slope
             dscore = torch.where(vis, (D + 8) * E * mag + 8 * E * softcap, 0.0).max() if Sk else 0.0
             kappa = 2 * float(dscore) + (Sk + 8) * E
             o = P @ vv
-            A = P @ vv.abs() + tiny * (vis.double() @ vv.abs())
+            A = P @ vv.abs() + inner * (vis.double() @ vv.abs())
             to = u * o.abs() + tiny + (u + kappa) * A
             out["o"][0][b, :, h], out["o"][1][b, :, h] = o, to
             lse = torch.where(some, top + torch.log(torch.where(some, l, 1.0)), -math.inf)
@@ -103,14 +105,14 @@ def _oracle(q, k, v, type, do=None, causal=False, softcap=0.0, scale=None, slope
             dS = torch.where(vis, P * (dP - delta) * fac, 0.0)
             edp = (D + 8) * E * (g.abs() @ vv.abs().T) + (g.abs() * (to + (D + 8) * E * o.abs())).sum(1, keepdim=True)
             eds = torch.where(vis, P * ((u + kappa + 16 * E) * (dP - delta).abs() * fac + edp * fac
-                                        + (dP - delta).abs() * 8 * (float(dscore) / max(softcap, 1e-9) + E if softcap else 0.0)) + tiny, 0.0)
+                                        + (dP - delta).abs() * 8 * (float(dscore) / max(softcap, 1e-9) + E if softcap else 0.0)) + inner, 0.0)
             dq = dS @ kk * scale
             out["dq"][0][b, :, h] = dq
             out["dq"][1][b, :, h] = u * dq.abs() + tiny + scale * (eds @ kk.abs() + Sk * E * (dS.abs() @ kk.abs()))
             out["dk"][0][b, :, c] += dS.T @ qq * scale
             out["dk"][1][b, :, c] += scale * (eds.T @ qq.abs() + (Sq * H // Hk) * E * (dS.abs().T @ qq.abs()))
             out["dv"][0][b, :, c] += P.T @ g
-            out["dv"][1][b, :, c] += (u + kappa + (Sq * H // Hk) * E) * (P.T @ g.abs()) + tiny * (vis.double().T @ g.abs())
+            out["dv"][1][b, :, c] += (u + kappa + (Sq * H // Hk) * E) * (P.T @ g.abs()) + inner * (vis.double().T @ g.abs())
     for n in ("dk", "dv") if do is not None else ():
         out[n][1] += u * out[n][0].abs() + tiny
     return out
@@ -250,6 +252,27 @@ def test_attention_rows_that_see_nothing():
     got = _attention("bf16", 2, 8, 20, 2, 1, 64, seed=440, train=True, causal=True, k_lens=[3, 0])
     assert not got["o"][0, :5].any() and not got["o"][1].any() and torch.isneginf(got["lse"][1]).all()
     assert not got["dq"][1].any() and not got["dk"][1].any() and not got["dk"][0, 3:].any()
+
+
+@pytest.mark.parametrize("std", [2.0 ** -10, 2.0 ** 9])
+def test_fp16_gradients_of_any_size(std):
+    """Rows of 2000 keys: p and ds lie far below fp16's 2^-14, or above 2^15 with a large gradient; the backward pass scales
+    them, so that no absolute step of theirs enters (o's does: the forward pass takes p as it is)."""
+    import torch
+    from paper_2206_08720_amd import seq
+    q, k, v = (_rand((1, n, 1, 64), 530 + i, "f16") for i, n in enumerate((70, 2000, 2000)))
+    do = _rand((1, 70, 1, 64), 533, "f16", std)
+    o, lse = seq.attention(q.cuda(), k.cuda(), v.cuda(), return_lse=True)
+    grads = seq.attention_backward(do.cuda(), q.cuda(), k.cuda(), v.cuda(), o, lse)
+    ref = _oracle(q, k, v, "f16", do, inner=0.0)
+    loose = _oracle(q, k, v, "f16", do)
+    _close("o", o, *loose["o"])
+    # delta is formed from the stored o: its step there, times |dout|, enters ds through p
+    extra = float((loose["o"][1] - ref["o"][1]).max()) * float(do.double().abs().sum(-1).max())
+    P = torch.softmax(q[0, :, 0].double() @ k[0, :, 0].double().T / 8, 1)
+    more = {"dq": extra / 8 * (P @ k[0, :, 0].double().abs())[None, :, None], "dk": extra / 8 * (P.T @ q[0, :, 0].double().abs())[None, :, None], "dv": 0.0}
+    for name, g in zip(("dq", "dk", "dv"), grads):
+        _close(name, g, ref[name][0], ref[name][1] + more[name])
 
 
 def test_attention_gradient_against_differences():
