@@ -37,7 +37,7 @@ extern "C" {
  *   x, residual   [rows, width], `*_stride` elements between rows (>= width).
  *   weight        [width] of type wtype: dtype, or NTK_F32.
  *   y             [rows, width] contiguous, of dtype; or, with `scale` not NULL, 8-bit e4m3 values q with
- *                 q[row] scale[row] = y: scale = max|y| / 448, 1 for a row of zeros.
+ *                 q[row] scale[row] = y: scale = max|y| / 448 (at least 2^-126), 1 for a row of zeros.
  *   h             [rows, width] contiguous, of dtype: the sum, for the next block and the backward pass; may
  *                 be NULL, and may be x or residual itself where that is contiguous.
  *   scale         [rows] fp32, or NULL.
@@ -113,13 +113,15 @@ int ntk_rotary(int dtype, int batch, int length, int q_heads, int k_heads, int d
  *   docs                     [batch, k_len] int32 or NULL: a document number a position, negative for padding.
  *   slopes                   [heads] fp32 or NULL.
  *   lse                      [batch, heads, q_len] fp32 or NULL: log of the softmax's sum (natural).
+ *   o                        must not overlap q, k or v.
  *   workspace                ntk_attention_workspace(desc, 0) bytes, 16-byte aligned: partial results of the ranges that
- *                            the keys are cut into where there are few rows (it may be 0).
+ *                            the keys are cut into where there are few rows, and flags (it may be 0).
  *
  * ntk_attention_bwd -- dq, dk and dv from dout, with o and lse of the forward call.  softcap, slopes and masks as
  * there; the slopes get no gradient.  Keys past k_lens get zeros.  dq, dk, dv must not overlap the inputs.
  *   workspace                ntk_attention_workspace(desc, 1) bytes.
- * The p and ds factors of the products over the keys (rows) are rounded to dtype. */
+ * The p and ds factors of the products over the keys (rows) are rounded to dtype, in fp16 under powers of two that keep
+ * them in its range. */
 typedef struct ntk_attention_desc {
     int dtype, batch, q_len, k_len, heads, kv_heads, head_dim, causal;
     float scale, softcap;

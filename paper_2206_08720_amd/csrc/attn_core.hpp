@@ -471,6 +471,10 @@ __device__ __forceinline__ f32x16 mma_visible(typename Num<T>::Frag a, typename 
 constexpr int kAgainBlocks = 256;
 template <class Body>
 __device__ __forceinline__ void again(const int* flags, int blocks, Body body) {
+  // first all of this workgroup's flags at once: mostly none is set
+  int any = 0;
+  for (int id = blockIdx.x + threadIdx.x * gridDim.x; id < blocks; id += blockDim.x * gridDim.x) any |= flags[id];
+  if (!__syncthreads_or(any)) return;
   for (int id = blockIdx.x; id < blocks; id += gridDim.x)
     if (flags[id]) {
       body(id);

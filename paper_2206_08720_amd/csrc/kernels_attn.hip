@@ -464,12 +464,16 @@ AttnPlan attn_plan_fwd(int dtype, int B, int Hk, int R, int Sk, int D) {
   p.tokens = R <= 32;
   p.tiles = (R + kFwdRows - 1) / kFwdRows;
   const long long blocks = (long long)B * Hk * (p.tokens ? 1 : p.tiles);
-  // ranges: enough workgroups for two on each of 256 compute units, none of fewer than 256 keys (64 for many rows in fp32,
-  // whose products take 16 times as long)
-  const int least = dtype == 0 && !p.tokens ? 64 : 256;
-  const long long want = (512 + blocks - 1) / blocks, most = std::max(1, (Sk + least - 1) / least);
-  p.splits = (int)std::max(1LL, std::min(want, most));
-  if (!p.tokens && blocks >= 192) p.splits = 1;   // the join's traffic would cost more than idle units do
+  // Ranges of the keys.  Tokens: enough workgroups for two on each of 256 compute units, each with at least 64 KB of
+  // keys: a call over 777 keys of 8 heads of 64 takes 13.5 us in one range and 20 in four, with the join and its
+  // launch; with heads of 128 the ranges pay on the GPU (12 us against 18).  Many rows: as many as run at once, of
+  // at least 256 keys (64 in fp32, whose products take 16 times as long); from 192 tiles on the join's traffic
+  // would cost more than idle units do.
+  const int row_bytes = (D <= 64 ? 64 : 128) * (dtype == 0 ? 4 : 2);
+  if (p.tokens)
+    p.splits = (int)std::max(1LL, std::min((512 + blocks - 1) / blocks, (long long)Sk * row_bytes / 65536));
+  else
+    p.splits = blocks >= 192 ? 1 : (int)std::max(1LL, std::min(512 / blocks, (long long)Sk / (dtype == 0 ? 64 : 256)));
   const int dp = D <= 64 ? 64 : 128;
   p.part_floats = p.splits > 1 ? (long long)p.splits * B * Hk * R * (dp + 2) : 0;
   p.flag_ints = p.tokens ? 0 : blocks * p.splits;

@@ -133,7 +133,7 @@ __global__ void __launch_bounds__(TPR < kBlock ? kBlock : TPR) k_rms_norm(const 
 #pragma unroll
     for (int i = 0; i < kE; ++i) most = fmaxf(most, fabsf(h[c][i]));
   most = row_all<TPR, true>(most, s);
-  const float scale = most > 0.f ? most / kMostE4m3 : 1.f;
+  const float scale = most > 0.f ? fmaxf(most / kMostE4m3, 0x1p-126f) : 1.f;   // its inverse stays finite
   if (t == 0) a.scale[row] = scale;
   const float inv = 1.f / scale;
   unsigned char* q = (unsigned char*)a.y + row * n;

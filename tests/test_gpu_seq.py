@@ -311,6 +311,33 @@ def test_attention_offsets_past_32_bits():
     _close("o", seq.attention(q2.cuda(), k, v, causal=True), *_oracle(q2, kc, vc, "bf16", causal=True)["o"])
 
 
+def test_many_documents_in_long_rows():
+    """More tiles than the lists of a workgroup hold (2^14 tiles of 32 rows; of 32 and of 64 keys): what lies past them is
+    left to the masks."""
+    import torch
+    from paper_2206_08720_amd import seq
+    n, D, doc = 530000, 64, 90
+    docs = (torch.arange(n) // doc).int()
+    q, k, v, do = (torch.randn(1, n, 1, D, generator=torch.Generator("cuda").manual_seed(540 + i), device="cuda").bfloat16() for i in range(4))
+    opt = {"causal": True, "docs": docs[None].cuda()}
+    o, lse = seq.attention(q, k, v, return_lse=True, **opt)
+    grads = seq.attention_backward(do, q, k, v, o, lse, **opt)
+    last = n - (n - 1) // doc * doc
+    for a, b in ((0, 2 * doc), (262080, 262080 + doc), (n - last - doc, n)):   # whole documents
+        part = [t[:, a:b].cpu() for t in (q, k, v)]
+        ref = _oracle(*part, "bf16", do[:, a:b].cpu(), causal=True, docs=docs[None, a:b])
+        for name, t in zip(("o", "dq", "dk", "dv"), (o,) + grads):
+            _close(f"{name} {a}", t[:, a:b], *ref[name])
+    # one token, and a few rows, over two copies of the keys
+    ids = torch.cat((docs, docs + docs[-1] + 1))
+    far = {"docs": ids[None].cuda()}
+    k2, v2 = torch.cat((k, k), 1), torch.cat((v, v), 1)
+    for rows in (1, 40):
+        a = n - last
+        ref = _oracle(q[:, n - rows:].cpu(), k[:, a:].cpu(), v[:, a:].cpu(), "bf16", docs=docs[None, a:])
+        _close(f"o {rows}", seq.attention(q[:, n - rows:], k2, v2, **far), *ref["o"])
+
+
 # ---- norm -----------------------------------------------------------------------------------------------------------
 
 def _norm_reference(x, res, w, eps, type, dy=None, dh=None, h_saved=None):
@@ -359,6 +386,16 @@ def test_rms_norm(type, rows, n):
         _close("dw", dw, val, tol - U[type] * val.abs() + U[wtype] * val.abs())
     y = seq.rms_norm(x.cuda(), w.cuda())
     _close("y", y, *_norm_reference(x, None, w, 1e-6, type)["y"])
+
+
+def test_rms_norm_e4m3_of_tiny_rows():
+    """max|y| / 448 below the smallest normal fp32: the scale stays at it and nothing turns into NaN."""
+    import torch
+    from paper_2206_08720_amd import seq
+    x = torch.zeros(1, 64, device="cuda")
+    x[0, 3] = 1.0
+    q, scale = seq.rms_norm_e4m3(x, torch.full((64,), 1e-43, device="cuda"))
+    assert float(scale) == 2.0 ** -126 and torch.isfinite(q.float()).all()
 
 
 @pytest.mark.parametrize("type,rows,n", [("bf16", 5, 2048), ("f16", 3, 777), ("f32", 2, 20000), ("bf16", 1, 1)])
