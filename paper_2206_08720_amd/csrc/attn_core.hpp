@@ -33,6 +33,7 @@ typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
 typedef float f32x8 __attribute__((ext_vector_type(8)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef int i32x4 __attribute__((ext_vector_type(4)));
 
 constexpr float kLog2e = 1.44269504088896340736f;
 constexpr float kLn2 = 0.69314718055994530942f;
@@ -92,6 +93,15 @@ struct AttnArgs {
   float cap_in, cap_out, cap_inv;  // softcap > 0: 2 log2(e) scale / cap, cap log2(e) and 1 / (cap log2(e)); else 0
   FastDiv gdiv;
 };
+
+// The kernel's arguments (its first parameter is an AttnArgs), read again from where the launch put them: a loop that
+// names them this way does not hold a hundred scalar registers of them, which the compiler would spill.
+__device__ __forceinline__ const AttnArgs& args_again() {
+  typedef const __attribute__((address_space(4))) AttnArgs Const;
+  Const* p = (Const*)__builtin_amdgcn_kernarg_segment_ptr();
+  asm volatile("" : "+s"(p));
+  return *(const AttnArgs*)p;
+}
 
 // What a batch entry's queries see: query i stands at position off + i, the keys are 0 .. len - 1, and
 // a query at position p sees the keys below klim(p).

@@ -61,9 +61,10 @@ struct FwdRows {
       }
       if (a.docs) {
 #pragma unroll
-        for (int v = 0; v < 16; ++v) {
-          const int k = 8 * (v >> 2) + (v & 3);
-          s[v] = k < left && ids[32 * nb + h4 + k] == doc ? s[v] : -__builtin_inff();
+        for (int q = 0; q < 4; ++q) {
+          const i32x4 id = *reinterpret_cast<const i32x4*>(ids + 32 * nb + h4 + 8 * q);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) s[4 * q + i] = 8 * q + i < left && id[i] == doc ? s[4 * q + i] : -__builtin_inff();
         }
       } else {
 #pragma unroll

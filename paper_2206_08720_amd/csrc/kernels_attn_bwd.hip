@@ -12,33 +12,50 @@
 namespace ntk {
 namespace {
 
-// p and ds of 16 (row, key) pairs of a lane: `s` the raw products q k, `dp` the products dout v.  dist(v): |position -
-// key| for the slope.
-template <class T, class L, class Dl, class Sl, class Dist>
-__device__ __forceinline__ void weights(const AttnArgs& a, f32x16& s, f32x16& dp, L lse2, Dl delta, Sl slope2, Dist dist) {
+// p and ds of 16 (row, key) pairs of a lane: `s` the raw products q k, `dp` the products dout v.  The functions give the
+// numbers of registers 4 q .. 4 q + 3; far(q): |position - key| for the slope.
+template <class T, class L, class Dl, class Sl, class Far>
+__device__ __forceinline__ void weights(const AttnArgs& a, f32x16& s, f32x16& dp, L lse2, Dl delta, Sl slope2, Far far) {
+  // a few numbers at a time (sched_barrier): registers are short
+  unrolled<4>([&](auto quad) {
+    constexpr int q = decltype(quad)::value;
+    const f32x4 d = delta(q);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) dp[4 * q + i] -= d[i];
+  });
+  float c = a.c;
   if (a.cap_in != 0.f || a.slopes) {
+    // to scores in log2 units, the cap's factor taken along
+    c = 1.f;
+    if (a.cap_in != 0.f) {
 #pragma unroll
-    for (int v = 0; v < 16; ++v) {
-      float x = s[v], fac = 1.f;
-      if (a.cap_in != 0.f) {
-        x = capped<T>(a, x);
-        const float t = x * a.cap_inv;
-        fac = fmaf(-t, t, 1.f);
-      } else {
-        x *= a.c;
+      for (int v = 0; v < 16; ++v) {
+        s[v] = capped<T>(a, s[v]);
+        const float t = s[v] * a.cap_inv;
+        dp[v] *= fmaf(-t, t, 1.f);
       }
-      if (a.slopes) x -= slope2(v) * dist(v);
-      s[v] = exp2_hw(x - lse2(v));
-      dp[v] = s[v] * (dp[v] - delta(v)) * fac;
-      if (v % 4 == 3) __builtin_amdgcn_sched_barrier(0);   // the rows' numbers four at a time: registers are short
-    }
-    return;
-  }
+    } else {
 #pragma unroll
-  for (int v = 0; v < 16; ++v) {
-    s[v] = exp2_hw(fmaf(s[v], a.c, -lse2(v)));
-    dp[v] = s[v] * (dp[v] - delta(v));
+      for (int v = 0; v < 16; ++v) s[v] *= a.c;
+    }
+    if (a.slopes)
+      unrolled<4>([&](auto quad) {
+        constexpr int q = decltype(quad)::value;
+        const f32x4 m = slope2(q), f = far(q);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) s[4 * q + i] -= m[i] * f[i];
+        __builtin_amdgcn_sched_barrier(0);
+      });
   }
+  unrolled<4>([&](auto quad) {
+    constexpr int q = decltype(quad)::value;
+    const f32x4 l = lse2(q);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      s[4 * q + i] = exp2_hw(fmaf(s[4 * q + i], c, -l[i]));
+      dp[4 * q + i] *= s[4 * q + i];
+    }
+  });
 }
 // the hidden ones (cleared bits of vis) are zero, whatever their operands held
 __device__ __forceinline__ void hide(f32x16& s, f32x16& dp, unsigned vis) {
@@ -227,12 +244,22 @@ __device__ __forceinline__ bool dq_body(const AttnArgs& a, char* smem, int block
             if (base + 8 * (v >> 2) + (v & 3) >= klim) vis &= ~(1u << v);
           if (docs) {
 #pragma unroll
-            for (int v = 0; v < 16; ++v)
-              if (sids[st * BN + 32 * nb + h4 + 8 * (v >> 2) + (v & 3)] != doc) vis &= ~(1u << v);
+            for (int q = 0; q < 4; ++q) {
+              const i32x4 id = *reinterpret_cast<const i32x4*>(sids + st * BN + 32 * nb + h4 + 8 * q);
+#pragma unroll
+              for (int i = 0; i < 4; ++i)
+                if (id[i] != doc) vis &= ~(1u << (4 * q + i));
+            }
           }
         }
-        weights<T>(a, s, dp, [&](int) { return lse2; }, [&](int) { return delta; }, [&](int) { return slope2; },
-                   [&](int v) { return (float)abs(pos - (base + 8 * (v >> 2) + (v & 3))); });
+        auto same = [](float x) { return f32x4{x, x, x, x}; };
+        weights<T>(a, s, dp, [&](int) { return same(lse2); }, [&](int) { return same(delta); }, [&](int) { return same(slope2); },
+                   [&](int q) {
+                     f32x4 f;
+#pragma unroll
+                     for (int i = 0; i < 4; ++i) f[i] = (float)abs(pos - (base + 8 * q + i));
+                     return f;
+                   });
         if (masked) hide(s, dp, vis);
         dscale.apply(dp, acc);
         unrolled<2>([&](auto step) {
@@ -335,11 +362,8 @@ __device__ __forceinline__ bool dkv_body(const AttnArgs& a, char* smem, int bloc
     });
     __syncthreads();
   }
-  const T* qh = (const T*)a.q.p + b * a.q.sb + (long long)hk * a.G * a.q.sh;
-  const T* gh = (const T*)a.dout.p + b * a.dout.sb + (long long)hk * a.G * a.dout.sh;
 
   const long long stat = ((long long)b * a.H + (long long)hk * a.G) * a.Sq;   // [group][q_len] of this head
-  const auto lse_rs = buffer_rsrc(a.lse2 + stat, (uint32_t)a.R * 4u), delta_rs = buffer_rsrc(a.delta + stat, (uint32_t)a.R * 4u);
 
   typename Tile::Lane tl(lane);
   f32x16 dk[DB], dv[DB];
@@ -351,20 +375,22 @@ __device__ __forceinline__ bool dkv_body(const AttnArgs& a, char* smem, int bloc
       zero16(dv[d]);
     }
     dscale = {};
-    auto issue = [&](int t, int st) {
+    auto issue = [&](const AttnArgs& a, int t, int st) {
       int lane = tid & 63;
       asm volatile("" : "+v"(lane));   // the places are formed here, not held over the products
+      const T* qh = (const T*)a.q.p + b * a.q.sb + (long long)hk * a.G * a.q.sh;
+      const T* gh = (const T*)a.dout.p + b * a.dout.sb + (long long)hk * a.G * a.dout.sh;
       Load::packed(qh, a.q.ss, a.q.sh, t * BR, a.R, a.gdiv, a.D, sq + st * Load::BYTES, wave, lane);
       Load::packed(gh, a.dout.ss, a.dout.sh, t * BR, a.R, a.gdiv, a.D, sg + st * Load::BYTES, wave, lane);
       if (wave == 0) {   // rows past the last read zeros: their operands are zero too
         const int r = t * BR + lane, i = (int)a.gdiv.div((uint32_t)r), g = r - i * a.G;
         const uint32_t off = lane < BR && r < a.R ? (uint32_t)((g * a.Sq + i) * 4) : 0x80000000u;
-        buffer_dma4(lse_rs, off, stats[st].lse2);
-        buffer_dma4(delta_rs, off, stats[st].delta);
+        buffer_dma4(buffer_rsrc(a.lse2 + stat, (uint32_t)a.R * 4u), off, stats[st].lse2);
+        buffer_dma4(buffer_rsrc(a.delta + stat, (uint32_t)a.R * 4u), off, stats[st].delta);
       }
     };
     // what only masks and slopes ask for, formed after the tile before
-    auto keep = [&](int t, int st) {
+    auto keep = [&](const AttnArgs& a, int t, int st) {
       if (tid < BR) {
         const int rc = min(t * BR + tid, a.R - 1), i = (int)a.gdiv.div((uint32_t)rc), pos = sc.off + i;
         const int d = docs && pos >= 0 ? docs[pos] : 0;
@@ -376,14 +402,15 @@ __device__ __forceinline__ bool dkv_body(const AttnArgs& a, char* smem, int bloc
     };
     int t = rt.from(rt.t0), st = 0;
     if (t < rt.t1) {
-      issue(t, 0);
-      keep(t, 0);
+      issue(a, t, 0);
+      keep(a, t, 0);
     }
     while (t < rt.t1) {
       __builtin_amdgcn_s_waitcnt(0x0070);
       __syncthreads();
+      const AttnArgs& a = args_again();
       const int tn = rt.from(t + 1);
-      if (tn < rt.t1) issue(tn, st ^ 1);
+      if (tn < rt.t1) issue(a, tn, st ^ 1);
       const int p_first = sc.off + (int)a.gdiv.div((uint32_t)(t * BR));
       const bool masked = docs || k0 + kBwdKeyTile > sc.klim(p_first);
       tl.fresh();
@@ -399,22 +426,26 @@ __device__ __forceinline__ bool dkv_body(const AttnArgs& a, char* smem, int bloc
         if (x % 2) __builtin_amdgcn_sched_barrier(0);   // no more fragments in flight than the accumulators leave room for
       }
       const int rr = 4 * (lane >> 5);
-      auto at = [&](int v) { return rr + 8 * (v >> 2) + (v & 3); };
-      weights<T>(a, s, dp, [&](int v) { return rs.lse2[at(v)]; }, [&](int v) { return rs.delta[at(v)]; },
-                 [&](int v) { return rs.slope2[at(v)]; }, [&](int v) { return (float)abs(rs.pos[at(v)] - j); });
+      auto four = [&](const float* x, int q) { return *reinterpret_cast<const f32x4*>(x + rr + 8 * q); };
+      auto four_i = [&](const int* x, int q) { return *reinterpret_cast<const i32x4*>(x + rr + 8 * q); };
+      weights<T>(a, s, dp, [&](int q) { return four(rs.lse2, q); }, [&](int q) { return four(rs.delta, q); },
+                 [&](int q) { return four(rs.slope2, q); },
+                 [&](int q) {
+                   const i32x4 p = four_i(rs.pos, q);
+                   f32x4 f;
+#pragma unroll
+                   for (int i = 0; i < 4; ++i) f[i] = (float)abs(p[i] - j);
+                   return f;
+                 });
       unsigned vis = 0xffffu;
       if (masked) {
 #pragma unroll
-        for (int v = 0; v < 16; ++v) {
-          if (j >= rs.klim[at(v)]) vis &= ~(1u << v);
-          if (v % 4 == 3) __builtin_amdgcn_sched_barrier(0);
-        }
-        if (docs) {
+        for (int q = 0; q < 4; ++q) {
+          const i32x4 lim = four_i(rs.klim, q), id = four_i(rs.doc, q);
 #pragma unroll
-          for (int v = 0; v < 16; ++v) {
-            if (rs.doc[at(v)] != doc) vis &= ~(1u << v);
-            if (v % 4 == 3) __builtin_amdgcn_sched_barrier(0);
-          }
+          for (int i = 0; i < 4; ++i)
+            if (j >= lim[i] || (docs && id[i] != doc)) vis &= ~(1u << (4 * q + i));
+          __builtin_amdgcn_sched_barrier(0);
         }
         hide(s, dp, vis);
       }
@@ -448,7 +479,7 @@ __device__ __forceinline__ bool dkv_body(const AttnArgs& a, char* smem, int bloc
           __builtin_amdgcn_sched_barrier(0);
         }
       });
-      if (tn < rt.t1) keep(tn, st ^ 1);
+      if (tn < rt.t1) keep(a, tn, st ^ 1);
       t = tn;
       st ^= 1;
     }
