@@ -472,7 +472,7 @@ AttnPlan attn_plan_fwd(int dtype, int B, int Hk, int R, int Sk, int D) {
   // Ranges of the keys.  Tokens: enough workgroups for two on each of 256 compute units, each with at least 64 KB of
   // keys: a call over 777 keys of 8 heads of 64 takes 13.5 us in one range and 20 in four, with the join and its
   // launch; with heads of 128 the ranges pay on the GPU (12 us against 18).  Many rows: as many as run at once, of
-  // at least 256 keys (64 in fp32, whose products take 16 times as long); from 192 tiles on the join's traffic
+  // at least 256 keys (64 in fp32, whose products take several times as long); from 192 tiles on the join's traffic
   // would cost more than idle units do.
   const int row_bytes = (D <= 64 ? 64 : 128) * (dtype == 0 ? 4 : 2);
   if (p.tokens)

@@ -611,9 +611,9 @@ hipError_t run_bwd_dim(hipStream_t s, AttnArgs& a, const AttnBwdPlan& plan, floa
 }
 
 // Ranges of the summed axis: where the tiles are too few for two workgroups on each of 256 compute units, the axis is cut
-// into as many ranges as make 512 of them, of at least 256 keys or rows (64 in fp32, whose products take 16 times as
-// long).  fp32 keeps one workgroup a compute unit busy, but in ranges this short the causal tiles' unequal work
-// evens out: dk and dv of 2 x 8 heads over 2, 513 positions of 64, take 41 us in 25 ranges and 52 in 12.
+// into as many ranges as make 512 of them, of at least 256 keys or rows (64 in fp32, whose products take several
+// times as long).  fp32 keeps one workgroup a compute unit busy, but in shorter ranges the causal tiles' unequal work
+// evens out: half as many made dk and dv of 2 x 8 heads over 2, 513 positions of 64, a quarter slower.
 int ranges(long long blocks, long long axis, int dtype) {
   if (blocks >= 256) return 1;   // the partial sums' traffic would cost more than it gains
   return (int)std::max(1LL, std::min(512 / blocks, axis / (dtype == 0 ? 64 : 256)));
