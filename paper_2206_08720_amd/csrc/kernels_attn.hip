@@ -5,8 +5,8 @@
 //   o' = o 2^(m - m') + v^T p,
 // and o / l at the end, lse = m + log l.  Scores are held in fp32 in units of log2; p is rounded to the
 // inputs' type for the value product (its sum l is not), o and l are fp32.
-#include "attn_core.hpp"
-#include "launch_attn.hpp"
+#include "seq/attn_core.hpp"
+#include "seq/launch_attn.hpp"
 
 namespace ntk {
 namespace {
@@ -251,7 +251,7 @@ __device__ __forceinline__ bool fwd_body(const AttnArgs& a, char* smem, int bloc
   return false;
 }
 template <class T, int DP, bool VEC>
-__global__ void __launch_bounds__(256, 2) k_attn_fwd(const AttnArgs a) {
+__global__ void __launch_bounds__(256, (sizeof(T) * DP <= 256 ? 2 : 1)) k_attn_fwd(const AttnArgs a) {
   extern __shared__ __align__(1024) char smem[];
   const bool bad = fwd_body<T, DP, VEC, false>(a, smem, blockIdx.x);
   if (threadIdx.x == 0) a.flags[blockIdx.x] = bad;

@@ -6,8 +6,8 @@
 // (dq), one owns keys and sums over the rows of every query head that shares them (dk, dv).  Forming the
 // scores twice costs 7 products instead of 5, and buys results that no order of atomics changes.
 // p and ds are rounded to the inputs' type for the products; everything else is fp32.
-#include "attn_core.hpp"
-#include "launch_attn.hpp"
+#include "seq/attn_core.hpp"
+#include "seq/launch_attn.hpp"
 
 namespace ntk {
 namespace {

@@ -10,7 +10,7 @@
 // the columns' sums.
 #include <hip/hip_runtime.h>
 
-#include "launch_seq.hpp"
+#include "seq/launch_seq.hpp"
 
 namespace ntk {
 namespace {
@@ -269,9 +269,9 @@ hipError_t run(hipStream_t s, const NormArgs* f, const NormBwdArgs* b, bool vec)
   }
   const int parts = norm_bwd_parts(b->rows, b->width);
   const dim3 grid((unsigned)(parts / rpb));
-  if (vec)
+  if (parts && vec)
     k_rms_norm_bwd<T, W, TPR, CH, true><<<grid, threads, 0, s>>>(*b);
-  else
+  else if (parts)   // no rows: dw is zero
     k_rms_norm_bwd<T, W, TPR, CH, false><<<grid, threads, 0, s>>>(*b);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;

@@ -7,7 +7,7 @@
 // of 32 + 8 heads of 128 in bf16: 68 us, 5.0 TB/s.
 #include <hip/hip_runtime.h>
 
-#include "launch_seq.hpp"
+#include "seq/launch_seq.hpp"
 
 namespace ntk {
 namespace {

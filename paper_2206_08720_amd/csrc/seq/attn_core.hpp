@@ -21,8 +21,8 @@
 #include <type_traits>
 #include <utility>
 
-#include "gemm_core.hpp"
-#include "index_math.hpp"
+#include "../gemm_core.hpp"
+#include "../index_math.hpp"
 
 namespace ntk {
 

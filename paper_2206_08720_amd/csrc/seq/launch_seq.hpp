@@ -4,7 +4,7 @@
 
 #include <algorithm>
 
-#include "index_math.hpp"
+#include "../index_math.hpp"
 
 namespace ntk {
 

@@ -3,9 +3,9 @@
 #include <math.h>
 #include <stdio.h>
 
-#include "attn_core.hpp"
-#include "launch_attn.hpp"
-#include "launch_seq.hpp"
+#include "seq/attn_core.hpp"
+#include "seq/launch_attn.hpp"
+#include "seq/launch_seq.hpp"
 #include "ntk_seq.h"
 
 namespace ntk {

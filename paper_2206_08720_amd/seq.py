@@ -87,10 +87,13 @@ def _views(*tensors):
 
 
 def _rows(t):
-    """A tensor's rows [rows, width] as (tensor, row stride), without a copy where the rows are evenly spaced."""
+    """A tensor's rows [rows, width] as (tensor, row stride), without a copy where they are evenly spaced and apart (rows of an
+    expanded tensor are not)."""
     if t.dim() != 2:
         t = t.reshape(-1, t.shape[-1])
     rows, width = t.shape
+    if rows > 1 and t.stride(0) < width:
+        t = t.contiguous()
     return t, t.stride(0) if rows > 1 else width
 
 
@@ -102,7 +105,7 @@ def _rms_norm(x, weight, residual, eps, stream, e4m3):
     if x.dim() < 1:
         raise ValueError("x needs a last dimension")
     width = x.shape[-1]
-    if weight.dtype != torch.float32 and weight.dtype != x.dtype:
+    if not isinstance(weight, torch.Tensor) or weight.dtype not in (torch.float32, x.dtype):
         raise TypeError(f"weight must be float32 or {x.dtype}")
     _check(weight, "weight", weight.dtype, device=x.device, shape=x.shape[-1:])
     if residual is not None:
@@ -141,7 +144,7 @@ def rms_norm_backward(dy, h, weight, dh=None, eps=1e-6, stream=None):
     _check(dy, "dy", h.dtype, device=h.device, shape=h.shape)
     if dh is not None:
         _check(dh, "dh", h.dtype, device=h.device, shape=h.shape)
-    if weight.dtype != torch.float32 and weight.dtype != h.dtype:
+    if not isinstance(weight, torch.Tensor) or weight.dtype not in (torch.float32, h.dtype):
         raise TypeError(f"weight must be float32 or {h.dtype}")
     _check(weight, "weight", weight.dtype, device=h.device, shape=h.shape[-1:])
     with _Call(h, stream, (dy, h, weight, dh)) as call:
@@ -150,8 +153,6 @@ def rms_norm_backward(dy, h, weight, dh=None, eps=1e-6, stream=None):
         dr, ds = (None, 0) if dh is None else _rows(dh)
         dx, dweight = torch.empty(h.shape, dtype=h.dtype, device=h.device), torch.empty_like(weight)
         rows = hr.shape[0]
-        if rows == 0:
-            return dx, dweight.zero_()
         need = lib.ntk_rms_norm_workspace(rows, width)
         if need < 0:
             _lib.check(need)

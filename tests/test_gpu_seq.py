@@ -423,6 +423,9 @@ def test_rms_norm_strides_and_values_in_place():
     for lo in (0, 8, 13):
         x = wide[:, lo:lo + 1001]
         _close("y", seq.rms_norm(x, w), *_norm_reference(x.cpu(), None, w.cpu(), 1e-6, "bf16")["y"])
+    one = _rand((1, 1, 64), 631, "bf16").cuda()
+    y, h = seq.rms_norm(one.expand(5, 3, 64), w[:64].clone(), residual=one.expand(5, 3, 64))    # broadcast rows
+    assert torch.equal(y[4, 2], y[0, 0]) and torch.equal(h[4, 2], 2 * one[0, 0])
     x = wide[:3, :64].clone()
     x[1, 5] = math.nan
     y = seq.rms_norm(x, w[:64].clone())
@@ -610,6 +613,11 @@ def test_refusals():
     assert e.value.code == _lib.NTK_E_UNSUPPORTED
     with pytest.raises(ValueError):
         seq.rms_norm(q, torch.zeros(63, device="cuda"))
+    for weight in (None, torch.zeros(64, device="cuda").half(), torch.zeros(64)):
+        with pytest.raises(TypeError):
+            seq.rms_norm(q, weight)
+        with pytest.raises(TypeError):
+            seq.rms_norm_backward(q, q, weight)
     with pytest.raises(_lib.NTKError) as e:
         seq.rotary(q, seq.rotary_table(8, 66))
     assert e.value.code == _lib.NTK_E_SHAPE
