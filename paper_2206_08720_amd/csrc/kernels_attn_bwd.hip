@@ -308,8 +308,8 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) k_attn_dq(const A
 // A wave's keys stay in registers and its values in LDS: with both in registers (and dk, dv in 128 more) only one
 // wave a SIMD would fit, and nothing would run beside its MFMAs.  The loop is written to need no more than 256
 // registers: a reload from scratch memory would wait for the next tile's loads too.  The same sizes as dq's: 386 us and
-// 31 for the sums of two ranges, 660 TFLOP/s of the four products (965 without the causal order, whose first
-// tiles last longest).  dk and dv in workgroups of their own, with one product more, took 500.
+// 31 for the sums of two ranges, 660 TFLOP/s of the four products (about 950 without the causal order, whose first
+// tiles last longest).  dk and dv in workgroups of their own, with one product more, took 520 where this took 440.
 constexpr int kBwdRowTile = 32;
 constexpr int kBwdKeyTile = 128;
 

@@ -86,6 +86,13 @@ def _views(*tensors):
     return [None if t is None else ctypes.byref(array, 32 * i) for i, t in enumerate(tensors)]
 
 
+def _like(t, dtype=None):
+    """A contiguous tensor of t's shape."""
+    if dtype is None and t.is_contiguous():
+        return torch.empty_like(t)
+    return torch.empty(t.shape, dtype=dtype or t.dtype, device=t.device)
+
+
 def _rows(t):
     """A tensor's rows [rows, width] as (tensor, row stride), without a copy where they are evenly spaced and apart (rows of an
     expanded tensor are not)."""
@@ -113,8 +120,8 @@ def _rms_norm(x, weight, residual, eps, stream, e4m3):
     with _Call(x, stream, (x, weight, residual)) as call:
         xr, xs = _rows(x)
         rr, rs = (None, 0) if residual is None else _rows(residual)
-        y = torch.empty(x.shape, dtype=torch.float8_e4m3fn if e4m3 else x.dtype, device=x.device)
-        h = None if residual is None else torch.empty(x.shape, dtype=x.dtype, device=x.device)
+        y = _like(x, torch.float8_e4m3fn if e4m3 else None)
+        h = None if residual is None else _like(x)
         scale = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device) if e4m3 else None
         _lib.check(lib.ntk_rms_norm(_DTYPES[x.dtype], _DTYPES[weight.dtype], xr.shape[0], width, _ptr(xr), xs, _ptr(rr), rs,
                                     _ptr(weight), eps, _ptr(y), _ptr(h), _ptr(scale), call.handle))
@@ -151,7 +158,7 @@ def rms_norm_backward(dy, h, weight, dh=None, eps=1e-6, stream=None):
         hr, hs = _rows(h)
         yr, ys = _rows(dy)
         dr, ds = (None, 0) if dh is None else _rows(dh)
-        dx, dweight = torch.empty(h.shape, dtype=h.dtype, device=h.device), torch.empty_like(weight)
+        dx, dweight = _like(h), _like(weight)
         rows = hr.shape[0]
         need = lib.ntk_rms_norm_workspace(rows, width)
         if need < 0:
@@ -206,8 +213,8 @@ def rotary(q, table, positions=0, k=None, interleaved=False, inverse=False, inpl
         if not positions.is_contiguous():
             raise ValueError("positions must be contiguous")
     with _Call(q, stream, (q, table, k, positions if per_token else None)) as call:
-        qo = q if inplace else torch.empty((b, n, heads, dim), dtype=q.dtype, device=q.device)
-        ko = k if inplace or k is None else torch.empty(k.shape, dtype=k.dtype, device=k.device)
+        qo = q if inplace else _like(q)
+        ko = k if inplace or k is None else _like(k)
         qv, kv, qov, kov = _views(q, k, qo, ko)
         _lib.check(lib.ntk_rotary(_DTYPES[q.dtype], b, n, heads, 0 if k is None else k.shape[2], dim, 2 * table.shape[1],
                                   int(interleaved), int(inverse), qv, kv, _ptr(table), table.shape[0],
@@ -256,7 +263,7 @@ def attention(q, k, v, causal=False, softcap=0.0, scale=None, slopes=None, k_len
     if out is not None:
         _check(out, "out", q.dtype, device=q.device, shape=q.shape)
     with _Call(q, stream, (q, k, v, slopes, k_lens, prefix, docs, out)) as call:
-        o = torch.empty((b, sq, heads, dim), dtype=q.dtype, device=q.device) if out is None else out
+        o = _like(q) if out is None else out
         lse = torch.empty((b, heads, sq), dtype=torch.float32, device=q.device) if return_lse else None
         work, need = _workspace(lib, desc, 0, q.device)
         _lib.check(lib.ntk_attention(ctypes.byref(desc), *_views(q, k, v, o), _ptr(lse), _ptr(work), need, call.handle))
@@ -275,8 +282,7 @@ def attention_backward(do, q, k, v, o, lse, causal=False, softcap=0.0, scale=Non
     if not lse.is_contiguous():
         raise ValueError("lse must be contiguous")
     with _Call(q, stream, (do, q, k, v, o, lse, slopes, k_lens, prefix, docs)) as call:
-        dq = torch.empty((b, sq, heads, dim), dtype=q.dtype, device=q.device)
-        dk, dv = (torch.empty(k.shape, dtype=k.dtype, device=k.device) for _ in range(2))
+        dq, dk, dv = _like(q), _like(k), _like(v)
         work, need = _workspace(lib, desc, 1, q.device)
         views = _views(do, q, k, v, o, dq, dk, dv)
         _lib.check(lib.ntk_attention_bwd(ctypes.byref(desc), *views[:5], _ptr(lse), *views[5:], _ptr(work), need, call.handle))

@@ -247,6 +247,28 @@ def test_other_documents_values_do_not_spread(type):
     assert torch.isinf(o[0, 60:80, 1, 7]).all() and torch.isfinite(o[0, 60:80, 1, :7]).all()
 
 
+@pytest.mark.parametrize("seed", range(60))
+def test_random_attention(seed):
+    """Random types, sizes, head groups, lengths, masks and layouts, forward and backward."""
+    import random
+    rng = random.Random(9000 + seed)
+    type = rng.choice(("bf16", "f16", "f32"))
+    B, Hk, G = rng.choice((1, 1, 2, 3)), rng.choice((1, 2, 3)), rng.choice((1, 2, 3, 5, 8))
+    D = rng.choice((64, 128, rng.randrange(1, 129), 8 * rng.randrange(1, 17)))
+    Sk = rng.choice((1, rng.randrange(2, 40), rng.randrange(40, 400), 64 * rng.randrange(1, 6)))
+    Sq = rng.choice((1, Sk, Sk, rng.randrange(1, Sk + 1), min(Sk + 3, 50)))
+    causal = rng.random() < 0.6
+    opt = {"causal": causal, "softcap": rng.choice((0.0, 0.0, 3.0, 30.0)), "slopes": rng.random() < 0.3,
+           "scale": rng.choice((None, None, 0.01, 0.6)), "layout": rng.choice(("plain", "plain", "heads_first", "odd"))}
+    if rng.random() < 0.4:
+        opt["k_lens"] = [rng.choice((0, 1, Sk, rng.randrange(Sk + 1))) for _ in range(B)]
+    if causal and rng.random() < 0.3:
+        opt["prefix"] = [rng.randrange(Sk + 1) for _ in range(B)]
+    if rng.random() < 0.4:
+        opt["docs"] = [rng.choice((-1, 0, 0, 1, 2)) if rng.random() < 0.1 else j // rng.choice((20, 70)) for _ in range(B) for j in range(Sk)]
+    _attention(type, B, Sq, Sk, G * Hk, Hk, D, seed=9100 + 7 * seed, train=rng.random() < 0.7, **opt)
+
+
 def test_attention_rows_that_see_nothing():
     import torch
     got = _attention("bf16", 2, 8, 20, 2, 1, 64, seed=440, train=True, causal=True, k_lens=[3, 0])
