@@ -104,6 +104,19 @@ struct DsScale {
   __device__ __forceinline__ float undo() const { return 1.f / (mul * kPScale<T>); }
 };
 
+// With heads of 128 the wave that multiplies into dq, dk or dv goes before the other one of its SIMD (2 x 16 heads over 8,
+// 4096 positions: 924 us a backward pass against 990, 600 against 634-666 causal).  Heads of 64 gain nothing, nor does
+// the forward kernel.
+template <int DP>
+__device__ __forceinline__ void multiply_first(int on) {
+  if constexpr (DP == 128) {
+    if (on)
+      __builtin_amdgcn_s_setprio(1);
+    else
+      __builtin_amdgcn_s_setprio(0);
+  }
+}
+
 template <class T, bool VEC>
 __global__ void __launch_bounds__(256) k_attn_delta(const AttnArgs a, float* __restrict__ lse2, float* __restrict__ delta,
                                                     long long rows) {
@@ -141,8 +154,8 @@ __global__ void __launch_bounds__(256) k_attn_delta(const AttnArgs a, float* __r
 }
 
 // ---- dq: four waves of 32 rows over the key tiles -----------------------------------------------------
-// The forward kernel's plan with a third product.  bf16, 2 x 16 heads over 8 of 128, 4096 positions, causal: 225 us,
-// 915 TFLOP/s of its three products.
+// The forward kernel's plan with a third product.  bf16, 2 x 16 heads over 8 of 128, 4096 positions, causal: 210 us,
+// 982 TFLOP/s of its three products.
 template <class T>
 constexpr int kBwdKeys = sizeof(T) == 2 ? 64 : 32;
 constexpr int kBwdRows = 128;
@@ -264,6 +277,7 @@ __device__ __forceinline__ bool dq_body(const AttnArgs& a, char* smem, int block
                    });
         if (masked) hide(s, dp, vis);
         dscale.apply(dp, acc);
+        multiply_first<DP>(1);
         unrolled<2>([&](auto step) {
           constexpr int u = decltype(step)::value;
           const Frag w = to_frag<T>(dp, u);
@@ -282,6 +296,7 @@ __device__ __forceinline__ bool dq_body(const AttnArgs& a, char* smem, int block
             for (int d = 0; d < DB; ++d) acc[d] = N::mma(kc[d], w, acc[d]);
           }
         });
+        multiply_first<DP>(0);
       });
       if (docs && tn < kt.t1 && tid < BN) sids[(st ^ 1) * BN + tid] = nid;
       t = tn;
@@ -307,8 +322,8 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) k_attn_dq(const A
 // ---- dk, dv: four waves of 32 keys over the row tiles -----------------------------------------------------
 // A wave's keys stay in registers and its values in LDS: with both in registers (and dk, dv in 128 more) only one
 // wave a SIMD would fit, and nothing would run beside its MFMAs.  The loop is written to need no more than 256
-// registers: a reload from scratch memory would wait for the next tile's loads too.  The same sizes as dq's: 386 us and
-// 31 for the sums of two ranges, 660 TFLOP/s of the four products (about 950 without the causal order, whose first
+// registers: a reload from scratch memory would wait for the next tile's loads too.  The same sizes as dq's: 372 us and
+// 31 for the sums of two ranges, 682 TFLOP/s of the four products (about 1000 without the causal order, whose first
 // tiles last longest).  dk and dv in workgroups of their own, with one product more, took 520 where this took 440.
 constexpr int kBwdRowTile = 32;
 constexpr int kBwdKeyTile = 128;
@@ -460,6 +475,7 @@ __device__ __forceinline__ bool dkv_body(const AttnArgs& a, char* smem, int bloc
       dscale.apply(dp, dk);
       const Frag pf[2] = {to_frag<T>(s, 0), to_frag<T>(s, 1)}, wf[2] = {to_frag<T>(dp, 0), to_frag<T>(dp, 1)};
       __builtin_amdgcn_sched_barrier(0);
+      multiply_first<DP>(1);
       unrolled<2>([&](auto step) {
         constexpr int u = decltype(step)::value;
         const Frag p = pf[u], w = wf[u];
@@ -484,6 +500,7 @@ __device__ __forceinline__ bool dkv_body(const AttnArgs& a, char* smem, int bloc
           __builtin_amdgcn_sched_barrier(0);
         }
       });
+      multiply_first<DP>(0);
       if (tn < rt.t1) keep(a, tn, st ^ 1);
       t = tn;
       st ^= 1;
