@@ -4,7 +4,7 @@
 //   s = score(k q^T), m' = max(m, max s), p = 2^(s - m'), l' = l 2^(m - m') + sum p,
 //   o' = o 2^(m - m') + v^T p,
 // and o / l at the end, lse = m + log l.  Scores are held in fp32 in units of log2; p is rounded to the
-// inputs' type for the value product (its sum l is not), o and l are fp32.
+// inputs' type for the value product (its sum l is not), in fp16 times 2^14 (kWeightBits); o and l are fp32.
 #include "seq/attn_core.hpp"
 #include "seq/launch_attn.hpp"
 
@@ -102,7 +102,8 @@ struct FwdRows {
 #pragma unroll
         for (int v = 0; v < 16; ++v) acc[d][v] *= f;
     }
-    const float mu = m == -__builtin_inff() ? 0.f : -m * unit;    // nothing seen yet: every weight is 2^-inf = 0
+    // nothing seen yet: every weight is 2^-inf = 0
+    const float mu = m == -__builtin_inff() ? 0.f : fmaf(-m, unit, kWeightBits<T>);
     float sum = 0.f;
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb)
@@ -156,7 +157,7 @@ __device__ __forceinline__ void finish_row(const AttnArgs& a, FwdRows<T, DP>& w,
   T* o = (T*)a.o.p + b * a.o.sb + i * a.o.ss + head * a.o.sh;
   store_owned<T, DP, VEC>(o, a.D, lane, w.acc, inv);
   if (a.lse && lane < 32)
-    a.lse[((long long)b * a.H + head) * a.Sq + i] = w.l == 0.f ? -__builtin_inff() : m2 * kLn2 + logf(w.l);
+    a.lse[((long long)b * a.H + head) * a.Sq + i] = w.l == 0.f ? -__builtin_inff() : m2 * kLn2 + logf(w.l * kWeightOne<T>);
 }
 
 // ---- many rows: four waves of 32 rows share the key tiles in LDS ---------------------------------------
@@ -424,7 +425,7 @@ __global__ void __launch_bounds__(DP) k_attn_join(const AttnArgs a) {
   const int i = (int)a.gdiv.div((uint32_t)r), head = hk * a.G + r - i * a.G;
   if (d < a.D) ((T*)a.o.p)[b * a.o.sb + i * a.o.ss + head * a.o.sh + d] = (T)(l == 0.f ? 0.f : o / l);
   if (a.lse && d == 0)
-    a.lse[((long long)b * a.H + head) * a.Sq + i] = l == 0.f ? -__builtin_inff() : m * kLn2 + logf(l);
+    a.lse[((long long)b * a.H + head) * a.Sq + i] = l == 0.f ? -__builtin_inff() : m * kLn2 + logf(l * kWeightOne<T>);
 }
 
 template <class T, int DP, bool VEC>

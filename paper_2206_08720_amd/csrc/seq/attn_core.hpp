@@ -448,6 +448,14 @@ __device__ __forceinline__ float half_sum(float x) {
   return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
 
+// fp16 keeps 11 bits only above 2^-14 and nothing below 2^-25, and thousands of weights that small can make up a result
+// whose largest weight meets a value near zero.  The forward pass forms its weights times 2^14, at most a quarter of the largest
+// fp16; their sum l and the products carry the factor alike, so that only lse has to take it out.
+template <class T>
+constexpr float kWeightBits = std::is_same_v<T, _Float16> ? 14.f : 0.f;
+template <class T>
+constexpr float kWeightOne = std::is_same_v<T, _Float16> ? 0x1p-14f : 1.f;   // 2^-kWeightBits
+
 __device__ __forceinline__ float exp2_hw(float x) { return __builtin_amdgcn_exp2f(x); }
 
 // The capped score in log2 units, cap log2(e) tanh(scale x / cap), with tanh(y) = 1 - 2 / (e^2y + 1): an absolute
