@@ -38,7 +38,7 @@ struct FwdRows {
                                          int lane, const typename Tile::Lane& tl, f32x16& s, unsigned& vis) const {
     zero16(s);
 #pragma unroll
-    for (int t = 0; t < KT; ++t) s = N::mma(Tile::rows(sk, 32 * nb, t, tl), q[t], s);
+    for (int t = 0; t < KT; ++t) s = N::template product<Careful::value>(Tile::rows(sk, 32 * nb, t, tl), q[t], s);
     const int h4 = 4 * (lane >> 5), base = key0 + 32 * nb + h4;
     if (a.cap_in != 0.f) {
 #pragma unroll

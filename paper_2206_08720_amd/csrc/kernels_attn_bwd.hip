@@ -247,8 +247,8 @@ __device__ __forceinline__ bool dq_body(const AttnArgs& a, char* smem, int block
         zero16(dp);
 #pragma unroll
         for (int x = 0; x < KT; ++x) {
-          s = N::mma(Tile::rows(k_, 32 * nb, x, tl), q[x], s);
-          dp = N::mma(Tile::rows(v_, 32 * nb, x, tl), g[x], dp);
+          s = N::template product<CAREFUL>(Tile::rows(k_, 32 * nb, x, tl), q[x], s);
+          dp = N::template product<CAREFUL>(Tile::rows(v_, 32 * nb, x, tl), g[x], dp);
           if (x % 2) __builtin_amdgcn_sched_barrier(0);
         }
         const int h4 = 4 * (lane >> 5), base = t * BN + 32 * nb + h4;
@@ -441,8 +441,8 @@ __device__ __forceinline__ bool dkv_body(const AttnArgs& a, char* smem, int bloc
       zero16(dp);
 #pragma unroll
       for (int x = 0; x < KT; ++x) {
-        s = N::mma(Tile::rows(q_, 0, x, tl), k[x], s);
-        dp = N::mma(Tile::rows(g_, 0, x, tl), Tile::rows(sv, 32 * wave, x, tl), dp);
+        s = N::template product<CAREFUL>(Tile::rows(q_, 0, x, tl), k[x], s);
+        dp = N::template product<CAREFUL>(Tile::rows(g_, 0, x, tl), Tile::rows(sv, 32 * wave, x, tl), dp);
         if (x % 2) __builtin_amdgcn_sched_barrier(0);   // no more fragments in flight than the accumulators leave room for
       }
       const int rr = 4 * (lane >> 5);

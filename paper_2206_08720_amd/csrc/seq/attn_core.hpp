@@ -46,6 +46,8 @@ struct Num<__bf16> {
   __device__ static __forceinline__ f32x16 mma(Frag a, Frag b, f32x16 c) {
     return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
   }
+  template <bool CAREFUL>
+  __device__ static __forceinline__ f32x16 product(Frag a, Frag b, f32x16 c) { return mma(a, b, c); }
 };
 template <>
 struct Num<_Float16> {
@@ -54,16 +56,19 @@ struct Num<_Float16> {
   __device__ static __forceinline__ f32x16 mma(Frag a, Frag b, f32x16 c) {
     return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
   }
+  template <bool CAREFUL>
+  __device__ static __forceinline__ f32x16 product(Frag a, Frag b, f32x16 c) { return mma(a, b, c); }
 };
 template <>
 struct Num<float> {
   using Frag = f32x8;
   using Four = f32x4;
   // x = h + m + l in three bf16 values of 8 bits each (the whole 24 of an fp32, at its full range; h is cut, not
-  // rounded, so that the largest stay finite).  What is not finite stays in h alone: the rest is clamped, so that
-  // inf - inf does not enter.  Six products of parts take 192 cycles of the matrix cores where eight fp32 MFMAs of the
-  // same 16 k take 512; what bounds the fp32 kernels then is the splitting on the vector units (8 heads of 64, 4096
-  // positions: 320 us forward and 1130 backward, against 359 and 1202 on the fp32 MFMAs).
+  // rounded, so that the largest stay finite).  Six products of parts take 192 cycles of the matrix cores where eight
+  // fp32 MFMAs of the same 16 k take 512; what bounds the fp32 kernels then is the splitting on the vector units (8 heads
+  // of 64, 4096 positions: 320 us forward and 1130 backward, against 359 and 1202 on the fp32 MFMAs).
+  // What is not finite has parts that are NaN, so every result that it meets is NaN; such a result is formed again on the
+  // fp32 MFMAs (product<true>), where inf times a number is inf of the right sign.
   struct Parts {
     bf16x8 h, m, l;
   };
@@ -72,7 +77,7 @@ struct Num<float> {
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       const uint32_t u = __float_as_uint(x[i]);
-      const float r = fminf(fmaxf(x[i] - __uint_as_float(u & 0xffff0000u), -0x1p121f), 0x1p121f);
+      const float r = x[i] - __uint_as_float(u & 0xffff0000u);   // inf and NaN: NaN
       const __bf16 m = (__bf16)r;
       p.h[i] = __builtin_bit_cast(__bf16, (unsigned short)(u >> 16));
       p.m[i] = m;
@@ -89,6 +94,17 @@ struct Num<float> {
     c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x.m, y.h, c, 0, 0, 0);
     c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x.h, y.m, c, 0, 0, 0);
     return __builtin_amdgcn_mfma_f32_32x32x16_bf16(x.h, y.h, c, 0, 0, 0);
+  }
+  // CAREFUL: eight fp32 MFMAs, the i-th on the i-th element of both operands
+  template <bool CAREFUL>
+  __device__ static __forceinline__ f32x16 product(Frag a, Frag b, f32x16 c) {
+    if constexpr (CAREFUL) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a[i], b[i], c, 0, 0, 0);
+      return c;
+    } else {
+      return mma(a, b, c);
+    }
   }
 };
 
@@ -486,7 +502,7 @@ __device__ __forceinline__ f32x16 mma_visible(typename Num<T>::Frag a, typename 
 #pragma unroll
   for (int i = 0; i < 8; ++i) f[i] = (T)(__builtin_isfinite((float)a[i]) ? 0.f : 1.f);
   __builtin_amdgcn_sched_barrier(0);
-  z = Num<T>::mma(f, vis, z);               // how many of them an element meets
+  z = Num<T>::template product<true>(f, vis, z);               // how many of them an element meets
   unsigned n[4] = {0, 0, 0, 0};             // at most 16: a byte each
 #pragma unroll
   for (int v = 0; v < 16; ++v) n[v >> 2] |= (unsigned)z[v] << (8 * (v & 3));
@@ -494,11 +510,11 @@ __device__ __forceinline__ f32x16 mma_visible(typename Num<T>::Frag a, typename 
   zero16(z);
 #pragma unroll
   for (int i = 0; i < 8; ++i) f[i] = (T)(__builtin_isinf((float)a[i]) ? ((float)a[i] > 0.f ? 1.f : -1.f) : 0.f);
-  z = Num<T>::mma(f, vis, z);               // inf counted up, -inf down
+  z = Num<T>::template product<true>(f, vis, z);               // inf counted up, -inf down
   __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
   for (int i = 0; i < 8; ++i) f[i] = __builtin_isfinite((float)a[i]) ? a[i] : (T)0.f;
-  acc = Num<T>::mma(f, w, acc);
+  acc = Num<T>::template product<true>(f, w, acc);
 #pragma unroll
   for (int v = 0; v < 16; ++v) {
     const float c = (float)((n[v >> 2] >> (8 * (v & 3))) & 255u);

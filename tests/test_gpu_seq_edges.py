@@ -28,3 +28,94 @@ def test_fp16_weights_far_below_the_largest(rows, keys, heads, gap):
     ref = _oracle(q[:, :, few], k[:, :, few], v[:, :, few], "f16", inner=2.0 ** -39)
     _close("o", o[:, :, few], *ref["o"])
     _close("lse", lse[:, few], *ref["lse"])
+
+
+# ---- infinities -----------------------------------------------------------------------------------------------------
+
+FORMS = [("f32", 1), ("f32", 64), ("bf16", 1), ("bf16", 64), ("f16", 64)]
+
+
+@pytest.mark.parametrize("type,rows", FORMS)
+def test_visible_key_at_minus_infinity(type, rows):
+    """A key that is -inf where all queries are positive has scores of -inf and no weight: o, lse, dv and the other keys' dk are
+    those without it, its own dk and dv are 0; dq meets 0 * inf in that component alone."""
+    import torch
+    from paper_2206_08720_amd import seq
+    n, D, at, d = 150, 64, 70, 3
+    q, k, v, do = (_rand((1, m, 2, D), 910 + i, type) for i, m in enumerate((rows, n, n, rows)))
+    q[..., d] = q[..., d].abs() + 0.5
+    keep = [j for j in range(n) if j != at]
+    ref = _oracle(q, k[:, keep], v[:, keep], type, do)
+    k[0, at, :, d] = -math.inf
+    o, lse = seq.attention(q.cuda(), k.cuda(), v.cuda(), return_lse=True)
+    _close("o", o, *ref["o"])
+    _close("lse", lse, *ref["lse"])
+    if rows % 32:
+        return
+    dq, dk, dv = seq.attention_backward(do.cuda(), q.cuda(), k.cuda(), v.cuda(), o, lse)
+    _close("dk", dk[:, keep], *ref["dk"])
+    _close("dv", dv[:, keep], *ref["dv"])
+    assert not dk[0, at].any() and not dv[0, at].any()
+    rest = [c for c in range(D) if c != d]
+    _close("dq", dq[..., rest], ref["dq"][0][..., rest], ref["dq"][1][..., rest])
+    assert not torch.isfinite(dq[..., d]).any()
+
+
+@pytest.mark.parametrize("type,rows", FORMS)
+def test_infinities_reach_what_meets_them(type, rows):
+    """An infinite key: rows whose score is -inf do without it, those at +inf or 0 * inf are NaN.  An infinite query: its row alone.
+    An infinite value or gradient of o: its component alone, with its sign."""
+    import torch
+    from paper_2206_08720_amd import seq
+    n, D, at, d = 150, 64, 20, 5
+    q, k, v = (_rand((1, m, 2, D), 920 + i, type) for i, m in enumerate((rows, n, n)))
+    keep = [j for j in range(n) if j != at]
+    q[0, -1, :, d] = 0.0
+    for value in (math.inf, -math.inf):
+        spoilt = k.clone()
+        spoilt[0, at, :, d] = value
+        out = seq.attention(q.cuda(), spoilt.cuda(), v.cuda()).cpu()
+        without = (q[..., d].double() * value == -math.inf)[..., None].expand(out.shape)
+        ref, tol = _oracle(q, k[:, keep], v[:, keep], type)["o"]
+        _close("o", torch.where(without, out.double(), 0.0), torch.where(without, ref, 0.0), tol)
+        assert torch.isnan(out[~without]).all()
+        spoilt = v.clone()
+        spoilt[0, at, :, d] = value
+        out = seq.attention(q.cuda(), k.cuda(), spoilt.cuda()).cpu()
+        ref, tol = _oracle(q, k, v, type)["o"]
+        assert (out[..., d] == value).all()
+        out[..., d], ref[..., d] = 0.0, 0.0
+        _close("o", out, ref, tol)
+        spoilt = q.clone()
+        spoilt[0, 0, 0, d] = value
+        out = seq.attention(spoilt.cuda(), k.cuda(), v.cuda()).cpu()
+        ref, tol = _oracle(q, k, v, type)["o"]
+        assert torch.isnan(out[0, 0, 0]).all()
+        out[0, 0, 0], ref[0, 0, 0] = 0.0, 0.0
+        _close("o", out, ref, tol)
+
+
+@pytest.mark.parametrize("type", ["f32", "bf16", "f16"])
+def test_infinite_gradient_reaches_its_component_of_dv(type):
+    import torch
+    from paper_2206_08720_amd import seq
+    q, k, v, do = (_rand((1, m, 2, 64), 930 + i, type) for i, m in enumerate((64, 150, 150, 64)))
+    ref, tol = _oracle(q, k, v, type, do)["dv"]
+    do[0, 9, :, 5] = -math.inf
+    o, lse = seq.attention(q.cuda(), k.cuda(), v.cuda(), return_lse=True)
+    dv = seq.attention_backward(do.cuda(), q.cuda(), k.cuda(), v.cuda(), o, lse)[2].cpu()
+    assert (dv[..., 5] == -math.inf).all()
+    dv[..., 5], ref[..., 5] = 0.0, 0.0
+    _close("dv", dv, ref, tol)
+
+
+@pytest.mark.parametrize("rows", [1, 64])
+def test_nan_of_any_payload_stays_nan(rows):
+    """fp32 NaN whose payload lies in the lowest bit, of either sign."""
+    import torch
+    from paper_2206_08720_amd import seq
+    q, k, v = (_rand((1, m, 1, 64), 940 + i) for i, m in enumerate((rows, 150, 150)))
+    q[..., 5] = q[..., 5].abs() + 0.5
+    for bits in (0x7f800001, 0xff800001 - (1 << 32)):
+        k[0, 20].view(torch.int32)[0, 5] = bits
+        assert torch.isnan(seq.attention(q.cuda(), k.cuda(), v.cuda())).all()
