@@ -129,7 +129,7 @@ struct FwdRows {
         for (int i = 0; i < 8; ++i) w[i] = (T)((vis[nb] >> (8 * u + i)) & 1 ? 1.f : 0.f);
         unrolled<DB>([&](auto block) {
           constexpr int d = decltype(block)::value;
-          acc[d] = mma_visible<T>(vc.template read_one<16 * X, d>(tl), p, w, acc[d]);
+          acc[d] = mma_visible<T, true>(vc.template read_one<16 * X, d>(tl), p, w, acc[d]);
         });
       }
     });

@@ -287,7 +287,7 @@ __device__ __forceinline__ bool dq_body(const AttnArgs& a, char* smem, int block
             for (int e = 0; e < 8; ++e) on[e] = (T)((vis >> (8 * u + e)) & 1 ? 1.f : 0.f);
             unrolled<DB>([&](auto db) {
               constexpr int d = decltype(db)::value;
-              acc[d] = mma_visible<T>(cols.template read_one<32 * nb + 16 * u, d>(tl), w, on, acc[d]);
+              acc[d] = mma_visible<T, false>(cols.template read_one<32 * nb + 16 * u, d>(tl), w, on, acc[d]);
             });
           } else {
             Frag kc[DB];
@@ -485,8 +485,8 @@ __device__ __forceinline__ bool dkv_body(const AttnArgs& a, char* smem, int bloc
           for (int e = 0; e < 8; ++e) on[e] = (T)((vis >> (8 * u + e)) & 1 ? 1.f : 0.f);
           unrolled<DB>([&](auto db) {
             constexpr int d = decltype(db)::value;
-            dv[d] = mma_visible<T>(qcols.template read_one<16 * u, d, GQ>(tl), p, on, dv[d]);
-            dk[d] = mma_visible<T>(qcols.template read_one<16 * u, d>(tl), w, on, dk[d]);
+            dv[d] = mma_visible<T, true>(qcols.template read_one<16 * u, d, GQ>(tl), p, on, dv[d]);
+            dk[d] = mma_visible<T, false>(qcols.template read_one<16 * u, d>(tl), w, on, dk[d]);
           });
         } else {
           Frag gc[DB], qc[DB];

@@ -489,9 +489,13 @@ __device__ __forceinline__ void zero16(f32x16& a) {
 
 // ---- operands that are not finite ------------------------------------------------------------------
 // A hidden (row, key) pair has weight 0, and 0 * inf is NaN: where a result comes out not finite, the tile is
-// computed again with this product.  It multiplies the finite elements and adds, as inf, -inf or NaN,
-// the others that a *visible* pair meets: `vis` holds 1 for such pairs, 0 for the hidden ones.
-template <class T>
+// computed again with this product.  It multiplies the finite elements and adds what the others give that a *visible* pair
+// meets (`vis` holds 1 for such pairs, 0 for the hidden ones):
+//   POSITIVE   the weights are a softmax's: inf, -inf or NaN, as the elements are, also where a weight is too small
+//              for its type;
+//   else       they are ds, and `a` is k or q: its infinity made the pair's score -inf, +inf or +-cap, so ds is 0 or
+//              NaN, and the sum NaN.
+template <class T, bool POSITIVE>
 __device__ __forceinline__ f32x16 mma_visible(typename Num<T>::Frag a, typename Num<T>::Frag w, typename Num<T>::Frag vis,
                                               f32x16 acc) {
   using Frag = typename Num<T>::Frag;
@@ -502,16 +506,18 @@ __device__ __forceinline__ f32x16 mma_visible(typename Num<T>::Frag a, typename 
 #pragma unroll
   for (int i = 0; i < 8; ++i) f[i] = (T)(__builtin_isfinite((float)a[i]) ? 0.f : 1.f);
   __builtin_amdgcn_sched_barrier(0);
-  z = Num<T>::template product<true>(f, vis, z);               // how many of them an element meets
-  unsigned n[4] = {0, 0, 0, 0};             // at most 16: a byte each
+  z = Num<T>::template product<true>(f, vis, z);   // how many of them an element meets
+  unsigned n[4] = {0, 0, 0, 0};                    // at most 16: a byte each
 #pragma unroll
   for (int v = 0; v < 16; ++v) n[v >> 2] |= (unsigned)z[v] << (8 * (v & 3));
   __builtin_amdgcn_sched_barrier(0);
   zero16(z);
+  if constexpr (POSITIVE) {
 #pragma unroll
-  for (int i = 0; i < 8; ++i) f[i] = (T)(__builtin_isinf((float)a[i]) ? ((float)a[i] > 0.f ? 1.f : -1.f) : 0.f);
-  z = Num<T>::template product<true>(f, vis, z);               // inf counted up, -inf down
-  __builtin_amdgcn_sched_barrier(0);
+    for (int i = 0; i < 8; ++i) f[i] = (T)(__builtin_isinf((float)a[i]) ? ((float)a[i] > 0.f ? 1.f : -1.f) : 0.f);
+    z = Num<T>::template product<true>(f, vis, z);   // inf counted up, -inf down
+    __builtin_amdgcn_sched_barrier(0);
+  }
 #pragma unroll
   for (int i = 0; i < 8; ++i) f[i] = __builtin_isfinite((float)a[i]) ? a[i] : (T)0.f;
   acc = Num<T>::template product<true>(f, w, acc);
