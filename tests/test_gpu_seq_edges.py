@@ -141,3 +141,41 @@ def test_infinite_operand_against_a_weight_of_zero_is_nan(type, cap):
             o, lse = seq.attention(q.cuda(), k.cuda(), v.cuda(), softcap=cap, return_lse=True)
             dq, dk, _ = seq.attention_backward(do.cuda(), q.cuda(), k.cuda(), v.cuda(), o, lse, softcap=cap)
             assert torch.isnan(dk[..., 3]).all() and torch.isfinite(dk[..., :3]).all() and torch.isfinite(dq).all()
+
+
+# ---- heads dealt out to the dies ------------------------------------------------------------------------------------
+
+def _spoil_tail(q, k, v, do):
+    k[0, -40:], v[0, -40:] = math.nan, math.inf
+
+
+EIGHTS = [
+    # batch * kv_heads is 8 or 16: each die takes its own heads; several tiles and ranges a head
+    ("bf16", 1, 300, 300, 8, 8, 64, {"causal": True, "train": True}),
+    ("f32", 2, 300, 300, 8, 8, 64, {"causal": True, "train": True}),
+    ("bf16", 2, 520, 520, 16, 8, 128, {"causal": True, "train": True}),
+    ("f16", 4, 200, 390, 4, 2, 80, {"train": True, "softcap": 20.0}),
+    ("f16", 2, 300, 300, 16, 4, 64, {"causal": True, "train": True, "docs": [j // 90 for _ in range(2) for j in range(300)]}),
+    ("bf16", 2, 1, 4000, 16, 8, 128, {"k_lens": [4000, 1777]}),
+    ("f32", 8, 3, 1200, 2, 1, 64, {"causal": True}),
+    ("bf16", 2, 1, 4000, 8, 8, 64, {"k_lens": [3960, 4000], "spoil": _spoil_tail}),
+    ("bf16", 2, 300, 300, 8, 4, 64, {"causal": True, "train": True, "k_lens": [260, 300], "spoil": _spoil_tail}),
+    ("f32", 1, 200, 300, 8, 8, 128, {"train": True, "k_lens": [260], "spoil": _spoil_tail}),
+]
+
+
+@pytest.mark.parametrize("case", EIGHTS, ids=lambda c: f"{c[0]}-{c[1]}x{c[2]}x{c[3]}-{c[4]}.{c[5]}.{c[6]}-{'.'.join(c[7])}")
+def test_heads_in_eights(case):
+    _attention(*case[:7], seed=950, **case[7])
+
+
+@pytest.mark.parametrize("seed", range(12))
+def test_random_attention_of_eight_heads(seed):
+    import random
+    rng = random.Random(9500 + seed)
+    type, B, G = rng.choice(("bf16", "f16", "f32")), rng.choice((1, 2)), rng.choice((1, 2))
+    Sk = rng.randrange(130, 420)
+    opt = {"causal": rng.random() < 0.6, "softcap": rng.choice((0.0, 10.0)), "slopes": rng.random() < 0.3}
+    if rng.random() < 0.4:
+        opt["k_lens"] = [rng.randrange(Sk + 1) for _ in range(B)]
+    _attention(type, B, rng.choice((2, Sk, Sk)), Sk, 8 * G, 8, rng.choice((40, 64, 128)), seed=9600 + 7 * seed, train=True, **opt)
