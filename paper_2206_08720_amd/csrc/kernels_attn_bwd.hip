@@ -402,7 +402,7 @@ __device__ __forceinline__ bool dkv_body(const AttnArgs& a, char* smem, int bloc
       const T* gh = (const T*)a.dout.p + b * a.dout.sb + (long long)hk * a.G * a.dout.sh;
       Load::packed(qh, a.q.ss, a.q.sh, t * BR, a.R, a.gdiv, a.D, sq + st * Load::BYTES, wave, lane);
       Load::packed(gh, a.dout.ss, a.dout.sh, t * BR, a.R, a.gdiv, a.D, sg + st * Load::BYTES, wave, lane);
-      if (wave == 0) {   // rows past the last read zeros: their operands are zero too
+      if (wave == 0) {   // rows past the last read zeros, and see no key
         const int r = t * BR + lane, i = (int)a.gdiv.div((uint32_t)r), g = r - i * a.G;
         const uint32_t off = lane < BR && r < a.R ? (uint32_t)((g * a.Sq + i) * 4) : 0x80000000u;
         buffer_dma4(buffer_rsrc(a.lse2 + stat, (uint32_t)a.R * 4u), off, stats[st].lse2);
@@ -415,7 +415,7 @@ __device__ __forceinline__ bool dkv_body(const AttnArgs& a, char* smem, int bloc
         const int rc = min(t * BR + tid, a.R - 1), i = (int)a.gdiv.div((uint32_t)rc), pos = sc.off + i;
         const int d = docs && pos >= 0 ? docs[pos] : 0;
         stats[st].slope2[tid] = a.slopes ? a.slopes[hk * a.G + rc - i * a.G] * kLog2e : 0.f;
-        stats[st].klim[tid] = d >= 0 ? sc.klim(pos) : 0;
+        stats[st].klim[tid] = d >= 0 && t * BR + tid < a.R ? sc.klim(pos) : 0;
         stats[st].pos[tid] = pos;
         stats[st].doc[tid] = d;
       }
@@ -432,7 +432,8 @@ __device__ __forceinline__ bool dkv_body(const AttnArgs& a, char* smem, int bloc
       const int tn = rt.from(t + 1);
       if (tn < rt.t1) issue(a, tn, st ^ 1);
       const int p_first = sc.off + (int)a.gdiv.div((uint32_t)(t * BR));
-      const bool masked = docs || k0 + kBwdKeyTile > sc.klim(p_first);
+      // rows past the last have operands of zeros, but a weight that is not finite would make them NaN
+      const bool masked = docs || k0 + kBwdKeyTile > sc.klim(p_first) || (t + 1) * BR > a.R;
       tl.fresh();
       const char *q_ = sq + st * Load::BYTES, *g_ = sg + st * Load::BYTES;
       const RowStats& rs = stats[st];

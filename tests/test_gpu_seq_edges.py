@@ -179,3 +179,73 @@ def test_random_attention_of_eight_heads(seed):
     if rng.random() < 0.4:
         opt["k_lens"] = [rng.randrange(Sk + 1) for _ in range(B)]
     _attention(type, B, rng.choice((2, Sk, Sk)), Sk, 8 * G, 8, rng.choice((40, 64, 128)), seed=9600 + 7 * seed, train=True, **opt)
+
+
+# ---- row tiles that end past the rows -------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("type", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("rows", [1, 50, 96])
+def test_key_at_minus_infinity_with_odd_rows(type, rows):
+    """As test_visible_key_at_minus_infinity, with the last tile of 32 rows partly empty: what is not a row meets no key."""
+    from paper_2206_08720_amd import seq
+    n, D, at, d = 150, 64, 70, 3
+    q, k, v, do = (_rand((1, m, 1, D), 960 + i, type) for i, m in enumerate((rows, n, n, rows)))
+    q[..., d] = q[..., d].abs() + 0.5
+    keep = [j for j in range(n) if j != at]
+    ref = _oracle(q, k[:, keep], v[:, keep], type, do)
+    k[0, at, :, d] = -math.inf
+    o, lse = seq.attention(q.cuda(), k.cuda(), v.cuda(), return_lse=True)
+    _, dk, dv = seq.attention_backward(do.cuda(), q.cuda(), k.cuda(), v.cuda(), o, lse)
+    _close("dk", dk[:, keep], *ref["dk"])
+    _close("dv", dv[:, keep], *ref["dv"])
+    assert not dk[0, at].any() and not dv[0, at].any()
+
+
+def _one_head(type, q, k, v, do, scale, cap=0.0, bias=None):
+    """{name: (value, tolerance)} for q, do [rows, D], k, v [n, D] that all see each other, in 64 bits.  The tolerances are those of
+    _oracle, with a score's error taken from the magnitudes of its terms (the bias [rows, n] may have any sign), and with that of the cap's
+    derivative taken relatively: 4 e / (1 + e)^2 with e = exp(-2 |y|), y = scale x / cap, changes by 2 |dy| and by
+    6 roundings of y's factor, which are 12 |y| E < 120 E here.  Weights below 2^-126 may vanish."""
+    import torch
+    u, tiny, D, n = U[type], TINY[type], q.shape[1], k.shape[0]
+    inner = 2.0 ** -35 if type == "f16" else 0.0         # fp16's p and ds are formed times 2^10 and more
+    q, k, v, do = (t.double() for t in (q, k, v, do))
+    x = q @ k.T * scale
+    far = torch.zeros_like(x) if bias is None else bias.double()
+    s = (cap * torch.tanh(x / cap) if cap else x) - far
+    P, lse = torch.softmax(s, 1), torch.logsumexp(s, 1)
+    dx = (D + 8) * E * float((q.abs() @ k.abs().T * scale + far.abs()).max())
+    kappa = 2 * (dx + 8 * E * cap) + (n + 8) * E
+    fac, rel = (1 / torch.cosh(x / cap) ** 2, 2 * dx / cap + 120 * E) if cap else (torch.ones_like(x), 0.0)
+    o = P @ v
+    least = 2.0 ** -126
+    to = u * o.abs() + tiny + (u + kappa) * (P @ v.abs()) + least * v.abs().sum(0)
+    dP, delta = do @ v.T, (do * o).sum(1, keepdim=True)
+    dS = P * (dP - delta) * fac
+    edp = (D + 8) * E * (do.abs() @ v.abs().T) + (do.abs() * (to + (D + 8) * E * o.abs())).sum(1, keepdim=True)
+    eds = P * fac * ((u + kappa + 16 * E + rel) * (dP - delta).abs() + edp) + least * (dP - delta).abs() + inner
+    out = {"o": (o, to), "lse": (lse, kappa + 4 * E * lse.abs())}
+    for name, a, b, err, m in (("dq", dS, k, eds, n), ("dk", dS.T, q, eds.T, len(q))):
+        g = a @ b * scale
+        out[name] = (g, u * g.abs() + tiny + scale * (err @ b.abs() + m * E * (a.abs() @ b.abs())))
+    dv = P.T @ do
+    out["dv"] = (dv, u * dv.abs() + tiny + (u + kappa + len(q) * E) * (P.T @ do.abs()) + (inner + least) * do.abs().sum(0))
+    return out
+
+
+@pytest.mark.parametrize("type", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("rows", [33, 64])
+def test_slopes_that_favour_distance(type, rows):
+    """Negative slopes: far keys weigh most, and e^(-slope distance) alone is not finite in 32 bits."""
+    import torch
+    from paper_2206_08720_amd import seq
+    q, k, v, do = (_rand((m, 64), 970 + i, type) for i, m in enumerate((rows, 200, 200, rows)))
+    far = (200 - rows + torch.arange(rows)[:, None] - torch.arange(200)).abs()
+    ref = _one_head(type, q, k, v, do, 0.125, bias=-far)
+    args = [t.cuda()[None, :, None] for t in (q, k, v)]
+    slopes = torch.tensor([-1.0], device="cuda")
+    o, lse = seq.attention(*args, slopes=slopes, return_lse=True)
+    grads = seq.attention_backward(do.cuda()[None, :, None], *args, o, lse, slopes=slopes)
+    _close("lse", lse[0, 0], *ref["lse"])
+    for name, t in zip(("o", "dq", "dk", "dv"), (o,) + grads):
+        _close(name, t[0, :, 0], *ref[name])
