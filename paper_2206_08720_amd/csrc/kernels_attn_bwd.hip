@@ -30,9 +30,9 @@ __device__ __forceinline__ void weights(const AttnArgs& a, f32x16& s, f32x16& dp
     if (a.cap_in != 0.f) {
 #pragma unroll
       for (int v = 0; v < 16; ++v) {
-        s[v] = capped<T>(a, s[v]);
-        const float t = s[v] * a.cap_inv;
-        dp[v] *= fmaf(-t, t, 1.f);
+        float slope;
+        s[v] = capped<T>(a, s[v], slope);
+        dp[v] *= slope;
       }
     } else {
 #pragma unroll

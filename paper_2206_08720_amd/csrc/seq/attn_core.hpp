@@ -131,7 +131,7 @@ struct AttnArgs {
   int causal;
   float scale;                     // of the raw product
   float c;                         // scale * log2(e)
-  float cap_in, cap_out, cap_inv;  // softcap > 0: 2 log2(e) scale / cap, cap log2(e) and 1 / (cap log2(e)); else 0
+  float cap_in, cap_out;           // softcap > 0: 2 log2(e) scale / cap and cap log2(e); else 0
   FastDiv gdiv;
 };
 
@@ -480,6 +480,16 @@ template <class T>
 __device__ __forceinline__ float capped(const AttnArgs& a, float x) {
   if constexpr (sizeof(T) == 4) return a.cap_out * tanhf(x * a.cap_in * (0.5f / kLog2e));
   return fmaf(-2.f * a.cap_out, __builtin_amdgcn_rcpf(exp2_hw(x * a.cap_in) + 1.f), a.cap_out);
+}
+
+// The same with the cap's derivative, 1 - tanh^2 = 4 E / (1 + E)^2 with E = e^2y: formed from tanh it would lose its
+// bits where scores come near the cap (6 % in fp32 at y = 8).  E = inf: inf * 0, which is 0 here.
+template <class T>
+__device__ __forceinline__ float capped(const AttnArgs& a, float x, float& slope) {
+  const float e4 = exp2_hw(fmaf(x, a.cap_in, 2.f)), r = __builtin_amdgcn_rcpf(fmaf(e4, 0.25f, 1.f));
+  slope = fmaxf(e4 * r * r, 0.f);
+  if constexpr (sizeof(T) == 4) return capped<T>(a, x);
+  return fmaf(-2.f * a.cap_out, r, a.cap_out);
 }
 
 __device__ __forceinline__ void zero16(f32x16& a) {

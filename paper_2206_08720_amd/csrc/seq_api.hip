@@ -107,7 +107,6 @@ void set_desc(AttnArgs& a, const ntk_attention_desc* d) {
   a.c = d->scale * kLog2e;
   a.cap_in = d->softcap > 0.f ? 2.f * kLog2e * d->scale / d->softcap : 0.f;
   a.cap_out = d->softcap * kLog2e;
-  a.cap_inv = d->softcap > 0.f ? 1.f / a.cap_out : 0.f;
   a.gdiv = FastDiv((uint32_t)a.G);
   a.splits = 1;
 }

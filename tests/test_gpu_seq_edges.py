@@ -249,3 +249,25 @@ def test_slopes_that_favour_distance(type, rows):
     _close("lse", lse[0, 0], *ref["lse"])
     for name, t in zip(("o", "dq", "dk", "dv"), (o,) + grads):
         _close(name, t[0, :, 0], *ref[name])
+
+
+# ---- saturated scores -----------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("type", ["f32", "bf16"])
+@pytest.mark.parametrize("sign", [1.0, -1.0])
+def test_gradient_of_saturated_scores(type, sign):
+    """Every score is 6 to 9 times the cap before it is capped (16 bits: 7.5 to 9): what is left of the gradient is the cap's derivative,
+    far below 1."""
+    import torch
+    from paper_2206_08720_amd import seq
+    n, rows, cap, scale = 70, 40, 2.0, 0.125
+    q, k = torch.zeros(rows, 64), _rand((n, 64), 980)
+    q[:, 0] = 16.0 * sign
+    k[:, 0] = torch.linspace(6.0 if type == "f32" else 7.5, 9.0, n)
+    q, k, v, do = (t.to(_types()[type]) for t in (q, k, _rand((n, 64), 981), _rand((rows, 64), 982)))
+    args = [t.cuda()[None, :, None] for t in (q, k, v)]
+    o, lse = seq.attention(*args, softcap=cap, scale=scale, return_lse=True)
+    grads = seq.attention_backward(do.cuda()[None, :, None], *args, o, lse, softcap=cap, scale=scale)
+    ref = _one_head(type, q, k, v, do, scale, cap)
+    for name, t in zip(("o", "dq", "dk", "dv"), (o,) + grads):
+        _close(name, t[0, :, 0], *ref[name])
