@@ -85,6 +85,34 @@ __device__ __forceinline__ float row_all(float x, float* s) {
   return x;
 }
 
+template <int CH>
+__device__ __forceinline__ float squares(const float (&h)[CH][kE]) {
+  float ss = 0.f;
+#pragma unroll
+  for (int c = 0; c < CH; ++c)
+#pragma unroll
+    for (int i = 0; i < kE; ++i) ss = fmaf(h[c][i], h[c][i], ss);
+  return ss;
+}
+
+// A row's sum of squares leaves fp32's range where h passes 2^63 or, with an eps that does not cover it, stays below 2^-40.
+// Such a row is multiplied by the power of two that this returns (1 for the others), and its sum formed again:
+// r of the row as it was is that power times (ss / n + eps power^2)^(-1/2).
+__device__ __forceinline__ float row_power(float ss, float eps) {
+  if (!(ss <= 0x1p126f)) return 0x1p-80f;
+  return ss < 0x1p-80f && eps < 0x1p-100f ? 0x1p100f : 1.f;
+}
+template <int CH>
+__device__ __forceinline__ void scale_row(float (&h)[CH][kE], float f) {
+#pragma unroll
+  for (int c = 0; c < CH; ++c)
+#pragma unroll
+    for (int i = 0; i < kE; ++i) h[c][i] *= f;
+}
+__device__ __forceinline__ float inverse_norm(float ss, int n, float eps, float power) {
+  return 1.f / sqrtf(ss / (float)n + eps * power * power);
+}
+
 template <class T, class W, int TPR, int CH, bool VEC>
 __global__ void __launch_bounds__(TPR < kBlock ? kBlock : TPR) k_rms_norm(const NormArgs a) {
   constexpr int RPB = TPR < kBlock ? kBlock / TPR : 1;
@@ -109,17 +137,17 @@ __global__ void __launch_bounds__(TPR < kBlock ? kBlock : TPR) k_rms_norm(const 
   }
 #pragma unroll
   for (int c = 0; c < CH; ++c) load8<W, VEC, TPR>((const W*)a.weight, c, t, n, w[c]);
-  float ss = 0.f;
-#pragma unroll
-  for (int c = 0; c < CH; ++c)
-#pragma unroll
-    for (int i = 0; i < kE; ++i) ss = fmaf(h[c][i], h[c][i], ss);
-  ss = row_all<TPR, false>(ss, s);
-  const float r = 1.f / sqrtf(ss / (float)n + a.eps);
+  float ss = row_all<TPR, false>(squares<CH>(h), s);
   if (a.h) {
 #pragma unroll
     for (int c = 0; c < CH; ++c) store8<T, VEC, TPR>((T*)a.h + row * n, c, t, n, h[c]);
   }
+  const float power = row_power(ss, a.eps);
+  if (power != 1.f) {
+    scale_row<CH>(h, power);
+    ss = row_all<TPR, false>(squares<CH>(h), s);
+  }
+  const float r = inverse_norm(ss, n, a.eps, power);
 #pragma unroll
   for (int c = 0; c < CH; ++c)
 #pragma unroll
@@ -187,18 +215,27 @@ __global__ void __launch_bounds__(TPR < kBlock ? kBlock : TPR) k_rms_norm_bwd(co
       load8<T, VEC, TPR>((const T*)a.h + row * a.h_stride, c, t, n, h[c]);
       load8<T, VEC, TPR>((const T*)a.dy + row * a.dy_stride, c, t, n, g[c]);
     }
-    float ss = 0.f, sg = 0.f;
+    auto sums = [&](float& ss, float& sg) {
+      ss = sg = 0.f;
 #pragma unroll
-    for (int c = 0; c < CH; ++c)
+      for (int c = 0; c < CH; ++c)
 #pragma unroll
-      for (int i = 0; i < kE; ++i) {
-        ss = fmaf(h[c][i], h[c][i], ss);
-        sg = fmaf(g[c][i] * w[c][i], h[c][i], sg);
-      }
-    ss = row_all<TPR, false>(ss, s);
-    sg = row_all<TPR, false>(sg, s);
-    const float r = 1.f / sqrtf(ss / (float)n + a.eps);
-    const float f = r * r * (sg / (float)n);
+        for (int i = 0; i < kE; ++i) {
+          ss = fmaf(h[c][i], h[c][i], ss);
+          sg = fmaf(g[c][i] * w[c][i], h[c][i], sg);
+        }
+      ss = row_all<TPR, false>(ss, s);
+      sg = row_all<TPR, false>(sg, s);
+    };
+    float ss, sg;
+    sums(ss, sg);
+    const float power = row_power(ss, a.eps);
+    if (power != 1.f) {
+      scale_row<CH>(h, power);
+      sums(ss, sg);
+    }
+    const float r = inverse_norm(ss, n, a.eps, power);
+    const float f = r * r * (sg / (float)n), rp = r * power;
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
       float e[kE];
@@ -211,7 +248,7 @@ __global__ void __launch_bounds__(TPR < kBlock ? kBlock : TPR) k_rms_norm_bwd(co
 #pragma unroll
       for (int i = 0; i < kE; ++i) {
         dw[c][i] = fmaf(g[c][i], h[c][i] * r, dw[c][i]);
-        e[i] += r * (g[c][i] * w[c][i] - h[c][i] * f);
+        e[i] += rp * (g[c][i] * w[c][i] - h[c][i] * f);
       }
       store8<T, VEC, TPR>((T*)a.dx + row * n, c, t, n, e);
     }

@@ -271,3 +271,30 @@ def test_gradient_of_saturated_scores(type, sign):
     ref = _one_head(type, q, k, v, do, scale, cap)
     for name, t in zip(("o", "dq", "dk", "dv"), (o,) + grads):
         _close(name, t[0, :, 0], *ref[name])
+
+
+# ---- norms of rows whose squares leave fp32's range -----------------------------------------------------------------
+
+@pytest.mark.parametrize("type", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,n", [(5, 96), (4, 785), (3, 2048), (2, 12289), (2, 32768)])
+@pytest.mark.parametrize("size,eps", [(1e25, 1e-6), (5e37, 1e-6), (1e-30, 0.0), (3e-25, 1e-44)])
+def test_rms_norm_of_any_size(type, rows, n, size, eps):
+    """h of 1e25 has squares past fp32's largest, h of 1e-30 below its smallest; ordinary rows stand beside them.  The 8-bit
+    form's y goes through the same numbers.  Tiny numbers: fp32's smallest step, 2^-149, in what is stored."""
+    import torch
+    from paper_2206_08720_amd import seq
+    x, res, dy, dh = (_rand((rows, n), 990 + i, type) for i in range(4))
+    x[0], res[0] = x[0].float().clamp(-3, 3) * size, res[0].float().clamp(-3, 3) * size
+    dy, dh = dy * (1e3 if size > 1 else 1e-3), dh * (1 / size)
+    w = (1 + 0.1 * _rand((n,), 995)).to(_types()[type])
+    y, h = seq.rms_norm(x.cuda(), w.cuda(), residual=res.cuda(), eps=eps)
+    eps = float(torch.tensor(eps, dtype=torch.float32))
+    ref = _norm_reference(x, res, w, eps, type, dy, dh, h.cpu())
+    _close("y", y, *ref["y"])
+    dx, dw = seq.rms_norm_backward(dy.cuda(), h, w.cuda(), dh=dh.cuda(), eps=eps)
+    _close("dx", dx, ref["dx"][0], ref["dx"][1] + 2.0 ** -133)
+    val, tol = ref["dw"]
+    _close("dw", dw, val, tol)
+    _, scale, _ = seq.rms_norm_e4m3(x.cuda(), w.cuda(), residual=res.cuda(), eps=eps)
+    most = ref["y"][0].abs().max(1).values
+    _close("scale", scale, most / 448, 2 * (n + 16) * E * most / 448)
