@@ -333,9 +333,12 @@ hipError_t by_type(hipStream_t s, int dtype, int wtype, const NormArgs* f, const
 
 }  // namespace
 
+int norm_threads(int width) { return std::max(shape_of(width).tpr, kBlock); }
+int norm_rows_per_block(int width) { return norm_threads(width) / shape_of(width).tpr; }
+
 int norm_bwd_parts(long long rows, int width) {
   const Shape h = shape_of(width);
-  const int rpb = h.tpr < kBlock ? kBlock / h.tpr : 1;
+  const int rpb = norm_rows_per_block(width);
   const long long groups = (rows + rpb - 1) / rpb;
   const long long most = h.tpr == 1024 ? 256 : 1024;    // workgroups: four (one of 1024 threads) a compute unit
   return (int)(groups < most ? groups : most) * rpb;

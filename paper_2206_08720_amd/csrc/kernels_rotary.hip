@@ -134,8 +134,7 @@ __global__ void __launch_bounds__(256) k_rotary_table(const RotaryTableArgs a) {
   a.table[2 * id + 1] = (float)(sn * mag);
 }
 
-template <class T>
-hipError_t run(hipStream_t s, const RotaryArgs& a, bool vec) {
+RotaryPlan plan_of(const RotaryArgs& a) {
   RotaryPlan p;
   p.turn = (a.rot / 2 + kPairs - 1) / kPairs;
   p.items = p.turn + (a.dim - a.rot + 2 * kPairs - 1) / (2 * kPairs);
@@ -147,7 +146,16 @@ hipError_t run(hipStream_t s, const RotaryArgs& a, bool vec) {
   long long rpb = std::max(1u, 1024u / p.per_row.d);
   while (rpb > 1 && (rows + rpb - 1) / rpb < 512) rpb = (rpb + 1) / 2;
   p.rows_per_block = (int)rpb;
-  const dim3 grid((unsigned)((rows + rpb - 1) / rpb));
+  return p;
+}
+long long blocks_of(const RotaryArgs& a, const RotaryPlan& p) {
+  return ((long long)a.batch * a.length + p.rows_per_block - 1) / p.rows_per_block;
+}
+
+template <class T>
+hipError_t run(hipStream_t s, const RotaryArgs& a, bool vec) {
+  const RotaryPlan p = plan_of(a);
+  const dim3 grid((unsigned)blocks_of(a, p));
   if (vec)
     k_rotary<T, true><<<grid, dim3(256), 0, s>>>(a, p);
   else
@@ -156,6 +164,8 @@ hipError_t run(hipStream_t s, const RotaryArgs& a, bool vec) {
 }
 
 }  // namespace
+
+long long rotary_blocks(const RotaryArgs& a) { return blocks_of(a, plan_of(a)); }
 
 hipError_t launch_rotary(hipStream_t s, int dtype, const RotaryArgs& a, bool vec) {
   if (dtype == 1) return run<__bf16>(s, a, vec);

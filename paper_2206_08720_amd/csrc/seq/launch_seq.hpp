@@ -28,6 +28,8 @@ struct NormBwdArgs {
   int width;
   float eps;
 };
+int norm_threads(int width);         // a workgroup's, and the rows it takes
+int norm_rows_per_block(int width);
 int norm_bwd_parts(long long rows, int width);
 hipError_t launch_rms_norm(hipStream_t s, int dtype, int wtype, const NormArgs& a, bool vec);
 hipError_t launch_rms_norm_bwd(hipStream_t s, int dtype, int wtype, const NormBwdArgs& a, bool vec);
@@ -44,6 +46,7 @@ struct RotaryArgs {
   int batch, length, dim, rot, interleaved;
   float sign;                          // 1, or -1 for the inverse
 };
+long long rotary_blocks(const RotaryArgs& a);   // workgroups, of 256 threads
 hipError_t launch_rotary(hipStream_t s, int dtype, const RotaryArgs& a, bool vec);
 
 // table[p][j] = mag (cos, sin)(p f_j); see ntk_rotary_table.

@@ -28,7 +28,7 @@ bool type_ok(int dtype) { return dtype == NTK_F32 || dtype == NTK_BF16 || dtype 
 bool whole16(const void* p) { return ((uintptr_t)p & 15) == 0; }
 bool aligned(const void* p, int e) { return ((uintptr_t)p & (uintptr_t)(e - 1)) == 0; }
 // a grid of `blocks` workgroups of `threads` fits a launch
-bool grid_ok(long long blocks, int threads) { return blocks * threads < (1LL << 32) && blocks < (1LL << 31); }
+bool grid_ok(long long blocks, int threads) { return blocks < (1LL << 31) && blocks * threads < (1LL << 32); }
 
 int norm_args(int dtype, int wtype, long long rows, int width, float eps) {
   if (!type_ok(dtype)) return bad(NTK_E_ARG, "rms_norm: dtype");
@@ -36,7 +36,6 @@ int norm_args(int dtype, int wtype, long long rows, int width, float eps) {
   if (rows < 0 || width < 1) return bad(NTK_E_ARG, "rms_norm: rows < 0 or width < 1");
   if (!(eps >= 0.f)) return bad(NTK_E_ARG, "rms_norm: eps < 0");
   if (width > 32768) return bad(NTK_E_UNSUPPORTED, "rms_norm: width over 32768");
-  if (!grid_ok(rows, width > 8192 ? 1024 : 256)) return bad(NTK_E_UNSUPPORTED, "rms_norm: too many rows for one launch");
   return NTK_OK;
 }
 
@@ -48,8 +47,8 @@ bool view_vec(const ntk_view* v, int e) {
   return whole16(v->data) && v->stride_batch % k == 0 && v->stride_position % k == 0 && v->stride_head % k == 0;
 }
 
-// Checks a descriptor; `plan` as the forward pass runs it.
-int attn_args(const ntk_attention_desc* d, AttnPlan* plan) {
+// Checks a descriptor for the pass asked for; `plan` as the forward pass runs it.
+int attn_args(const ntk_attention_desc* d, AttnPlan* plan, bool backward) {
   if (!d) return bad(NTK_E_ARG, "attention: the descriptor is NULL");
   if (!type_ok(d->dtype)) return bad(NTK_E_ARG, "attention: dtype");
   if (d->batch < 0 || d->q_len < 0 || d->k_len < 0) return bad(NTK_E_ARG, "attention: batch, q_len or k_len < 0");
@@ -66,11 +65,18 @@ int attn_args(const ntk_attention_desc* d, AttnPlan* plan) {
     return bad(NTK_E_UNSUPPORTED, "attention: q_len * group reaches 2^29 or k_len 2^31");
   if (R > 0 && bh > 0) {
     *plan = attn_plan_fwd(d->dtype, d->batch, d->kv_heads, (int)R, d->k_len, d->head_dim);
-    const long long tiles = plan->tokens ? 1 : plan->tiles;
-    const AttnBwdPlan back = attn_plan_bwd(d->dtype, d->batch, d->kv_heads, (int)R, d->k_len, d->head_dim, d->causal != 0);
-    if (!grid_ok(bh * tiles * plan->splits, 256) || !grid_ok(bh * back.dq_tiles * back.dq_splits, 256) ||
-        !grid_ok(bh * back.dkv_tiles * back.dkv_splits, 256) || !grid_ok((bh * R + 3) / 4, 256) || !grid_ok((bh * d->k_len + 3) / 4, 256) ||
-        (plan->splits > 1 && !grid_ok(bh * R, 128)))
+    const int dp = d->head_dim <= 64 ? 64 : 128;
+    const long long rows = bh * R, keys = bh * d->k_len, spr = 256 / (dp / 4);   // rows a workgroup of the ranges' sums
+    bool fits;
+    if (backward) {
+      const AttnBwdPlan back = attn_plan_bwd(d->dtype, d->batch, d->kv_heads, (int)R, d->k_len, d->head_dim, d->causal != 0);
+      fits = grid_ok(bh * back.dq_tiles * back.dq_splits, 256) && grid_ok(bh * back.dkv_tiles * back.dkv_splits, 256) &&
+             grid_ok(rows / 16 + 1, 256) && (back.dq_splits == 1 || grid_ok(rows / spr + 1, 256)) &&
+             (back.dkv_splits == 1 || grid_ok(keys / spr + 1, 256));
+    } else {
+      fits = grid_ok(bh * (plan->tokens ? 1 : plan->tiles) * plan->splits, 256) && (plan->splits == 1 || grid_ok(rows, dp));
+    }
+    if (!fits)
       return bad(NTK_E_UNSUPPORTED, "attention: too many rows for one launch");
   } else {
     *plan = AttnPlan{};
@@ -125,6 +131,8 @@ extern "C" int ntk_rms_norm(int dtype, int wtype, long long rows, int width, con
                             float* scale, void* hip_stream) {
   if (int rc = norm_args(dtype, wtype, rows, width, eps)) return rc;
   if (rows == 0) return NTK_OK;
+  const int rpb = norm_rows_per_block(width);
+  if (!grid_ok(rows / rpb + 1, norm_threads(width))) return bad(NTK_E_UNSUPPORTED, "rms_norm: too many rows for one launch");
   const int e = elem(dtype), we = elem(wtype);
   if (!x || !weight || !y) return bad(NTK_E_ARG, "rms_norm: x, weight or y is NULL");
   if (x_stride < width || (residual && residual_stride < width)) return bad(NTK_E_ARG, "rms_norm: a row stride is below width");
@@ -203,7 +211,7 @@ extern "C" int ntk_rotary(int dtype, int batch, int length, int q_heads, int k_h
   if ((q_heads && (!view_ok(q, e) || !view_ok(q_out, e))) || (k_heads && (!view_ok(k, e) || !view_ok(k_out, e))))
     return bad(NTK_E_ARG, "rotary: a view is missing, unaligned or has a negative stride");
   const long long rows = (long long)batch * length, items = (long long)(q_heads + k_heads) * (dim / 16 + 2);
-  if (rows >= (1LL << 31) || items >= (1LL << 20) || !grid_ok(rows, 256)) return bad(NTK_E_UNSUPPORTED, "rotary: too large for one launch");
+  if (rows >= (1LL << 31) || items >= (1LL << 20)) return bad(NTK_E_UNSUPPORTED, "rotary: too large for one launch");
   RotaryArgs a{};
   bool vec = rot % 16 == 0 && dim % 8 == 0 && whole16(table);
   const ntk_view* in[2] = {q, k};
@@ -232,13 +240,14 @@ extern "C" int ntk_rotary(int dtype, int batch, int length, int q_heads, int k_h
   a.rot = rot;
   a.interleaved = interleaved != 0;
   a.sign = inverse ? -1.f : 1.f;
+  if (!grid_ok(rotary_blocks(a), 256)) return bad(NTK_E_UNSUPPORTED, "rotary: too large for one launch");
   const hipError_t err = launch_rotary((hipStream_t)hip_stream, dtype, a, vec);
   return err == hipSuccess ? NTK_OK : hip_bad(err);
 }
 
 extern "C" long long ntk_attention_workspace(const ntk_attention_desc* desc, int backward) {
   AttnPlan plan;
-  if (int rc = attn_args(desc, &plan)) return rc;
+  if (int rc = attn_args(desc, &plan, backward != 0)) return rc;
   if (!backward) return (plan.part_floats + plan.flag_ints) * 4;
   const AttnBwdPlan back = bwd_plan(desc);
   return (back.part_floats + back.flag_ints + 2 * (long long)desc->batch * desc->heads * desc->q_len) * 4;
@@ -247,7 +256,7 @@ extern "C" long long ntk_attention_workspace(const ntk_attention_desc* desc, int
 extern "C" int ntk_attention(const ntk_attention_desc* desc, const ntk_view* q, const ntk_view* k, const ntk_view* v,
                              const ntk_view* o, float* lse, void* workspace, long long workspace_bytes, void* hip_stream) {
   AttnPlan plan;
-  if (int rc = attn_args(desc, &plan)) return rc;
+  if (int rc = attn_args(desc, &plan, false)) return rc;
   if (desc->batch == 0 || desc->q_len == 0) return NTK_OK;
   const int e = elem(desc->dtype), G = desc->heads / desc->kv_heads;
   if (!view_ok(q, e) || !view_ok(o, e) || (desc->k_len && (!view_ok(k, e) || !view_ok(v, e))))
@@ -280,7 +289,7 @@ extern "C" int ntk_attention_bwd(const ntk_attention_desc* desc, const ntk_view*
                                  const ntk_view* v, const ntk_view* o, const float* lse, const ntk_view* dq, const ntk_view* dk,
                                  const ntk_view* dv, void* workspace, long long workspace_bytes, void* hip_stream) {
   AttnPlan plan;
-  if (int rc = attn_args(desc, &plan)) return rc;
+  if (int rc = attn_args(desc, &plan, true)) return rc;
   if (desc->batch == 0) return NTK_OK;
   const int e = elem(desc->dtype), G = desc->heads / desc->kv_heads;
   const ntk_view* views[8] = {dout, q, o, dq, k, v, dk, dv};   // four of the queries' axis, four of the keys'

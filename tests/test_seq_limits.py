@@ -1,0 +1,38 @@
+"""The sequence operators' limits (include/ntk_seq.h), on the host: what a launch holds is refused by that launch alone."""
+import ctypes
+import os
+
+import pytest
+
+
+@pytest.fixture(scope="module")
+def lib():
+    from paper_2206_08720_amd import _lib
+    if not os.path.exists(_lib.LIB_PATH):
+        from paper_2206_08720_amd.build import build
+        build()
+    return _lib.load()
+
+
+def _workspace(lib, backward, **kw):
+    from paper_2206_08720_amd import _lib
+    d = dict(dtype=_lib.NTK_BF16, batch=2, q_len=8, k_len=64, heads=4, kv_heads=2, head_dim=64, causal=1, scale=0.125, softcap=0.0)
+    d.update(kw)
+    return lib.ntk_attention_workspace(ctypes.byref(_lib.ntk_attention_desc(**d)), backward)
+
+
+def test_tokens_over_large_caches(lib):
+    """512 sequences of 8 heads and 32768 places: 2^27 keys, in one launch of 4096 workgroups."""
+    assert _workspace(lib, 0, batch=512, q_len=1, k_len=32768, heads=32, kv_heads=8, head_dim=128) >= 0
+
+
+def test_rows_of_large_training_batches(lib):
+    """2^27 rows of 16 a workgroup, 2^20 tiles."""
+    sizes = dict(batch=64, q_len=65536, k_len=65536, heads=32, kv_heads=32, head_dim=64)
+    assert _workspace(lib, 0, **sizes) >= 0 and _workspace(lib, 1, **sizes) >= 0
+
+
+def test_what_one_launch_does_not_hold(lib):
+    from paper_2206_08720_amd import _lib
+    for backward in (0, 1):
+        assert _workspace(lib, backward, batch=1 << 14, q_len=1 << 18, k_len=1 << 18, heads=8, kv_heads=8) == _lib.NTK_E_UNSUPPORTED
