@@ -206,12 +206,13 @@ extern "C" int ntk_rotary(int dtype, int batch, int length, int q_heads, int k_h
   if (!k) k_heads = 0;
   if (max_pos < 1 || !table || !aligned(table, 4) || !aligned(positions, 4)) return bad(NTK_E_ARG, "rotary: table or positions");
   if (!positions && (first_position < 0 || first_position > 2147483647 - length)) return bad(NTK_E_ARG, "rotary: first_position");
-  if (batch == 0 || length == 0 || q_heads + k_heads == 0) return NTK_OK;
+  const long long heads = (long long)q_heads + k_heads;
+  if (batch == 0 || length == 0 || heads == 0) return NTK_OK;
   const int e = elem(dtype);
   if ((q_heads && (!view_ok(q, e) || !view_ok(q_out, e))) || (k_heads && (!view_ok(k, e) || !view_ok(k_out, e))))
     return bad(NTK_E_ARG, "rotary: a view is missing, unaligned or has a negative stride");
-  const long long rows = (long long)batch * length, items = (long long)(q_heads + k_heads) * (dim / 16 + 2);
-  if (rows >= (1LL << 31) || items >= (1LL << 20)) return bad(NTK_E_UNSUPPORTED, "rotary: too large for one launch");
+  const long long rows = (long long)batch * length, items = heads * (dim / 16 + 2);
+  if (rows >= (1LL << 31) || heads >= (1LL << 20) || items >= (1LL << 20)) return bad(NTK_E_UNSUPPORTED, "rotary: too large for one launch");
   RotaryArgs a{};
   bool vec = rot % 16 == 0 && dim % 8 == 0 && whole16(table);
   const ntk_view* in[2] = {q, k};

@@ -36,3 +36,11 @@ def test_what_one_launch_does_not_hold(lib):
     from paper_2206_08720_amd import _lib
     for backward in (0, 1):
         assert _workspace(lib, backward, batch=1 << 14, q_len=1 << 18, k_len=1 << 18, heads=8, kv_heads=8) == _lib.NTK_E_UNSUPPORTED
+
+
+def test_rotary_heads_past_32_bits(lib):
+    """2^30 heads of q and as many of k: their sum is counted in 64 bits."""
+    from paper_2206_08720_amd import _lib
+    v = ctypes.byref(_lib.ntk_view(4096, 0, 0, 0))
+    for q, k in ((1 << 30, 1 << 30), (2147483647, 2147483647), (1 << 30, 0), (1 << 20, 1)):
+        assert lib.ntk_rotary(1, 1, 1, q, k, 64, 64, 0, 0, v, v, 4096, 8, None, 0, v, v, None) == _lib.NTK_E_UNSUPPORTED
