@@ -35,6 +35,12 @@ def _check(t, name, dtype=None, ndim=None, device=None, shape=None):
         raise ValueError(f"{name} must be contiguous in its last dimension")
 
 
+def _sizes(*sizes):
+    """The library's sizes are 32-bit integers, and ctypes would cut larger ones."""
+    if max(sizes) > 0x7fffffff:
+        raise _lib.NTKError(_lib.NTK_E_UNSUPPORTED, f"a size of {max(sizes)} does not fit 32 bits")
+
+
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda i: torch.cuda.current_stream(i).cuda_stream)
 
 
@@ -112,6 +118,7 @@ def _rms_norm(x, weight, residual, eps, stream, e4m3):
     if x.dim() < 1:
         raise ValueError("x needs a last dimension")
     width = x.shape[-1]
+    _sizes(width)
     if not isinstance(weight, torch.Tensor) or weight.dtype not in (torch.float32, x.dtype):
         raise TypeError(f"weight must be float32 or {x.dtype}")
     _check(weight, "weight", weight.dtype, device=x.device, shape=x.shape[-1:])
@@ -148,6 +155,7 @@ def rms_norm_backward(dy, h, weight, dh=None, eps=1e-6, stream=None):
     lib = _lib.load()
     _check(h, "h")
     width = h.shape[-1]
+    _sizes(width)
     _check(dy, "dy", h.dtype, device=h.device, shape=h.shape)
     if dh is not None:
         _check(dh, "dh", h.dtype, device=h.device, shape=h.shape)
@@ -187,6 +195,7 @@ def rotary_table(max_pos, rot, base=10000.0, scaling=None, factor=1.0, original=
     dev = torch.device("cuda", torch.cuda.current_device() if device is None else torch.device(device).index or 0)
     if max_pos < 1 or rot < 2 or rot % 2:
         raise ValueError("rotary_table: max_pos < 1, or rot odd or < 2")
+    _sizes(max_pos, rot)
     s = _lib.ntk_rotary_scaling(kinds[scaling], float(factor), float(original or 1), float(low), float(high))
     with torch.cuda.device(dev), torch.cuda.stream(stream) if stream is not None else _NO_CONTEXT:
         table = torch.empty((max_pos, rot // 2, 2), dtype=torch.float32, device=dev)
@@ -212,6 +221,9 @@ def rotary(q, table, positions=0, k=None, interleaved=False, inverse=False, inpl
         _check(positions, "positions", torch.int32, device=q.device, shape=(b, n))
         if not positions.is_contiguous():
             raise ValueError("positions must be contiguous")
+    elif not -1 < positions <= 0x7fffffff:
+        raise _lib.NTKError(_lib.NTK_E_ARG, f"rotary: first position {positions}")
+    _sizes(b, n, heads, 0 if k is None else k.shape[2], dim, table.shape[0], 2 * table.shape[1])
     with _Call(q, stream, (q, table, k, positions if per_token else None)) as call:
         qo = q if inplace else _like(q)
         ko = k if inplace or k is None else _like(k)
@@ -233,6 +245,7 @@ def _attention_desc(q, k, v, causal, softcap, scale, slopes, k_lens, prefix, doc
     if k.shape[0] != b or k.shape[3] != dim:
         raise ValueError(f"k has shape {tuple(k.shape)}, expected ({b}, k_len, kv_heads, {dim})")
     _check(v, "v", q.dtype, device=q.device, shape=k.shape)
+    _sizes(b, sq, sk, heads, kv_heads, dim)
     for name, t, dtype, shape in (("k_lens", k_lens, torch.int32, (b,)), ("prefix", prefix, torch.int32, (b,)),
                                   ("docs", docs, torch.int32, (b, sk)), ("slopes", slopes, torch.float32, (heads,))):
         if t is not None:

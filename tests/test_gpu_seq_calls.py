@@ -30,3 +30,24 @@ def test_rows_past_2_to_the_24():
     ref = _oracle(q, kc, vc, "bf16")["o"]
     _close("o", o[:4], *ref)
     _close("o", o[-4:], *ref)
+
+
+def test_sizes_past_32_bits_are_refused():
+    """The library's sizes are 32-bit: what does not fit is refused, not cut."""
+    import torch
+    from paper_2206_08720_amd import _lib, seq
+    q = torch.zeros(1, 1, 1, 64, device="cuda")
+    table = seq.rotary_table(8, 64)
+    long = torch.zeros(1, 1, 1, 2, device="cuda").expand(1, 2 ** 32 + 1, 1, 2)
+    wide = torch.empty(2 ** 32 + 64, dtype=torch.bfloat16, device="cuda")
+    for call in (lambda: seq.attention(q, q.expand(1, 2 ** 32 + 8, 1, 64), q.expand(1, 2 ** 32 + 8, 1, 64)),
+                 lambda: seq.attention(q, q.expand(1, 2 ** 31 + 8, 1, 64), q.expand(1, 2 ** 31 + 8, 1, 64)),
+                 lambda: seq.rotary(long, table[:, :1].contiguous()),
+                 lambda: seq.rotary(q, table, 2 ** 32),
+                 lambda: seq.rotary(q, table, -2 ** 32),
+                 lambda: seq.rotary_table(2 ** 32 + 8, 2),
+                 lambda: seq.rms_norm(wide[None], wide),
+                 lambda: seq.rms_norm_backward(wide[None], wide[None], wide)):
+        with pytest.raises(_lib.NTKError) as e:
+            call()
+        assert e.value.code in (_lib.NTK_E_ARG, _lib.NTK_E_UNSUPPORTED)
