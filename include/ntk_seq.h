@@ -58,7 +58,8 @@ int ntk_rms_norm_bwd(int dtype, int wtype, long long rows, int width, const void
                      void* dweight, void* workspace, long long workspace_bytes, void* hip_stream);
 
 /* An array [batch, position, head, dim] in device memory: dim contiguous, the other strides in elements
- * (>= 0). */
+ * (>= 0).  Inputs may be broadcast (a stride of 0); an output whose stride is below the head size, or that starts where another
+ * array of its call does (but for rotary in place), is refused.  Other overlaps are the caller's to avoid. */
 typedef struct ntk_view {
     void* data;
     long long stride_batch, stride_position, stride_head;

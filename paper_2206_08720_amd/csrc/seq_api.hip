@@ -46,6 +46,11 @@ bool view_vec(const ntk_view* v, int e) {
   const long long k = 16 / e;
   return whole16(v->data) && v->stride_batch % k == 0 && v->stride_position % k == 0 && v->stride_head % k == 0;
 }
+// An output's elements share no memory: a stride below the head size would lay rows over each other.
+bool apart(const ntk_view* v, int batch, int positions, int heads, int dim) {
+  return (batch == 1 || v->stride_batch >= dim) && (positions == 1 || v->stride_position >= dim) && (heads == 1 || v->stride_head >= dim);
+}
+bool same_place(const ntk_view* a, const ntk_view* b) { return a->data == b->data; }
 
 // Checks a descriptor for the pass asked for; `plan` as the forward pass runs it.
 int attn_args(const ntk_attention_desc* d, AttnPlan* plan, bool backward) {
@@ -221,6 +226,8 @@ extern "C" int ntk_rotary(int dtype, int batch, int length, int q_heads, int k_h
   for (int i = 0; i < 2; ++i) {
     a.heads[i] = n[i];
     if (!n[i]) continue;
+    if (!apart(out[i], batch, length, n[i], dim) || (n[1 - i] && (same_place(out[i], out[1 - i]) || same_place(out[i], in[1 - i]))))
+      return bad(NTK_E_ARG, "rotary: an output overlaps itself or another array");
     a.x[i] = in[i]->data;
     a.xb[i] = in[i]->stride_batch;
     a.xs[i] = in[i]->stride_position;
@@ -267,6 +274,9 @@ extern "C" int ntk_attention(const ntk_attention_desc* desc, const ntk_view* q, 
   const long long need = (plan.part_floats + plan.flag_ints) * 4;
   if (need && (!workspace || !whole16(workspace) || workspace_bytes < need))
     return bad(NTK_E_ARG, "attention: the workspace is missing, unaligned or too small");
+  if (!apart(o, desc->batch, desc->q_len, desc->heads, desc->head_dim) || same_place(o, q) ||
+      (desc->k_len && (same_place(o, k) || same_place(o, v))))
+    return bad(NTK_E_ARG, "attention: o overlaps itself, q, k or v");
   AttnArgs a{};
   set_desc(a, desc);
   set_view(a.q, q);
@@ -305,6 +315,14 @@ extern "C" int ntk_attention_bwd(const ntk_attention_desc* desc, const ntk_view*
   const long long need = ntk_attention_workspace(desc, 1);
   if (need && (!workspace || !whole16(workspace) || workspace_bytes < need))
     return bad(NTK_E_ARG, "attention_bwd: the workspace is missing, unaligned or too small");
+  for (const int out : {3, 6, 7}) {                             // dq, dk, dv
+    const bool keys = out > 3;
+    if ((keys ? desc->k_len : desc->q_len) == 0) continue;
+    bool clear = apart(views[out], desc->batch, keys ? desc->k_len : desc->q_len, keys ? desc->kv_heads : desc->heads, desc->head_dim);
+    for (int i = 0; i < 8; ++i)
+      clear = clear && (i == out || (i < 4 ? desc->q_len : desc->k_len) == 0 || !same_place(views[out], views[i]));
+    if (!clear) return bad(NTK_E_ARG, "attention_bwd: dq, dk or dv overlaps itself or another array");
+  }
   AttnArgs a{};
   set_desc(a, desc);
   if (desc->q_len) {

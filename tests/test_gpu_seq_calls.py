@@ -51,3 +51,27 @@ def test_sizes_past_32_bits_are_refused():
         with pytest.raises(_lib.NTKError) as e:
             call()
         assert e.value.code in (_lib.NTK_E_ARG, _lib.NTK_E_UNSUPPORTED)
+
+
+def test_outputs_that_overlap_are_refused():
+    """An output whose elements share memory, or that starts where an operand does, would hold what came last."""
+    import torch
+    from paper_2206_08720_amd import _lib, seq
+    q, k = torch.ones(2, 40, 4, 64, device="cuda"), torch.ones(2, 50, 2, 64, device="cuda")
+    table = seq.rotary_table(64, 64)
+    one = torch.ones(1, 1, 1, 64, device="cuda")
+    for call in (lambda: seq.attention(q, k, k, out=one.expand(2, 40, 4, 64)),
+                 lambda: seq.attention(q, k, k, out=torch.ones(2, 1, 4, 64, device="cuda").expand(2, 40, 4, 64)),
+                 lambda: seq.attention(q, k, k, out=q),
+                 lambda: seq.attention(k, k, q[:, :, :2][:, :40].new_ones(2, 50, 2, 64), out=k),
+                 lambda: seq.rotary(q[:1].expand(2, 40, 4, 64), table, inplace=True),
+                 lambda: seq.rotary(q, table, k=k[:, :1].expand(2, 40, 2, 64), inplace=True)):
+        with pytest.raises(_lib.NTKError) as e:
+            call()
+        assert e.value.code == _lib.NTK_E_ARG
+    # one position, head or batch entry may have any stride, and inputs may be broadcast
+    out = torch.zeros(1, 1, 1, 64, device="cuda").expand(1, 1, 1, 64)
+    seq.attention(one, one.expand(1, 9, 1, 64), one.expand(1, 9, 1, 64), out=out)
+    assert torch.equal(out, one)
+    y = seq.rotary(one.expand(2, 3, 4, 64), table)
+    assert torch.equal(y[1, :, 3], seq.rotary(one.expand(1, 3, 1, 64).contiguous(), table)[0, :, 0])

@@ -44,3 +44,28 @@ def test_rotary_heads_past_32_bits(lib):
     v = ctypes.byref(_lib.ntk_view(4096, 0, 0, 0))
     for q, k in ((1 << 30, 1 << 30), (2147483647, 2147483647), (1 << 30, 0), (1 << 20, 1)):
         assert lib.ntk_rotary(1, 1, 1, q, k, 64, 64, 0, 0, v, v, 4096, 8, None, 0, v, v, None) == _lib.NTK_E_UNSUPPORTED
+
+
+def test_outputs_that_overlap(lib):
+    """Rows of an output over each other, or an output that starts where an operand does."""
+    from paper_2206_08720_amd import _lib
+    d = _lib.ntk_attention_desc(_lib.NTK_BF16, 2, 8, 64, 4, 2, 64, 1, 0.125, 0.0)
+
+    def view(place, b=1 << 20, n=256, h=64):
+        return ctypes.byref(_lib.ntk_view(4096 * place, b, n, h))
+
+    q, k, v, o = (view(i + 1) for i in range(4))
+    need = [lib.ntk_attention_workspace(ctypes.byref(d), i) for i in (0, 1)]
+    for out in (q, k, v, view(9, b=0), view(9, n=0), view(9, h=0), view(9, n=63)):
+        assert lib.ntk_attention(ctypes.byref(d), q, k, v, out, None, 4096, need[0], None) == _lib.NTK_E_ARG
+        assert "overlaps" in _lib.last_error()
+        for at in range(3):
+            grads = [view(10 + i) for i in range(3)]
+            grads[at] = out
+            assert lib.ntk_attention_bwd(ctypes.byref(d), view(8), q, k, v, o, 4096, *grads, 4096, need[1], None) == _lib.NTK_E_ARG
+            assert "overlaps" in _lib.last_error()
+    grads = [view(10), view(11), view(11)]
+    assert lib.ntk_attention_bwd(ctypes.byref(d), view(8), q, k, v, o, 4096, *grads, 4096, need[1], None) == _lib.NTK_E_ARG
+    for qo, ko in ((view(9, n=0), view(10)), (view(9), view(10, h=0)), (view(9), view(9)), (k, view(9)), (view(9), q)):
+        assert lib.ntk_rotary(1, 2, 8, 4, 2, 64, 64, 0, 0, q, k, 4096, 8, None, 0, qo, ko, None) == _lib.NTK_E_ARG
+        assert "overlaps" in _lib.last_error()
