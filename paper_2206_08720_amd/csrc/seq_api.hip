@@ -63,6 +63,9 @@ int attn_args(const ntk_attention_desc* d, AttnPlan* plan, bool backward) {
   if (d->head_dim > 128) return bad(NTK_E_UNSUPPORTED, "attention: head_dim over 128");
   if (!(d->scale > 0.f) || !isfinite(d->scale)) return bad(NTK_E_ARG, "attention: scale must be positive and finite");
   if (!(d->softcap >= 0.f) || !isfinite(d->softcap)) return bad(NTK_E_ARG, "attention: softcap must be >= 0 and finite");
+  // the kernels' constants: scale log2(e), softcap log2(e) and 2 scale log2(e) / softcap
+  if (!isfinite(d->scale * kLog2e) || !isfinite(d->softcap * kLog2e) || (d->softcap > 0.f && !isfinite(2.f * kLog2e * d->scale / d->softcap)))
+    return bad(NTK_E_ARG, "attention: scale, softcap or scale / softcap leaves fp32's range in units of log2");
   if (d->prefix && !d->causal) return bad(NTK_E_ARG, "attention: a prefix needs causal");
   // rows and grids are 32-bit; a margin for the last tile
   const long long G = d->heads / d->kv_heads, R = (long long)d->q_len * G, bh = (long long)d->batch * d->kv_heads;

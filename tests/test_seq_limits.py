@@ -69,3 +69,13 @@ def test_outputs_that_overlap(lib):
     for qo, ko in ((view(9, n=0), view(10)), (view(9), view(10, h=0)), (view(9), view(9)), (k, view(9)), (view(9), q)):
         assert lib.ntk_rotary(1, 2, 8, 4, 2, 64, 64, 0, 0, q, k, 4096, 8, None, 0, qo, ko, None) == _lib.NTK_E_ARG
         assert "overlaps" in _lib.last_error()
+
+
+def test_scores_constants_in_range(lib):
+    """scale log2(e), softcap log2(e) and their quotient are formed in fp32: inf times a raw score of 0 would be NaN."""
+    from paper_2206_08720_amd import _lib
+    for bad in (dict(scale=3e38), dict(softcap=3e38), dict(softcap=1e-40), dict(scale=1e30, softcap=1e-30)):
+        for backward in (0, 1):
+            assert _workspace(lib, backward, **bad) == _lib.NTK_E_ARG
+    for good in (dict(scale=2e38), dict(softcap=2e38), dict(softcap=1e-37), dict(scale=1e-40)):
+        assert _workspace(lib, 0, **good) >= 0
