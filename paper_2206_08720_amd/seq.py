@@ -9,6 +9,9 @@ float32, bfloat16 or float16 torch tensors on the GPU; only the last dimension h
 call enqueues on the current stream, or on `stream`, and returns before the work is done.  As in `ntk`, PyTorch
 supplies device memory and streams only: every step runs in libntk.so (include/ntk_seq.h has the
 formulas, the limits and what each mask means).
+
+autograd records none of these calls: their gradients are the calls above.  Where an argument requires a gradient (and
+gradients are enabled) the results require one too, and asking for it raises an error that names the call to make.
 """
 from __future__ import annotations
 
@@ -22,6 +25,7 @@ from . import _lib
 
 _DTYPES = {torch.float32: _lib.NTK_F32, torch.bfloat16: _lib.NTK_BF16, torch.float16: _lib.NTK_F16}
 _NO_CONTEXT = contextlib.nullcontext()
+_MOST = 0x7fffffff
 
 
 def _check(t, name, dtype=None, ndim=None, device=None, shape=None):
@@ -37,8 +41,47 @@ def _check(t, name, dtype=None, ndim=None, device=None, shape=None):
 
 def _sizes(*sizes):
     """The library's sizes are 32-bit integers, and ctypes would cut larger ones."""
-    if max(sizes) > 0x7fffffff:
+    if max(sizes) > _MOST:
         raise _lib.NTKError(_lib.NTK_E_UNSUPPORTED, f"a size of {max(sizes)} does not fit 32 bits")
+
+
+class _Unrecorded(torch.autograd.Function):
+    """Passes results on; a backward pass that reaches them ends with `message`."""
+
+    @staticmethod
+    def forward(ctx, message, outs, *inputs):
+        ctx.message = message
+        return outs
+
+    @staticmethod
+    def backward(ctx, *grads):
+        raise RuntimeError(ctx.message)
+
+
+_recording = torch.is_grad_enabled
+
+
+def _wanted(*inputs):
+    """Whether one of the tensors (or None) requires a gradient."""
+    for t in inputs:
+        if t is not None and t.requires_grad:
+            return True
+    return False
+
+
+def _unrecorded(name, gradient, inputs, *outs):
+    """The results of a call one of whose inputs requires a gradient."""
+    inputs = [t for t in inputs if t is not None]
+    return _Unrecorded.apply(f"autograd does not record seq.{name}: its gradient is {gradient}", outs, *inputs)
+
+
+def _written(name, inputs, *outs):
+    """Before arrays of the caller's are written: refused where a gradient would have to pass, and counted as a change."""
+    if _recording() and _wanted(*inputs, *outs):
+        raise RuntimeError(f"seq.{name} writes into its argument, which autograd does not record: an argument requires a gradient")
+    for t in outs:
+        if t is not None:
+            torch.autograd.graph.increment_version(t)
 
 
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda i: torch.cuda.current_stream(i).cuda_stream)
@@ -118,7 +161,8 @@ def _rms_norm(x, weight, residual, eps, stream, e4m3):
     if x.dim() < 1:
         raise ValueError("x needs a last dimension")
     width = x.shape[-1]
-    _sizes(width)
+    if width > _MOST:
+        _sizes(width)
     if not isinstance(weight, torch.Tensor) or weight.dtype not in (torch.float32, x.dtype):
         raise TypeError(f"weight must be float32 or {x.dtype}")
     _check(weight, "weight", weight.dtype, device=x.device, shape=x.shape[-1:])
@@ -139,6 +183,8 @@ def rms_norm(x, weight, residual=None, eps=1e-6, stream=None):
     """y = h weight / sqrt(mean(h^2) + eps) over the last dimension, with h = x.  With `residual`, h = x + residual
     and (y, h) is returned: h is what the next block adds to and what the backward pass reads."""
     y, h, _ = _rms_norm(x, weight, residual, eps, stream, False)
+    if _recording() and _wanted(x, weight, residual):
+        y, h = _unrecorded("rms_norm", "rms_norm_backward", (x, weight, residual), y, h)
     return y if residual is None else (y, h)
 
 
@@ -146,6 +192,8 @@ def rms_norm_e4m3(x, weight, residual=None, eps=1e-6, stream=None):
     """The norm in 8 bits: (q, scale) or, with `residual`, (q, scale, h), where q (float8_e4m3fn) times its row's scale
     is y, and scale = max|y| / 448."""
     q, h, scale = _rms_norm(x, weight, residual, eps, stream, True)
+    if _recording() and _wanted(x, weight, residual):
+        q, scale, h = _unrecorded("rms_norm_e4m3", "not defined", (x, weight, residual), q, scale, h)
     return (q, scale) if residual is None else (q, scale, h)
 
 
@@ -155,7 +203,8 @@ def rms_norm_backward(dy, h, weight, dh=None, eps=1e-6, stream=None):
     lib = _lib.load()
     _check(h, "h")
     width = h.shape[-1]
-    _sizes(width)
+    if width > _MOST:
+        _sizes(width)
     _check(dy, "dy", h.dtype, device=h.device, shape=h.shape)
     if dh is not None:
         _check(dh, "dh", h.dtype, device=h.device, shape=h.shape)
@@ -174,6 +223,8 @@ def rms_norm_backward(dy, h, weight, dh=None, eps=1e-6, stream=None):
         work = torch.empty(need, dtype=torch.uint8, device=h.device)
         _lib.check(lib.ntk_rms_norm_bwd(_DTYPES[h.dtype], _DTYPES[weight.dtype], rows, width, _ptr(yr), ys, _ptr(hr), hs, _ptr(weight),
                                         _ptr(dr), ds, eps, _ptr(dx), _ptr(dweight), _ptr(work), need, call.handle))
+    if _recording() and _wanted(dy, h, weight, dh):
+        return _unrecorded("rms_norm_backward", "not defined", (dy, h, weight, dh), dx, dweight)
     return dx, dweight
 
 
@@ -221,9 +272,12 @@ def rotary(q, table, positions=0, k=None, interleaved=False, inverse=False, inpl
         _check(positions, "positions", torch.int32, device=q.device, shape=(b, n))
         if not positions.is_contiguous():
             raise ValueError("positions must be contiguous")
-    elif not -1 < positions <= 0x7fffffff:
+    elif not -1 < positions <= _MOST:
         raise _lib.NTKError(_lib.NTK_E_ARG, f"rotary: first position {positions}")
-    _sizes(b, n, heads, 0 if k is None else k.shape[2], dim, table.shape[0], 2 * table.shape[1])
+    if q.numel() > _MOST or table.numel() > _MOST or (k is not None and k.numel() > _MOST):
+        _sizes(b, n, heads, 0 if k is None else k.shape[2], dim, table.shape[0], 2 * table.shape[1])
+    if inplace:
+        _written("rotary", (table,), q, k)
     with _Call(q, stream, (q, table, k, positions if per_token else None)) as call:
         qo = q if inplace else _like(q)
         ko = k if inplace or k is None else _like(k)
@@ -232,6 +286,8 @@ def rotary(q, table, positions=0, k=None, interleaved=False, inverse=False, inpl
                                   int(interleaved), int(inverse), qv, kv, _ptr(table), table.shape[0],
                                   _ptr(positions) if per_token else None, 0 if per_token else int(positions),
                                   qov, kov, call.handle))
+    if not inplace and _recording() and _wanted(q, table, k):
+        qo, ko = _unrecorded("rotary", "rotary with `inverse` turned round, its backward pass", (q, table, k), qo, ko)
     return qo if k is None else (qo, ko)
 
 
@@ -245,7 +301,8 @@ def _attention_desc(q, k, v, causal, softcap, scale, slopes, k_lens, prefix, doc
     if k.shape[0] != b or k.shape[3] != dim:
         raise ValueError(f"k has shape {tuple(k.shape)}, expected ({b}, k_len, kv_heads, {dim})")
     _check(v, "v", q.dtype, device=q.device, shape=k.shape)
-    _sizes(b, sq, sk, heads, kv_heads, dim)
+    if q.numel() > _MOST or k.numel() > _MOST:
+        _sizes(b, sq, sk, heads, kv_heads, dim)
     for name, t, dtype, shape in (("k_lens", k_lens, torch.int32, (b,)), ("prefix", prefix, torch.int32, (b,)),
                                   ("docs", docs, torch.int32, (b, sk)), ("slopes", slopes, torch.float32, (heads,))):
         if t is not None:
@@ -275,11 +332,14 @@ def attention(q, k, v, causal=False, softcap=0.0, scale=None, slopes=None, k_len
     b, sq, heads, dim = q.shape
     if out is not None:
         _check(out, "out", q.dtype, device=q.device, shape=q.shape)
+        _written("attention(out=)", (q, k, v, slopes), out)
     with _Call(q, stream, (q, k, v, slopes, k_lens, prefix, docs, out)) as call:
         o = _like(q) if out is None else out
         lse = torch.empty((b, heads, sq), dtype=torch.float32, device=q.device) if return_lse else None
         work, need = _workspace(lib, desc, 0, q.device)
         _lib.check(lib.ntk_attention(ctypes.byref(desc), *_views(q, k, v, o), _ptr(lse), _ptr(work), need, call.handle))
+    if out is None and _recording() and _wanted(q, k, v, slopes):
+        o, lse = _unrecorded("attention", "attention_backward", (q, k, v, slopes), o, lse)
     return (o, lse) if return_lse else o
 
 
@@ -299,4 +359,6 @@ def attention_backward(do, q, k, v, o, lse, causal=False, softcap=0.0, scale=Non
         work, need = _workspace(lib, desc, 1, q.device)
         views = _views(do, q, k, v, o, dq, dk, dv)
         _lib.check(lib.ntk_attention_bwd(ctypes.byref(desc), *views[:5], _ptr(lse), *views[5:], _ptr(work), need, call.handle))
+    if _recording() and _wanted(do, q, k, v, o, lse, slopes):
+        return _unrecorded("attention_backward", "not defined", (do, q, k, v, o, lse, slopes), dq, dk, dv)
     return dq, dk, dv

@@ -75,3 +75,43 @@ def test_outputs_that_overlap_are_refused():
     assert torch.equal(out, one)
     y = seq.rotary(one.expand(2, 3, 4, 64), table)
     assert torch.equal(y[1, :, 3], seq.rotary(one.expand(1, 3, 1, 64).contiguous(), table)[0, :, 0])
+
+
+def test_gradients_are_not_lost_in_silence():
+    """No call is recorded by autograd.  Its results from tensors that require a gradient stand, and say so when one is asked for; what is
+    written in place counts as changed."""
+    import torch
+    from paper_2206_08720_amd import seq
+    q, x = torch.randn(1, 40, 2, 64, device="cuda"), torch.randn(6, 64, device="cuda")
+    w, table = torch.nn.Parameter(torch.ones(64, device="cuda")), seq.rotary_table(64, 64)
+    p = q.clone().requires_grad_()
+    plain = (seq.rms_norm(x, w.detach()), *seq.rms_norm(x, w.detach(), residual=x), seq.rotary(q, table), seq.attention(q, q, q, causal=True))
+    got = (seq.rms_norm(x, w), *seq.rms_norm(x, w, residual=x), seq.rotary(p, table), seq.attention(p, q, p, causal=True))
+    for a, b in zip(got, plain):
+        assert torch.equal(a, b) and a.requires_grad and not b.requires_grad
+        with pytest.raises(RuntimeError, match="backward"):
+            a.sum().backward()
+    assert w.grad is None and p.grad is None
+    o, lse = seq.attention(p, q, q, return_lse=True)
+    for t in seq.attention_backward(q, p, q, q, o.detach(), lse.detach()) + seq.rms_norm_backward(x, x, w):
+        with pytest.raises(RuntimeError, match="gradient"):
+            t.sum().backward()
+    with torch.no_grad():
+        assert not seq.rms_norm(x, w).requires_grad and not seq.attention(p, p, p).requires_grad
+    # a leaf that requires a gradient is not written; anything else that is written counts as changed
+    with pytest.raises(RuntimeError):
+        seq.rotary(p, table, inplace=True)
+    with pytest.raises(RuntimeError):
+        seq.attention(q, q, q, out=p)
+    for call in (lambda t: seq.rotary(t, table, inplace=True), lambda t: seq.attention(q, q, q, out=t),
+                 lambda t: seq.rotary(q.clone(), table, k=t, inplace=True)):
+        t = q.clone()
+        before = t._version
+        call(t)
+        assert t._version > before
+    a = torch.randn(1, 40, 2, 64, device="cuda", requires_grad=True)
+    t = q.clone()
+    y = (a * t).sum()                                    # keeps t for a's gradient
+    seq.rotary(t, table, inplace=True)
+    with pytest.raises(RuntimeError, match="modified"):
+        y.backward()
