@@ -230,6 +230,14 @@ def rms_norm_backward(dy, h, weight, dh=None, eps=1e-6, stream=None):
 
 # ---- rotary positions ---------------------------------------------------------------------------------------
 
+def _gpu(device):
+    """The GPU that `device` names; the current one for None and for "cuda" without a number."""
+    dev = torch.device("cuda" if device is None else device)
+    if dev.type != "cuda":
+        raise ValueError(f"device {dev} is not a GPU")
+    return torch.device("cuda", torch.cuda.current_device()) if dev.index is None else dev
+
+
 def rotary_table(max_pos, rot, base=10000.0, scaling=None, factor=1.0, original=None, low=1.0, high=32.0, device=None,
                  stream=None):
     """[max_pos, rot / 2, 2] float32: the cosine and sine of every position and pair, angles in 64 bits.  For
@@ -243,7 +251,7 @@ def rotary_table(max_pos, rot, base=10000.0, scaling=None, factor=1.0, original=
         raise ValueError(f"scaling is one of {list(kinds)}")
     if scaling == "ramp" and original is None:
         raise ValueError('scaling="ramp" needs original')
-    dev = torch.device("cuda", torch.cuda.current_device() if device is None else torch.device(device).index or 0)
+    dev = _gpu(device)
     if max_pos < 1 or rot < 2 or rot % 2:
         raise ValueError("rotary_table: max_pos < 1, or rot odd or < 2")
     _sizes(max_pos, rot)

@@ -79,3 +79,14 @@ def test_scores_constants_in_range(lib):
             assert _workspace(lib, backward, **bad) == _lib.NTK_E_ARG
     for good in (dict(scale=2e38), dict(softcap=2e38), dict(softcap=1e-37), dict(scale=1e-40)):
         assert _workspace(lib, 0, **good) >= 0
+
+
+def test_the_table_goes_to_the_current_gpu(monkeypatch):
+    import torch
+    from paper_2206_08720_amd import seq
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 3)
+    for device in (None, "cuda", torch.device("cuda")):
+        assert seq._gpu(device) == torch.device("cuda", 3)
+    assert seq._gpu("cuda:1") == torch.device("cuda", 1) and seq._gpu(torch.device("cuda", 0)).index == 0
+    with pytest.raises(ValueError):
+        seq._gpu("cpu")
