@@ -68,13 +68,11 @@ __device__ __forceinline__ void hide(f32x16& s, f32x16& dp, unsigned vis) {
 }
 
 // delta, and lse in units of log2; a row that sees nothing (lse = -inf) gets weights 0 through inf.
-// fp16 keeps 11 bits only above 2^-14, and p and ds of long rows lie below.  p is formed times 2^10 (its offset is in
-// lse2).  ds, whose size is that of the gradient, is multiplied by a power of two that follows the lane's
-// largest so far, as the running maximum of a softmax does; the sums of the lane change with it.
+// fp16: p is formed times 2^14, as in the forward pass (its offset is in lse2).  ds, whose size is that of the gradient,
+// is multiplied by a power of two that follows the lane's largest so far, as the running maximum of a softmax does; the sums of
+// the lane change with it.
 template <class T>
 constexpr bool kIsF16 = std::is_same_v<T, _Float16>;
-template <class T>
-constexpr float kPScale = kIsF16<T> ? 1024.f : 1.f;
 constexpr float kDsTop = 16384.f;         // a quarter of the largest fp16
 
 template <class T, int N>
@@ -101,7 +99,7 @@ struct DsScale {
     }
   }
   // what the sums are multiplied by at the end
-  __device__ __forceinline__ float undo() const { return 1.f / (mul * kPScale<T>); }
+  __device__ __forceinline__ float undo() const { return kWeightOne<T> / mul; }
 };
 
 // With heads of 128 the wave that multiplies into dq, dk or dv goes before the other one of its SIMD (2 x 16 heads over 8,
@@ -149,7 +147,7 @@ __global__ void __launch_bounds__(256) k_attn_delta(const AttnArgs a, float* __r
   const long long at = ((long long)b * a.H + head) * a.Sq + i;
   const float l = a.lse[at];
   const bool empty = l == -__builtin_inff();
-  lse2[at] = empty ? __builtin_inff() : l * kLog2e - (kIsF16<T> ? 10.f : 0.f);
+  lse2[at] = empty ? __builtin_inff() : l * kLog2e - kWeightBits<T>;
   delta[at] = empty ? 0.f : s;
 }
 
@@ -513,12 +511,12 @@ __device__ __forceinline__ bool dkv_body(const AttnArgs& a, char* smem, int bloc
   if (a.splits > 1) {
     const long long keys = (long long)a.B * a.Hk * a.Sk, row = (long long)bh * a.Sk + j;
     store_owned<float, DP, true>(a.part + ((long long)split * keys + row) * DP, DP, lane, dk, dscale.undo());
-    store_owned<float, DP, true>(a.part + ((long long)(a.splits + split) * keys + row) * DP, DP, lane, dv, 1.f / kPScale<T>);
+    store_owned<float, DP, true>(a.part + ((long long)(a.splits + split) * keys + row) * DP, DP, lane, dv, kWeightOne<T>);
     return false;
   }
   // keys past the batch entry's length get zeros
   store_owned<T, DP, VEC>((T*)a.dk.p + b * a.dk.sb + j * a.dk.ss + hk * a.dk.sh, a.D, lane, dk, a.scale * dscale.undo());
-  store_owned<T, DP, VEC>((T*)a.dv.p + b * a.dv.sb + j * a.dv.ss + hk * a.dv.sh, a.D, lane, dv, 1.f / kPScale<T>);
+  store_owned<T, DP, VEC>((T*)a.dv.p + b * a.dv.sb + j * a.dv.ss + hk * a.dv.sh, a.D, lane, dv, kWeightOne<T>);
   return false;
 }
 template <class T, int DP, bool VEC>

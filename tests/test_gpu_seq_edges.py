@@ -30,6 +30,21 @@ def test_fp16_weights_far_below_the_largest(rows, keys, heads, gap):
     _close("lse", lse[:, few], *ref["lse"])
 
 
+def test_fp16_gradient_of_values_of_small_weight():
+    """Weights of 2^-33, whose sum over the rows with large gradients is dv: formed times 2^14 too.  (The heavy key's own dv is past fp16's
+    largest.)"""
+    import torch
+    from paper_2206_08720_amd import seq
+    q, k, v = torch.zeros(1, 64, 1, 64).half(), torch.zeros(1, 300, 1, 64).half(), _rand((1, 300, 1, 64), 905, "f16")
+    do = (1000 * (1 + _rand((1, 64, 1, 64), 906).abs())).half()
+    q[..., 0], k[0, 77, :, 0] = 8.0, 23.0
+    o, lse = seq.attention(q.cuda(), k.cuda(), v.cuda(), return_lse=True)
+    dv = seq.attention_backward(do.cuda(), q.cuda(), k.cuda(), v.cuda(), o, lse)[2]
+    keep = [j for j in range(300) if j != 77]
+    ref, tol = _oracle(q, k, v, "f16", do, inner=2.0 ** -39)["dv"]
+    _close("dv", dv[:, keep], ref[:, keep], tol[:, keep])
+
+
 # ---- infinities -----------------------------------------------------------------------------------------------------
 
 FORMS = [("f32", 1), ("f32", 64), ("bf16", 1), ("bf16", 64), ("f16", 64)]
