@@ -41,10 +41,11 @@ extern "C" {
  *   h             [rows, width] contiguous, of dtype: the sum, for the next block and the backward pass; may
  *                 be NULL, and may be x or residual itself where that is contiguous.
  *   scale         [rows] fp32, or NULL.
- * y follows from h before h is rounded to dtype.  1 <= width <= 32768; rows may be 0.
+ * y follows from h before h is rounded to dtype.  Rows of any size keep their bits: where squares would leave fp32's range
+ * the row is taken times a power of two.  1 <= width <= 32768; rows may be 0.
  *
  * ntk_rms_norm_bwd: with g = dy weight,  dx = r (g - h r^2 mean(g h)) + dh  (the gradient of x and of the residual),
- * dweight = sum over rows of dy h r.
+ * dweight = sum over rows of dy h r, all at the h that is given: the one that the forward pass rounded to dtype.
  *   dh            the gradient that reaches h otherwise, or NULL.
  *   dx            [rows, width] contiguous, of dtype; may be dy or dh where that is contiguous.
  *   dweight       [width] of wtype.
@@ -78,7 +79,8 @@ typedef struct ntk_view {
  *
  * ntk_rotary -- turns the first `rot` elements of every head of q (and of k, unless NULL) at its position:
  * (u, v) -> (u c - v s, v c + u s), and copies the others.  The pairs are (x[j], x[j + rot / 2]), or with `interleaved`
- * (x[2 j], x[2 j + 1]).  `inverse`: by -s, which undoes it and carries gradients back.
+ * (x[2 j], x[2 j + 1]).  `inverse`: by -s, which carries gradients back, and undoes the turn where mag is 1 (with
+ * NTK_ROTARY_RAMP it gives mag^2 times what was turned).
  *   positions   [batch, length] int32, or NULL: first_position + index.  A position outside the table gives NaN.
  *   q_out       may be q itself (in place), and k_out k; no other overlap.
  * rot is even, 2 <= rot <= dim.  batch, length and head counts may be 0. */
@@ -121,8 +123,10 @@ int ntk_rotary(int dtype, int batch, int length, int q_heads, int k_heads, int d
  * ntk_attention_bwd -- dq, dk and dv from dout, with o and lse of the forward call.  softcap, slopes and masks as
  * there; the slopes get no gradient.  Keys past k_lens get zeros.  dq, dk, dv must not overlap the inputs.
  *   workspace                ntk_attention_workspace(desc, 1) bytes.
- * The p and ds factors of the products over the keys (rows) are rounded to dtype, in fp16 under powers of two that keep
- * them in its range. */
+ * The p and ds factors of the products over the keys (rows), forward and backward, are rounded to dtype, in fp16 under powers of
+ * two that keep them in its range, and the backward pass goes by the o that was rounded to dtype.  With a cap, scores of bf16 and fp16
+ * have an absolute error of about 2^-22 softcap.  fp32 products are formed from three bf16 parts of each operand and are
+ * good to 2^-22; where one meets an infinity or a NaN, on the fp32 matrix instructions. */
 typedef struct ntk_attention_desc {
     int dtype, batch, q_len, k_len, heads, kv_heads, head_dim, causal;
     float scale, softcap;

@@ -470,7 +470,8 @@ AttnPlan attn_plan_fwd(int dtype, int B, int Hk, int R, int Sk, int D) {
   p.tokens = R <= 32;
   p.tiles = (R + kFwdRows - 1) / kFwdRows;
   const long long blocks = (long long)B * Hk * (p.tokens ? 1 : p.tiles);
-  // Ranges of the keys.  Tokens: enough workgroups for two on each of 256 compute units, each with at least 64 KB of
+  // Ranges of the keys.  Tokens: 512 workgroups or more, two for each of 256 compute units (heads over 64 leave room for one at
+  // a time, by their registers and LDS; the second evens out what lengths of their own leave idle), each with at least 64 KB of
   // keys: a call over 777 keys of 8 heads of 64 takes 13.5 us in one range and 20 in four, with the join and its
   // launch; with heads of 128 the ranges pay on the GPU (12 us against 18).  Many rows: as many as run at once, of
   // at least 256 keys (64 in fp32, whose products take several times as long); from 192 tiles on the join's traffic

@@ -5,7 +5,8 @@
 // (c the capped score; the factor is 1 without a cap).  Two kernels: one owns rows and sums over the keys
 // (dq), one owns keys and sums over the rows of every query head that shares them (dk, dv).  Forming the
 // scores twice costs 7 products instead of 5, and buys results that no order of atomics changes.
-// p and ds are rounded to the inputs' type for the products; everything else is fp32.
+// p and ds are rounded to the inputs' type for the products, as the matrix cores take them (fp16: in powers of two that keep
+// them in its range), and delta is formed with the o that the forward pass stored; everything else is fp32.
 #include "seq/attn_core.hpp"
 #include "seq/launch_attn.hpp"
 
@@ -320,9 +321,11 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) k_attn_dq(const A
 // ---- dk, dv: four waves of 32 keys over the row tiles -----------------------------------------------------
 // A wave's keys stay in registers and its values in LDS: with both in registers (and dk, dv in 128 more) only one
 // wave a SIMD would fit, and nothing would run beside its MFMAs.  The loop is written to need no more than 256
-// registers: a reload from scratch memory would wait for the next tile's loads too.  The same sizes as dq's: 372 us and
-// 31 for the sums of two ranges, 682 TFLOP/s of the four products (about 1000 without the causal order, whose first
-// tiles last longest).  dk and dv in workgroups of their own, with one product more, took 520 where this took 440.
+// registers: a reload from scratch memory would wait for the next tile's loads too.  The same sizes as dq's: 365 us, 750
+// TFLOP/s of the four products (in full 650 us, 850), and 32 more for the sums of two ranges.  Counters: the matrix cores are busy
+// 39 % of the time (42 % in full), the vector units 41 %, LDS 30 % with no bank conflict, and the compute units throughout; so it is
+// two waves a SIMD that mostly take turns that bound it, neither LDS nor the unequal work of the causal order.  dk and dv in
+// workgroups of their own, with one product more, took 520 where this took 440.
 constexpr int kBwdRowTile = 32;
 constexpr int kBwdKeyTile = 128;
 
@@ -648,7 +651,8 @@ AttnBwdPlan attn_plan_bwd(int dtype, int B, int Hk, int R, int Sk, int D, bool c
   if (p.dq_tiles) p.dq_splits = ranges(bh * p.dq_tiles, Sk, dtype);
   if (p.dkv_tiles) p.dkv_splits = ranges(bh * p.dkv_tiles, R, dtype);
   // A causal tile's work falls with its place: where all workgroups run at once the first ones last twice as long as
-  // the mean.  Halved, they leave room that others fill (2 x 16 heads over 8, 4096 positions of 128: 467 us with the sums' addition against 626).
+  // the mean.  Halved, they leave room that others fill (2 x 16 heads over 8, 4096 positions of 128: 467 us with the sums' addition against
+  // 626).  Measured at this size; the traffic of the sums, which short rows feel most, is not weighed against it.
   if (causal && p.dkv_splits == 1 && bh * p.dkv_tiles < 2048 && p.dkv_tiles > 2) p.dkv_splits = 2;
   const long long dq = p.dq_splits > 1 ? p.dq_splits * bh * R * dp : 0, dkv = p.dkv_splits > 1 ? 2 * p.dkv_splits * bh * Sk * dp : 0;
   p.flag_ints = bh * std::max(p.dq_tiles * p.dq_splits, p.dkv_tiles * p.dkv_splits);

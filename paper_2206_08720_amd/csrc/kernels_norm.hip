@@ -3,11 +3,13 @@
 //   h = x + residual,  r = (mean h^2 + eps)^(-1/2),  y = h r w;   8 bits: s = max|y| / 448, q = e4m3(y / s)
 //   g = dy w,  dx = r (g - h r^2 mean(g h)) + dh,  dw = sum_rows dy h r
 //
-// A row is held in registers between its two uses, so every array moves once.  Sums are fp32; y follows from the
-// unrounded h, and the gradient from the h that was stored.  A row takes 64, 256 or 1024 threads, each
-// with CH groups of 8 elements: short rows share a workgroup, long ones fill one.  Bound by memory: 16384 rows of
-// 4096 in bf16 take 100 us forward (5.3 TB/s; a large copy reaches 4.7), 8192 rows of 2048 28 us backward and 5 for
-// the columns' sums.
+// A row is held in registers between its two uses, so every array moves once; only the backward kernels of more than 16384
+// columns spill (93 to 150 registers).  Sums are fp32; y follows from the unrounded h, and the gradient from the h that
+// was stored, which is all that the backward pass is given: in bf16 its dw is then 1.3 to 1.5 times as far off as from the
+// unrounded h.  A row takes 64, 256 or 1024 threads, each with CH groups of 8 elements: short rows share a workgroup, long ones
+// fill one (rows of 64 columns leave 56 of a wave's lanes idle, of 128 48: 262144 rows of 128 take 78 us, 3.4 TB/s).  Bound by
+// memory: 16384 rows of 4096 in bf16 take 100 us forward (5.4 TB/s; a large copy reaches 4.7), 8192 rows of 2048 30 us backward
+// with 5 for the columns' sums, 2048 rows of 32768 323 us, whose spills show.
 #include <hip/hip_runtime.h>
 
 #include "seq/launch_seq.hpp"

@@ -65,8 +65,9 @@ struct Num<float> {
   using Four = f32x4;
   // x = h + m + l in three bf16 values of 8 bits each (the whole 24 of an fp32, at its full range; h is cut, not
   // rounded, so that the largest stay finite).  Six products of parts take 192 cycles of the matrix cores where eight
-  // fp32 MFMAs of the same 16 k take 512; what bounds the fp32 kernels then is the splitting on the vector units (8 heads
-  // of 64, 4096 positions: 320 us forward and 1130 backward, against 359 and 1202 on the fp32 MFMAs).
+  // fp32 MFMAs of the same 16 k take 512; what bounds the fp32 kernels then is the splitting on the vector units, of both
+  // operands at every step (8 heads of 64, 4096 positions: 296 us forward and 1050 backward, against 359 and 1202 on the fp32
+  // MFMAs).
   // What is not finite has parts that are NaN, so every result that it meets is NaN; such a result is formed again on the
   // fp32 MFMAs (product<true>), where inf times a number is inf of the right sign.
   struct Parts {
@@ -85,7 +86,8 @@ struct Num<float> {
     }
     return p;
   }
-  // the six products of parts down to 2^-16 of the whole, smallest first; the three left out are below 2^-24 of it
+  // the six products of parts down to 2^-16 of the whole, smallest first.  m reaches 2^-7 of x and l 2^-16, so the three
+  // left out are up to 2^-22 of a product: four fp32 roundoffs at most, one on the average.
   __device__ static __forceinline__ f32x16 mma(Frag a, Frag b, f32x16 c) {
     const Parts x = split(a), y = split(b);
     c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x.l, y.h, c, 0, 0, 0);
@@ -543,7 +545,8 @@ __device__ __forceinline__ f32x16 mma_visible(typename Num<T>::Frag a, typename 
 // A kernel's body comes in two forms.  The ordinary one leaves a flag where its result has to be formed again; a second
 // launch, of the careful form with mma_visible, takes the flagged blocks (4.6 us where there are none).  Both in one kernel
 // took 700 us for dk and dv of 2 x 16 heads over 8, 4096 positions of 128, against 604: the careful form's registers
-// make the compiler spill in the ordinary loop.  The token kernel has registers to spare and holds both.
+// make the compiler spill in the ordinary loop.  The token kernel holds both: it is bound by memory, and only its forms
+// for heads of 65 to 128 without 16-byte accesses spill (16 bits 31 registers, fp32 177).
 constexpr int kAgainBlocks = 256;
 template <class Body>
 __device__ __forceinline__ void again(const int* flags, int blocks, Body body) {

@@ -266,7 +266,8 @@ def rotary_table(max_pos, rot, base=10000.0, scaling=None, factor=1.0, original=
 def rotary(q, table, positions=0, k=None, interleaved=False, inverse=False, inplace=False, stream=None):
     """Turns the first 2 * table.shape[1] elements of every head of q [batch, length, heads, dim], and of k with head counts of
     its own, by their positions: int32 [batch, length], or the first position of every sequence.  Returns q, or
-    (q, k).  `inverse` undoes it, which is also how the gradients pass."""
+    (q, k).  `inverse` turns the other way, which is how the gradients pass; it undoes the turn unless the table is a "ramp",
+    whose magnitude is not 1."""
     lib = _lib.load()
     _check(q, "q", ndim=4)
     _check(table, "table", torch.float32, ndim=3, device=q.device)
