@@ -1,6 +1,7 @@
 /*
  * ntk_seq.h -- C ABI of the operators of a sequence model's block on MI355X (gfx950): root-mean-square
- * norm, rotary positions and attention, forward, backward and for single tokens.
+ * norm, rotary positions and attention, forward, backward and for single tokens; of the cache of pages that it answers
+ * from; and of the log probabilities of the tokens that it answers with.
  *
  * They compute what stands in front of the networks of ntk.h when these read the features of a sequence
  * trunk: the trunk's pass (its output is the X of ntk_compute), the trunk's gradients, and its answer token
@@ -31,6 +32,7 @@ extern "C" {
 #define NTK_F32  0
 #define NTK_BF16 1
 #define NTK_F16  2
+#define NTK_E4M3 3   /* a cache's cells (ntk_cache) */
 
 /* ---- root-mean-square norm -----------------------------------------------------------------------
  * h = x + residual (residual NULL: h = x),  r = (mean(h^2) + eps)^(-1/2) over each row,  y = h r weight.
@@ -143,6 +145,79 @@ int ntk_attention(const ntk_attention_desc* desc, const ntk_view* q, const ntk_v
 int ntk_attention_bwd(const ntk_attention_desc* desc, const ntk_view* dout, const ntk_view* q, const ntk_view* k,
                       const ntk_view* v, const ntk_view* o, const float* lse, const ntk_view* dq, const ntk_view* dk,
                       const ntk_view* dv, void* workspace, long long workspace_bytes, void* hip_stream);
+
+/* ---- a cache in pages --------------------------------------------------------------------------------
+ * Keys and values of many sequences lie in pages of page_size places, handed out by the caller: place p of sequence b is slot
+ * p % page_size of page page_table[b, p / page_size].  The caller holds the cache between calls; the library keeps nothing.
+ *   dtype                    NTK_E4M3, or the type of the call's arrays.
+ *   k, v                     views [page, slot, head, dim], the strides in elements.  Heads that lie apart, [page, head, slot, dim], are
+ *                            read in whole lines.
+ *   k_scale, v_scale         [pages, kv_heads] fp32 contiguous, NTK_E4M3 only: the cells of a page and head stand for their values
+ *                            times it.  Always a power of two from 2^-126 on, as ntk_cache_append leaves it.
+ *   page_size                a power of two from 1 to 1024.
+ *   page_table               [batch, max_pages] int32.  Entries past a sequence's places are not used and may hold anything. */
+typedef struct ntk_cache {
+    int dtype, pages, page_size, kv_heads, head_dim;
+    ntk_view k, v;
+    float *k_scale, *v_scale;
+    const int* page_table;
+    int max_pages;
+} ntk_cache;
+
+/* Appends the first new_lens[b] (all `length` without new_lens) of the new tokens k, v [batch, length, kv_heads, head_dim] to
+ * each sequence, at the places from lens[b] on, k turned as by ntk_rotary to its position: positions[b, i], or its place
+ * without `positions`.  q [batch, length, q_heads, head_dim] (or NULL) is turned to q_out; its rows past new_lens[b] become zeros.
+ *   dtype         of q, k, v and q_out.  In a cache of that type cells are rounded once, from the turned fp32.
+ *   NTK_E4M3      the scale s of a page and head is the least power of two (from 2^-126 on) under which no new finite
+ *                 value is above 448 s; on a page whose first slots hold older tokens it is at least what it was, and where it grows, those
+ *                 slots are rounded again under it (exactly but for the type's subnormals).  Values that are not finite become NaN.
+ *                 Values of fp16 over 61440 become 61440, so that no query in fp16 reads them as infinity.
+ *   table         [max_pos, rot / 2, 2] fp32 of ntk_rotary_table, or NULL with rot = 0: nothing turns.  A position that it lacks
+ *                 gives NaN.
+ *   lens, new_lens  [batch] int32 (values are clamped to 0 .. max_pages page_size and 0 .. length).
+ * A token whose place is past max_pages page_size, or on a page number outside the cache, is dropped.  Slots that get no token keep
+ * their bytes.  The pages that one call writes belong to one sequence each: what two sequences write into the same page is undefined,
+ * as is a place that is read elsewhere meanwhile.  q_out must not overlap another array.  One launch. */
+int ntk_cache_append(int dtype, int batch, int length, int q_heads, const ntk_cache* cache, const int* lens, const int* new_lens,
+                     const ntk_view* k, const ntk_view* v, const ntk_view* q, const ntk_view* q_out, const float* table,
+                     int max_pos, int rot, int interleaved, const int* positions, void* hip_stream);
+
+/* Attention over a cache: as ntk_attention, with k_len = max_pages page_size places and k_lens[b] of them filled.
+ * Queries i < q_lens[b] (all q_len without q_lens) are the last of them: p_i = k_lens[b] - q_lens[b] + i.  The rows of o
+ * past them are zeros, their lse -inf.  A place on a page number outside the cache reads as NaN.
+ *   desc          dtype of q and o; heads, kv_heads, head_dim, q_len, causal, scale, softcap, slopes as there; k_lens is
+ *                 required, prefix and docs must be NULL; k_len is max_pages page_size.
+ *   cache         with NTK_E4M3 cells take dtype times their scale: over 65504 that is an infinity in fp16.
+ *   o             must not overlap q or the cache.
+ *   workspace     ntk_attention_cached_workspace(desc, cache->dtype) bytes, 16-byte aligned. */
+long long ntk_attention_cached_workspace(const ntk_attention_desc* desc, int cache_dtype);
+int ntk_attention_cached(const ntk_attention_desc* desc, const ntk_cache* cache, const int* q_lens, const ntk_view* q,
+                         const ntk_view* o, float* lse, void* workspace, long long workspace_bytes, void* hip_stream);
+
+/* ---- log probabilities of given tokens --------------------------------------------------------------
+ * Of every row of logits [rows, vocab], with x = scale logits in fp32 and p = softmax(x):
+ *   logp[r]      = log p[t] for the token t = tokens[r]; 0 for t < 0 (a prompt, padding); NaN for t >= vocab.
+ *   entropy[r]   = -sum p log p (natural); may be NULL.
+ *   lse[r]       two numbers, m = the largest logit and log sum e^(x - scale m), for the gradient: log sum e^x is scale times the first
+ *                plus the second, which as one number would lose what large logits leave of it.  May be NULL.
+ *   top_logp, top_tokens [rows, top]   the `top` most likely tokens in order (of equal logits the lower token first; NaN
+ *                before all) and their log probabilities.  0 <= top <= 64, top <= vocab; with top = 0 they are not used.
+ * Logits of -inf are tokens that are ruled out: they have p = 0.  In a row of nothing else every log probability
+ * is -inf, the entropy 0, and lse (-inf, 0).  A NaN or +inf makes its row's results NaN.
+ *   logits       `stride` elements between rows (>= vocab).   scale > 0 (one over the temperature).
+ *   workspace    ntk_logprobs_workspace(...) bytes, 16-byte aligned: partial results of the ranges that few rows are cut into.
+ *
+ * ntk_logprobs_bwd: dlogits[r, j] = scale (dlogp[r] (1[j = t] - p_j) - dentropy[r] p_j (log p_j + entropy[r])), with the lse and
+ * entropy of the forward call; dlogp or dentropy may be NULL (zeros).  Tokens t < 0 take no part in dlogp.  Rows in which every
+ * token is ruled out get zeros.  Alternatives carry no gradient.
+ *   dlogits      dtype, `dlogits_stride` elements between rows (>= vocab); may be logits itself (with the same stride), no other overlap. */
+long long ntk_logprobs_workspace(int dtype, long long rows, int vocab, int top);
+int ntk_logprobs(int dtype, long long rows, int vocab, const void* logits, long long stride, const int* tokens, float scale, int top,
+                 float* logp, float* entropy, float* lse, float* top_logp, int* top_tokens, void* workspace,
+                 long long workspace_bytes, void* hip_stream);
+int ntk_logprobs_bwd(int dtype, long long rows, int vocab, const void* logits, long long stride, const int* tokens, float scale,
+                     const float* lse, const float* entropy, const float* dlogp, const float* dentropy, void* dlogits,
+                     long long dlogits_stride, void* hip_stream);
 
 #ifdef __cplusplus
 }

@@ -38,10 +38,12 @@ EXPORTED_SYMBOLS = ("ntk_init", "ntk_compute", "ntk_free", "ntk_last_error", "nt
                     "ntk_profile_read", "ntk_device_info", "ntk_mfma_peak",
                     "ntk_vector_product", "ntk_compute_static")
 # include/ntk_seq.h
-NTK_F32, NTK_BF16, NTK_F16 = 0, 1, 2
+NTK_F32, NTK_BF16, NTK_F16, NTK_E4M3 = 0, 1, 2, 3
 NTK_ROTARY_PLAIN, NTK_ROTARY_LINEAR, NTK_ROTARY_BASE, NTK_ROTARY_RAMP = 0, 1, 2, 3
 EXPORTED_SEQ_SYMBOLS = ("ntk_rms_norm", "ntk_rms_norm_workspace", "ntk_rms_norm_bwd", "ntk_rotary_table", "ntk_rotary",
-                        "ntk_attention_workspace", "ntk_attention", "ntk_attention_bwd")
+                        "ntk_attention_workspace", "ntk_attention", "ntk_attention_bwd", "ntk_cache_append",
+                        "ntk_attention_cached_workspace", "ntk_attention_cached", "ntk_logprobs_workspace", "ntk_logprobs",
+                        "ntk_logprobs_bwd")
 STATIC_SCRATCH_BYTES = 64 * 1024 * 1024   # NTK_STATIC_SCRATCH_BYTES
 
 
@@ -70,6 +72,12 @@ class ntk_attention_desc(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int) for n in ("dtype", "batch", "q_len", "k_len", "heads", "kv_heads", "head_dim", "causal")] + [
         ("scale", ctypes.c_float), ("softcap", ctypes.c_float), ("k_lens", ctypes.c_void_p), ("prefix", ctypes.c_void_p),
         ("docs", ctypes.c_void_p), ("slopes", ctypes.c_void_p)]
+
+
+class ntk_cache(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int) for n in ("dtype", "pages", "page_size", "kv_heads", "head_dim")] + [
+        ("k", ntk_view), ("v", ntk_view), ("k_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p),
+        ("page_table", ctypes.c_void_p), ("max_pages", ctypes.c_int)]
 
 
 class NTKError(RuntimeError):
@@ -122,6 +130,7 @@ def load():
     lib.ntk_mfma_peak.argtypes = [ctypes.c_int, ctypes.POINTER(ctypes.c_double)]
     lib.ntk_mfma_peak.restype = ctypes.c_int
     I, L, F = ctypes.c_int, ctypes.c_longlong, ctypes.c_float
+    C = ctypes.POINTER(ntk_cache)
     V, D = P, ctypes.POINTER(ntk_attention_desc)   # views: byref() of an ntk_view, or of its four numbers in an array
     for name, args, res in (
             ("ntk_rms_norm", [I, I, L, I, P, L, P, L, P, F, P, P, P, P], I),
@@ -131,7 +140,13 @@ def load():
             ("ntk_rotary", [I] * 9 + [V, V, P, I, P, I, V, V, P], I),
             ("ntk_attention_workspace", [D, I], L),
             ("ntk_attention", [D, V, V, V, V, P, P, L, P], I),
-            ("ntk_attention_bwd", [D, V, V, V, V, V, P, V, V, V, P, L, P], I)):
+            ("ntk_attention_bwd", [D, V, V, V, V, V, P, V, V, V, P, L, P], I),
+            ("ntk_cache_append", [I, I, I, I, C, P, P, V, V, V, V, P, I, I, I, P, P], I),
+            ("ntk_attention_cached_workspace", [D, I], L),
+            ("ntk_attention_cached", [D, C, P, V, V, P, P, L, P], I),
+            ("ntk_logprobs_workspace", [I, L, I, I], L),
+            ("ntk_logprobs", [I, L, I, P, L, P, F, I, P, P, P, P, P, P, L, P], I),
+            ("ntk_logprobs_bwd", [I, L, I, P, L, P, F, P, P, P, P, P, L, P], I)):
         f = getattr(lib, name)
         f.argtypes, f.restype = args, res
     _lib = lib

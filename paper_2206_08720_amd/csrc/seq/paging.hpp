@@ -1,0 +1,54 @@
+// paging.hpp -- where a position of a sequence lies in a cache of pages (integer arithmetic, for the kernels and for the host).
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+namespace ntk {
+
+// A sequence's place `pos` is slot pos % 2^shift of the page that entry pos / 2^shift of its row of the table names.
+struct PageTable {
+  const int* table = nullptr;    // [batch, most]
+  int most = 0, pages = 0, shift = 0;
+  __host__ __device__ __forceinline__ int slot(int pos) const { return pos & ((1 << shift) - 1); }
+  // the page, or -1 where the row ends before it or names none of the cache's
+  __host__ __device__ __forceinline__ int page(int b, int pos) const {
+    const int e = pos >> shift;
+    if (pos < 0 || e >= most) return -1;
+    const int id = table[(long long)b * most + e];
+    return (unsigned)id < (unsigned)pages ? id : -1;
+  }
+};
+
+// The tokens that an append adds to one sequence: positions first .. first + count - 1.
+struct AppendSpan {
+  int first, count;
+  __host__ __device__ __forceinline__ AppendSpan(const PageTable& t, int held, int new_tokens, int length) {
+    const int places = t.most << t.shift;    // places + length < 2^31, checked on the host
+    first = held < 0 ? 0 : held > places ? places : held;
+    count = new_tokens < 0 ? 0 : new_tokens > length ? length : new_tokens;
+  }
+  // the slots [lo, hi) of the sequence's page number `e` that get new tokens, and the index of the first one's token
+  __host__ __device__ __forceinline__ bool slots(const PageTable& t, int e, int& lo, int& hi, int& token) const {
+    const int size = 1 << t.shift;
+    if (e >= t.most) return false;
+    const int at = e << t.shift, end = first + count;
+    lo = first > at ? first - at : 0;
+    hi = end - at < size ? end - at : size;
+    token = at + lo - first;
+    return lo < hi;
+  }
+};
+// pages that `length` new tokens of a sequence can touch
+__host__ __device__ inline int append_pages(int length, int shift) {
+  return length < 1 ? 0 : (int)(((long long)length + (1 << shift) - 2) >> shift) + 1;
+}
+
+// The exponent of the least power of two that `most` (finite, >= 0) is at most 448 times of, but at least -126.
+__host__ __device__ inline int e4m3_exponent(float most) {
+  uint32_t u;
+  __builtin_memcpy(&u, &most, 4);
+  const int e = (int)(u >> 23) - 127 - 8 + ((u & 0x7fffffu) > 0x600000u ? 1 : 0);   // 448 = 1.75 2^8
+  return e < -126 ? -126 : e;
+}
+
+}  // namespace ntk

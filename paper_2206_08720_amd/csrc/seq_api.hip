@@ -3,8 +3,9 @@
 #include <math.h>
 #include <stdio.h>
 
-#include "seq/attn_core.hpp"
+#include "seq/attn_cached.hpp"
 #include "seq/launch_attn.hpp"
+#include "seq/launch_cache.hpp"
 #include "seq/launch_seq.hpp"
 #include "ntk_seq.h"
 
@@ -52,8 +53,8 @@ bool apart(const ntk_view* v, int batch, int positions, int heads, int dim) {
 }
 bool same_place(const ntk_view* a, const ntk_view* b) { return a->data == b->data; }
 
-// Checks a descriptor for the pass asked for; `plan` as the forward pass runs it.
-int attn_args(const ntk_attention_desc* d, AttnPlan* plan, bool backward) {
+// Checks a descriptor for the pass asked for; `plan` as the forward pass runs it.  cells: the type of a cache in pages, or -1.
+int attn_args(const ntk_attention_desc* d, AttnPlan* plan, bool backward, int cells = -1) {
   if (!d) return bad(NTK_E_ARG, "attention: the descriptor is NULL");
   if (!type_ok(d->dtype)) return bad(NTK_E_ARG, "attention: dtype");
   if (d->batch < 0 || d->q_len < 0 || d->k_len < 0) return bad(NTK_E_ARG, "attention: batch, q_len or k_len < 0");
@@ -72,7 +73,8 @@ int attn_args(const ntk_attention_desc* d, AttnPlan* plan, bool backward) {
   if (R >= (1LL << 29) - 1024 || d->k_len >= (1LL << 31) - 1024 || bh >= (1LL << 31))
     return bad(NTK_E_UNSUPPORTED, "attention: q_len * group reaches 2^29 or k_len 2^31");
   if (R > 0 && bh > 0) {
-    *plan = attn_plan_fwd(d->dtype, d->batch, d->kv_heads, (int)R, d->k_len, d->head_dim);
+    *plan = cells < 0 ? attn_plan_fwd(d->dtype, d->batch, d->kv_heads, (int)R, d->k_len, d->head_dim)
+                      : attn_plan_cached(d->dtype, cells == NTK_E4M3, d->batch, d->kv_heads, (int)R, d->k_len, d->head_dim);
     const int dp = d->head_dim <= 64 ? 64 : 128;
     const long long rows = bh * R, keys = bh * d->k_len, spr = 256 / (dp / 4);   // rows a workgroup of the ranges' sums
     bool fits;
@@ -130,6 +132,57 @@ bool span_ok(const ntk_view* v, int rows, int G, int D, int e) {
   const long long lim = (1LL << 31) - (1 << 16);
   if (v->stride_position > lim / (rows + 1) / e || v->stride_head > lim / (G + 1) / e) return false;
   return ((rows + 1) * v->stride_position + G * v->stride_head + D) * e < lim;
+}
+
+// A cache that calls of type `dtype` use; `what` names the call.
+int cache_args(const ntk_cache* c, int dtype, int batch, const char* what) {
+  char text[160];
+  auto no = [&](int code, const char* why) {
+    snprintf(text, sizeof text, "%s: %s", what, why);
+    return bad(code, text);
+  };
+  if (!c) return no(NTK_E_ARG, "the cache is NULL");
+  if (c->dtype != NTK_E4M3 && c->dtype != dtype) return no(NTK_E_ARG, "the cache's dtype is the call's or NTK_E4M3");
+  if (c->pages < 0 || c->max_pages < 0) return no(NTK_E_ARG, "pages or max_pages < 0");
+  if (c->page_size < 1 || c->page_size > 1024 || (c->page_size & (c->page_size - 1)))
+    return no(NTK_E_UNSUPPORTED, "page_size must be a power of two from 1 to 1024");
+  if (c->kv_heads < 1) return no(NTK_E_SHAPE, "kv_heads < 1");
+  if (c->head_dim < 1) return no(NTK_E_ARG, "head_dim < 1");
+  if (c->head_dim > 128) return no(NTK_E_UNSUPPORTED, "head_dim over 128");
+  if ((long long)c->max_pages * c->page_size >= (1LL << 31) - 1024) return no(NTK_E_UNSUPPORTED, "max_pages * page_size reaches 2^31");
+  if (batch > 0 && c->max_pages > 0 && (!c->page_table || !aligned(c->page_table, 4))) return no(NTK_E_ARG, "page_table is NULL or unaligned");
+  if (c->pages > 0) {
+    const int e = c->dtype == NTK_E4M3 ? 1 : elem(dtype);
+    if (!view_ok(&c->k, e) || !view_ok(&c->v, e)) return no(NTK_E_ARG, "the cache's k or v is missing, unaligned or has a negative stride");
+    if (c->dtype == NTK_E4M3 && (!c->k_scale || !c->v_scale || !aligned(c->k_scale, 4) || !aligned(c->v_scale, 4) || c->k_scale == c->v_scale))
+      return no(NTK_E_ARG, "k_scale or v_scale is NULL, unaligned, or the other one");
+  }
+  return NTK_OK;
+}
+int shift_of(int page_size) {
+  int s = 0;
+  while ((1 << s) < page_size) ++s;
+  return s;
+}
+PageTable page_table(const ntk_cache* c) {
+  PageTable t;
+  t.table = c->page_table;
+  t.most = c->max_pages;
+  t.pages = c->pages;
+  t.shift = shift_of(c->page_size);
+  return t;
+}
+
+int logprob_args(int dtype, long long rows, int vocab, int top) {
+  if (!type_ok(dtype)) return bad(NTK_E_ARG, "logprobs: dtype");
+  if (rows < 0 || vocab < 1) return bad(NTK_E_ARG, "logprobs: rows < 0 or vocab < 1");
+  if (top < 0 || top > vocab) return bad(NTK_E_ARG, "logprobs: top < 0 or over vocab");
+  if (top > 64) return bad(NTK_E_UNSUPPORTED, "logprobs: top over 64");
+  // element numbers of a row are 32-bit, with a margin for the last workgroup's
+  if (vocab >= (1 << 30)) return bad(NTK_E_UNSUPPORTED, "logprobs: vocab reaches 2^30");
+  if (rows >= (1LL << 31) || (rows > 0 && (!grid_ok(rows * logprob_splits(dtype, rows, vocab), 256) || !grid_ok(rows * logprob_bwd_chunks(dtype, vocab), 256))))
+    return bad(NTK_E_UNSUPPORTED, "logprobs: too many rows for one launch");
+  return NTK_OK;
 }
 
 }  // namespace
@@ -342,5 +395,186 @@ extern "C" int ntk_attention_bwd(const ntk_attention_desc* desc, const ntk_view*
   }
   a.lse = const_cast<float*>(lse);
   const hipError_t err = launch_attn_bwd((hipStream_t)hip_stream, desc->dtype, a, bwd_plan(desc), (float*)workspace, vec);
+  return err == hipSuccess ? NTK_OK : hip_bad(err);
+}
+
+extern "C" int ntk_cache_append(int dtype, int batch, int length, int q_heads, const ntk_cache* cache, const int* lens,
+                                const int* new_lens, const ntk_view* k, const ntk_view* v, const ntk_view* q, const ntk_view* q_out,
+                                const float* table, int max_pos, int rot, int interleaved, const int* positions, void* hip_stream) {
+  if (!type_ok(dtype)) return bad(NTK_E_ARG, "cache_append: dtype");
+  if (batch < 0 || length < 0 || q_heads < 0) return bad(NTK_E_ARG, "cache_append: a size is negative");
+  if (int rc = cache_args(cache, dtype, batch, "cache_append")) return rc;
+  const int dim = cache->head_dim, kv = cache->kv_heads, e = elem(dtype);
+  const bool e4m3 = cache->dtype == NTK_E4M3;
+  if (rot < 0 || rot % 2 || rot > dim) return bad(NTK_E_SHAPE, "cache_append: rot must be even, 0 <= rot <= head_dim");
+  if (rot && (max_pos < 1 || !table || !aligned(table, 4))) return bad(NTK_E_ARG, "cache_append: table is NULL or unaligned, or max_pos < 1");
+  if (!q) q_heads = 0;
+  if (batch == 0 || length == 0) return NTK_OK;
+  if (!lens || !aligned(lens, 4) || !aligned(new_lens, 4) || !aligned(positions, 4))
+    return bad(NTK_E_ARG, "cache_append: lens is NULL, or a pointer is not aligned to its type");
+  if (!view_ok(k, e) || !view_ok(v, e) || (q_heads && (!view_ok(q, e) || !view_ok(q_out, e))))
+    return bad(NTK_E_ARG, "cache_append: a view is missing, unaligned or has a negative stride");
+  if (cache->pages > 0) {
+    const ntk_view* cells[2] = {&cache->k, &cache->v};
+    for (const ntk_view* c : cells)
+      if (!apart(c, cache->pages, cache->page_size, kv, dim) || same_place(c, k) || same_place(c, v) || (q_heads && (same_place(c, q) || same_place(c, q_out))))
+        return bad(NTK_E_ARG, "cache_append: the cache overlaps itself or another array");
+    if (same_place(cells[0], cells[1])) return bad(NTK_E_ARG, "cache_append: the cache overlaps itself or another array");
+  }
+  if (q_heads && (!apart(q_out, batch, length, q_heads, dim) || same_place(q_out, q) || same_place(q_out, k) || same_place(q_out, v)))
+    return bad(NTK_E_ARG, "cache_append: q_out overlaps itself or another array");
+  const long long rows = (long long)batch * length, heads = (long long)q_heads + 2LL * kv;
+  if (rows >= (1LL << 31) || heads * (dim / 16 + 2) >= (1LL << 20) || (long long)cache->max_pages * cache->page_size + length >= (1LL << 31) - 1024)
+    return bad(NTK_E_UNSUPPORTED, "cache_append: too large for one launch");
+  AppendArgs a{};
+  const ntk_view* in[3] = {q_heads ? q : k, k, v};
+  bool vec = dim % 8 == 0 && rot % 16 == 0 && whole16(table);
+  for (int i = 0; i < 3; ++i) {
+    a.x[i] = in[i]->data;
+    a.xb[i] = in[i]->stride_batch;
+    a.xs[i] = in[i]->stride_position;
+    a.xh[i] = in[i]->stride_head;
+    vec = vec && view_vec(in[i], e);
+  }
+  if (q_heads) {
+    a.qo = q_out->data;
+    a.qb = q_out->stride_batch;
+    a.qs = q_out->stride_position;
+    a.qh = q_out->stride_head;
+    vec = vec && view_vec(q_out, e);
+  }
+  const ntk_view* cells[2] = {&cache->k, &cache->v};
+  for (int i = 0; i < 2 && cache->pages > 0; ++i) {
+    a.cell[i] = cells[i]->data;
+    a.cb[i] = cells[i]->stride_batch;
+    a.cs[i] = cells[i]->stride_position;
+    a.ch[i] = cells[i]->stride_head;
+    vec = vec && view_vec(cells[i], e4m3 ? 1 : e);
+  }
+  a.scale[0] = e4m3 ? cache->k_scale : nullptr;
+  a.scale[1] = e4m3 ? cache->v_scale : nullptr;
+  a.quantize = e4m3;
+  a.pages = page_table(cache);
+  a.lens = lens;
+  a.news = new_lens;
+  a.positions = positions;
+  a.table = table;
+  a.max_pos = max_pos;
+  a.rot = rot;
+  a.interleaved = interleaved != 0;
+  a.batch = batch;
+  a.length = length;
+  a.heads = q_heads;
+  a.kv_heads = kv;
+  a.dim = dim;
+  const long long blocks = append_blocks(a);
+  if (blocks == 0) return NTK_OK;
+  if (!grid_ok(blocks, 256) || (long long)batch * append_pages(length, a.pages.shift) >= (1LL << 31))
+    return bad(NTK_E_UNSUPPORTED, "cache_append: too large for one launch");
+  const hipError_t err = launch_append((hipStream_t)hip_stream, dtype, a, vec);
+  return err == hipSuccess ? NTK_OK : hip_bad(err);
+}
+
+namespace {
+
+int cached_args(const ntk_attention_desc* d, int cells, AttnPlan* plan) {
+  if (!d) return bad(NTK_E_ARG, "attention_cached: the descriptor is NULL");
+  if (cells != NTK_E4M3 && cells != d->dtype) return bad(NTK_E_ARG, "attention_cached: the cache's dtype is the call's or NTK_E4M3");
+  if (d->prefix || d->docs) return bad(NTK_E_ARG, "attention_cached: prefix and docs must be NULL");
+  return attn_args(d, plan, false, cells);
+}
+
+}  // namespace
+
+extern "C" long long ntk_attention_cached_workspace(const ntk_attention_desc* desc, int cache_dtype) {
+  AttnPlan plan;
+  if (int rc = cached_args(desc, cache_dtype, &plan)) return rc;
+  return (plan.part_floats + plan.flag_ints) * 4;
+}
+
+extern "C" int ntk_attention_cached(const ntk_attention_desc* desc, const ntk_cache* cache, const int* q_lens, const ntk_view* q,
+                                    const ntk_view* o, float* lse, void* workspace, long long workspace_bytes, void* hip_stream) {
+  AttnPlan plan;
+  if (!cache) return bad(NTK_E_ARG, "attention_cached: the cache is NULL");
+  if (int rc = cached_args(desc, cache->dtype, &plan)) return rc;
+  if (int rc = cache_args(cache, desc->dtype, desc->batch, "attention_cached")) return rc;
+  if (cache->kv_heads != desc->kv_heads || cache->head_dim != desc->head_dim || (long long)cache->max_pages * cache->page_size != desc->k_len)
+    return bad(NTK_E_SHAPE, "attention_cached: kv_heads, head_dim or k_len is not the cache's");
+  if (desc->batch == 0 || desc->q_len == 0) return NTK_OK;
+  const bool e4m3 = cache->dtype == NTK_E4M3;
+  const int e = elem(desc->dtype);
+  if (!view_ok(q, e) || !view_ok(o, e)) return bad(NTK_E_ARG, "attention_cached: a view is missing, unaligned or has a negative stride");
+  if (!desc->k_lens || !aligned(desc->k_lens, 4) || !aligned(q_lens, 4) || !aligned(lse, 4) || !aligned(desc->slopes, 4))
+    return bad(NTK_E_ARG, "attention_cached: k_lens is NULL, or a pointer is not aligned to its type");
+  const long long need = (plan.part_floats + plan.flag_ints) * 4;
+  if (need && (!workspace || !whole16(workspace) || workspace_bytes < need))
+    return bad(NTK_E_ARG, "attention_cached: the workspace is missing, unaligned or too small");
+  if (!apart(o, desc->batch, desc->q_len, desc->heads, desc->head_dim) || same_place(o, q) ||
+      (cache->pages > 0 && (same_place(o, &cache->k) || same_place(o, &cache->v))))
+    return bad(NTK_E_ARG, "attention_cached: o overlaps itself, q or the cache");
+  CachedArgs a{};
+  set_desc(a, desc);
+  set_view(a.q, q);
+  set_view(a.o, o);
+  bool vec = desc->head_dim * (e4m3 ? 1 : e) % 16 == 0 && view_vec(q, e) && view_vec(o, e);
+  if (cache->pages > 0) {
+    set_view(a.k, &cache->k);
+    set_view(a.v, &cache->v);
+    vec = vec && view_vec(&cache->k, e4m3 ? 1 : e) && view_vec(&cache->v, e4m3 ? 1 : e);
+  }
+  a.k_scale = cache->k_scale;
+  a.v_scale = cache->v_scale;
+  a.q_lens = q_lens;
+  a.pages = page_table(cache);
+  a.lse = lse;
+  a.part = (float*)workspace;
+  a.flags = (int*)workspace + plan.part_floats;
+  a.tiles = plan.tiles;
+  a.splits = plan.splits;
+  const hipError_t err = e4m3 ? launch_attn_cached_e4m3((hipStream_t)hip_stream, desc->dtype, a, plan.tokens, vec)
+                              : launch_attn_cached((hipStream_t)hip_stream, desc->dtype, a, plan.tokens, vec);
+  return err == hipSuccess ? NTK_OK : hip_bad(err);
+}
+
+extern "C" long long ntk_logprobs_workspace(int dtype, long long rows, int vocab, int top) {
+  if (int rc = logprob_args(dtype, rows, vocab, top)) return rc;
+  return logprob_work_bytes(rows, top, logprob_splits(dtype, rows, vocab));
+}
+
+extern "C" int ntk_logprobs(int dtype, long long rows, int vocab, const void* logits, long long stride, const int* tokens, float scale,
+                            int top, float* logp, float* entropy, float* lse, float* top_logp, int* top_tokens, void* workspace,
+                            long long workspace_bytes, void* hip_stream) {
+  if (int rc = logprob_args(dtype, rows, vocab, top)) return rc;
+  if (!(scale > 0.f) || !isfinite(scale * kLog2e)) return bad(NTK_E_ARG, "logprobs: scale must be positive and finite");
+  if (rows == 0) return NTK_OK;
+  if (!logits || !tokens || !logp || (top && (!top_logp || !top_tokens))) return bad(NTK_E_ARG, "logprobs: an array is NULL");
+  if (stride < vocab) return bad(NTK_E_ARG, "logprobs: the row stride is below vocab");
+  for (const void* p : {(const void*)tokens, (const void*)logp, (const void*)entropy, (const void*)lse, (const void*)top_logp, (const void*)top_tokens})
+    if (!aligned(p, 4)) return bad(NTK_E_ARG, "logprobs: a pointer is not aligned to its type");
+  if (!aligned(logits, elem(dtype))) return bad(NTK_E_ARG, "logprobs: a pointer is not aligned to its type");
+  LogprobArgs a{logits, stride, tokens, logp, entropy, lse, top_logp, top_tokens, workspace, rows, vocab, top,
+                logprob_splits(dtype, rows, vocab), scale};
+  const long long need = logprob_work_bytes(rows, top, a.splits);
+  if (need && (!workspace || !whole16(workspace) || workspace_bytes < need))
+    return bad(NTK_E_ARG, "logprobs: the workspace is missing, unaligned or too small");
+  const hipError_t err = launch_logprobs((hipStream_t)hip_stream, dtype, a);
+  return err == hipSuccess ? NTK_OK : hip_bad(err);
+}
+
+extern "C" int ntk_logprobs_bwd(int dtype, long long rows, int vocab, const void* logits, long long stride, const int* tokens,
+                                float scale, const float* lse, const float* entropy, const float* dlogp, const float* dentropy,
+                                void* dlogits, long long dlogits_stride, void* hip_stream) {
+  if (int rc = logprob_args(dtype, rows, vocab, 0)) return rc;
+  if (!(scale > 0.f) || !isfinite(scale * kLog2e)) return bad(NTK_E_ARG, "logprobs_bwd: scale must be positive and finite");
+  if (rows == 0) return NTK_OK;
+  if (!logits || !tokens || !lse || (dentropy && !entropy) || !dlogits) return bad(NTK_E_ARG, "logprobs_bwd: an array is NULL");
+  if (stride < vocab || dlogits_stride < vocab) return bad(NTK_E_ARG, "logprobs_bwd: a row stride is below vocab");
+  if (dlogits == logits && dlogits_stride != stride) return bad(NTK_E_ARG, "logprobs_bwd: in place, the strides have to agree");
+  for (const void* p : {(const void*)tokens, (const void*)lse, (const void*)entropy, (const void*)dlogp, (const void*)dentropy})
+    if (!aligned(p, 4)) return bad(NTK_E_ARG, "logprobs_bwd: a pointer is not aligned to its type");
+  if (!aligned(logits, elem(dtype)) || !aligned(dlogits, elem(dtype))) return bad(NTK_E_ARG, "logprobs_bwd: a pointer is not aligned to its type");
+  LogprobBwdArgs a{logits, dlogits, stride, dlogits_stride, tokens, lse, entropy, dlogp, dentropy, rows, vocab,
+                   logprob_bwd_chunks(dtype, vocab), scale};
+  const hipError_t err = launch_logprobs_bwd((hipStream_t)hip_stream, dtype, a);
   return err == hipSuccess ? NTK_OK : hip_bad(err);
 }

@@ -1,10 +1,17 @@
-"""Operators of a sequence model's block: root-mean-square norm, rotary positions, attention.
+"""Operators of a sequence model's block: root-mean-square norm, rotary positions, attention; and of its answers.
 
     h = seq.rms_norm(x, weight)                                    # or (y, h) with residual=
     q, k = seq.rotary(q, table, positions, k=k)
     o = seq.attention(q, k, v, causal=True)                        # or one token over a cache: k_lens=
 
-and their gradients (`rms_norm_backward`, `rotary(..., inverse=True)`, `attention_backward`).  Arrays are
+a cache in pages, in the arrays' type or in 8 bits, and the log probabilities of the tokens that come out
+
+    cache = seq.paged_cache(pages, page_size, kv_heads, dim)       # dtype=torch.float8_e4m3fn
+    q = seq.cache_append(cache, page_table, lens, k, v, q=q, table=table)
+    o = seq.attention_cached(q, cache, page_table, lens + 1)
+    logp, entropy, lse, top_logp, top_tokens = seq.token_logprobs(logits, tokens, top=5)
+
+and their gradients (`rms_norm_backward`, `rotary(..., inverse=True)`, `attention_backward`, `token_logprobs_backward`).  Arrays are
 float32, bfloat16 or float16 torch tensors on the GPU; only the last dimension has to be contiguous.  Every
 call enqueues on the current stream, or on `stream`, and returns before the work is done.  As in `ntk`, PyTorch
 supplies device memory and streams only: every step runs in libntk.so (include/ntk_seq.h has the
@@ -18,6 +25,7 @@ from __future__ import annotations
 import contextlib
 import ctypes
 import math
+from typing import NamedTuple, Optional
 
 import torch
 
@@ -371,3 +379,234 @@ def attention_backward(do, q, k, v, o, lse, causal=False, softcap=0.0, scale=Non
     if _recording() and _wanted(do, q, k, v, o, lse, slopes):
         return _unrecorded("attention_backward", "not defined", (do, q, k, v, o, lse, slopes), dq, dk, dv)
     return dq, dk, dv
+
+
+# ---- a cache in pages ---------------------------------------------------------------------------------------
+
+class PagedCache(NamedTuple):
+    """Keys and values [pages, page_size, kv_heads, dim], only the last dimension contiguous; in float8_e4m3fn under a power of
+    two a page and head in k_scale and v_scale [pages, kv_heads]."""
+    k: torch.Tensor
+    v: torch.Tensor
+    k_scale: Optional[torch.Tensor] = None
+    v_scale: Optional[torch.Tensor] = None
+
+
+_E4M3 = torch.float8_e4m3fn
+
+
+def paged_cache(pages, page_size, kv_heads, dim, dtype=torch.bfloat16, device=None):
+    """A cache of zeros.  Each head's part of a page lies in one piece, which is what `attention_cached` reads in whole lines."""
+    if dtype not in _DTYPES and dtype != _E4M3:
+        raise TypeError("dtype must be float32, bfloat16, float16 or float8_e4m3fn")
+    if min(pages, kv_heads, dim) < 1 or not 1 <= page_size <= 1024 or page_size & (page_size - 1):
+        raise ValueError("paged_cache: a size is below 1, or page_size is no power of two up to 1024")
+    dev = _gpu(device)
+    k, v = (torch.zeros((pages, kv_heads, page_size, dim), dtype=torch.uint8 if dtype == _E4M3 else dtype, device=dev) for _ in range(2))
+    if dtype != _E4M3:
+        return PagedCache(k.transpose(1, 2), v.transpose(1, 2))
+    scales = (torch.full((pages, kv_heads), 2.0 ** -126, dtype=torch.float32, device=dev) for _ in range(2))
+    return PagedCache(k.view(_E4M3).transpose(1, 2), v.view(_E4M3).transpose(1, 2), *scales)
+
+
+def _ints(t, name, device, shape):
+    if t is not None:
+        _check(t, name, torch.int32, device=device, shape=shape)
+        if not t.is_contiguous():
+            raise ValueError(f"{name} must be contiguous")
+
+
+def _cache(cache, page_table, dtype, device, batch):
+    """The cache and its table as an ntk_cache."""
+    k, v, k_scale, v_scale = cache
+    cells = k.dtype if isinstance(k, torch.Tensor) else None
+    if cells not in (dtype, _E4M3):
+        raise TypeError(f"the cache must be of type {dtype} or {_E4M3}")
+    _check(k, "cache.k", cells, ndim=4, device=device)
+    _check(v, "cache.v", cells, device=device, shape=k.shape)
+    pages, size, heads, dim = k.shape
+    if cells == _E4M3:
+        for name, t in (("cache.k_scale", k_scale), ("cache.v_scale", v_scale)):
+            _check(t, name, torch.float32, device=device, shape=(pages, heads))
+            if not t.is_contiguous():
+                raise ValueError(f"{name} must be contiguous")
+    elif k_scale is not None or v_scale is not None:
+        raise ValueError(f"a cache of type {dtype} has no scales")
+    _check(page_table, "page_table", torch.int32, ndim=2, device=device)
+    if page_table.shape[0] != batch or not page_table.is_contiguous():
+        raise ValueError(f"page_table must be a contiguous [{batch}, max_pages] tensor")
+    _sizes(pages, size, heads, dim, page_table.shape[1])
+
+    def view(t):
+        return _lib.ntk_view(t.data_ptr(), *(t.stride(i) if t.shape[i] > 1 else 0 for i in range(3)))
+
+    return _lib.ntk_cache(_lib.NTK_E4M3 if cells == _E4M3 else _DTYPES[cells], pages, size, heads, dim, view(k), view(v),
+                          _ptr(k_scale), _ptr(v_scale), page_table.data_ptr(), page_table.shape[1])
+
+
+def cache_append(cache, page_table, lens, k, v, q=None, table=None, positions=None, new_lens=None, interleaved=False, stream=None):
+    """Appends new tokens' k and v [batch, length, kv_heads, dim] to sequences that hold lens[b] (int32 [batch]): token i < new_lens[b]
+    (all of them without new_lens) goes to place lens[b] + i, which lies in page page_table[b, place // page_size] (int32 [batch,
+    max_pages]).  With `table`, k turns as in `rotary` to its place (or to positions, int32 [batch, length]).  Returns q
+    [batch, length, heads, dim] turned alike, with zeros past new_lens, or None without q.  `lens` stays as it is.  Tokens
+    whose place the table or the cache does not have are dropped.  See include/ntk_seq.h for how a cache in 8 bits is rounded."""
+    lib = _lib.load()
+    _check(k, "k", ndim=4)
+    b, n, heads, dim = k.shape
+    dev = k.device
+    _check(v, "v", k.dtype, device=dev, shape=k.shape)
+    if q is not None:
+        _check(q, "q", k.dtype, device=dev, shape=(b, n, q.shape[2] if q.dim() == 4 else -1, dim))
+    _sizes(b, n, heads, 0 if q is None else q.shape[2])
+    if table is not None:
+        _check(table, "table", torch.float32, ndim=3, device=dev)
+        if not table.is_contiguous() or table.shape[2] != 2:
+            raise ValueError("table must be a contiguous [max_pos, rot / 2, 2] tensor")
+        _sizes(table.shape[0], 2 * table.shape[1])
+    elif positions is not None:
+        raise ValueError("positions need a table")
+    _ints(lens, "lens", dev, (b,))
+    if lens is None:
+        raise TypeError("lens must be a GPU tensor of type int32")
+    _ints(new_lens, "new_lens", dev, (b,))
+    _ints(positions, "positions", dev, (b, n))
+    desc = _cache(cache, page_table, k.dtype, dev, b)
+    if (desc.kv_heads, desc.head_dim) != (heads, dim):
+        raise ValueError(f"the cache holds {desc.kv_heads} heads of {desc.head_dim}, k has {heads} of {dim}")
+    _written("cache_append", (k, v, table), *cache)
+    with _Call(k, stream, (k, v, q, table, positions, lens, new_lens, page_table, *cache)) as call:
+        qo = None if q is None else _like(q)
+        kv, vv, qv, qov = _views(k, v, q, qo)
+        _lib.check(lib.ntk_cache_append(_DTYPES[k.dtype], b, n, 0 if q is None else q.shape[2], ctypes.byref(desc), _ptr(lens),
+                                        _ptr(new_lens), kv, vv, qv, qov, _ptr(table), 0 if table is None else table.shape[0],
+                                        0 if table is None else 2 * table.shape[1], int(interleaved), _ptr(positions), call.handle))
+    if q is not None and _recording() and _wanted(q):
+        return _unrecorded("cache_append", "not defined", (q,), qo)[0]
+    return qo
+
+
+def attention_cached(q, cache, page_table, k_lens, q_lens=None, causal=True, softcap=0.0, scale=None, slopes=None,
+                     return_lse=False, out=None, stream=None):
+    """`attention` of q [batch, q_len, heads, dim] over a cache of which sequence b fills k_lens[b] places (int32 [batch], the
+    queries' own tokens among them).  Queries i < q_lens[b] (all of them without q_lens) are its last ones; the rows of o past them
+    are zeros.  Returns o like q, or (o, lse).  It has no backward pass."""
+    lib = _lib.load()
+    _check(q, "q", ndim=4)
+    b, sq, heads, dim = q.shape
+    dev = q.device
+    desc = _cache(cache, page_table, q.dtype, dev, b)
+    if desc.head_dim != dim:
+        raise ValueError(f"the cache holds heads of {desc.head_dim}, q has heads of {dim}")
+    _sizes(b, sq, heads, desc.max_pages * desc.page_size)
+    if k_lens is None:
+        raise TypeError("k_lens must be a GPU tensor of type int32")
+    _ints(k_lens, "k_lens", dev, (b,))
+    _ints(q_lens, "q_lens", dev, (b,))
+    if slopes is not None:
+        _check(slopes, "slopes", torch.float32, device=dev, shape=(heads,))
+        if not slopes.is_contiguous():
+            raise ValueError("slopes must be contiguous")
+    if out is not None:
+        _check(out, "out", q.dtype, device=dev, shape=q.shape)
+        _written("attention_cached(out=)", (q, slopes, *cache), out)
+    scores = _lib.ntk_attention_desc(_DTYPES[q.dtype], b, sq, desc.max_pages * desc.page_size, heads, desc.kv_heads, dim, 1 if causal else 0,
+                                     1.0 / math.sqrt(max(dim, 1)) if scale is None else scale, softcap, _ptr(k_lens), None, None, _ptr(slopes))
+    with _Call(q, stream, (q, k_lens, q_lens, slopes, out, page_table, *cache)) as call:
+        o = _like(q) if out is None else out
+        lse = torch.empty((b, heads, sq), dtype=torch.float32, device=dev) if return_lse else None
+        need = lib.ntk_attention_cached_workspace(ctypes.byref(scores), desc.dtype)
+        if need < 0:
+            _lib.check(need)
+        work = torch.empty(need, dtype=torch.uint8, device=dev) if need else None
+        _lib.check(lib.ntk_attention_cached(ctypes.byref(scores), ctypes.byref(desc), _ptr(q_lens), *_views(q, o), _ptr(lse), _ptr(work),
+                                            need, call.handle))
+    if out is None and _recording() and _wanted(q, slopes, *cache):
+        o, lse = _unrecorded("attention_cached", "not defined", (q, slopes, *cache), o, lse)
+    return (o, lse) if return_lse else o
+
+
+# ---- log probabilities of given tokens ----------------------------------------------------------------------
+
+class TokenLogprobs(NamedTuple):
+    """logp and entropy [...] float32; lse [..., 2] float32: the largest logit m and log sum exp(scale (logits - m)); top_logp float32 and
+    top_tokens int32 [..., top], None where none were asked for."""
+    logp: torch.Tensor
+    entropy: torch.Tensor
+    lse: torch.Tensor
+    top_logp: Optional[torch.Tensor] = None
+    top_tokens: Optional[torch.Tensor] = None
+
+
+def _per_row(t, name, dtype, logits, each=()):
+    """One number (or `each` of them) a row, at any strides: contiguous, or None."""
+    if t is None:
+        return None
+    if not isinstance(t, torch.Tensor) or t.dtype != dtype or not t.is_cuda:
+        raise TypeError(f"{name} must be a GPU tensor of type {dtype}")
+    if t.device != logits.device or t.shape != logits.shape[:-1] + each:
+        raise ValueError(f"{name} is {tuple(t.shape)} on {t.device}, expected {tuple(logits.shape[:-1] + each)} on {logits.device}")
+    return t.contiguous()
+
+
+def _logits(logits):
+    _check(logits, "logits")
+    if logits.dim() < 1 or logits.shape[-1] < 1:
+        raise ValueError("logits need a last dimension of at least 1")
+    _sizes(logits.shape[-1])
+
+
+def token_logprobs(logits, tokens, top=0, scale=1.0, stream=None):
+    """TokenLogprobs of the rows of logits [..., vocab]: the log probability of tokens (int32 [...]; 0 for a negative one), the
+    entropy, the parts of log sum exp, and the `top` most likely tokens with their log probabilities, the lower token first among equal
+    logits.  Probabilities are softmax(scale * logits); logits of -inf are tokens that are ruled out."""
+    lib = _lib.load()
+    _logits(logits)
+    lead, vocab = logits.shape[:-1], logits.shape[-1]
+    if tokens is None:
+        raise TypeError("tokens must be a GPU tensor of type int32")
+    if not 0 <= top <= min(vocab, 64):
+        raise ValueError(f"top must be between 0 and {min(vocab, 64)}")
+    with _Call(logits, stream, (logits, tokens)) as call:
+        x, stride = _rows(logits)
+        rows = x.shape[0]
+        t = _per_row(tokens, "tokens", torch.int32, logits)
+        logp, entropy = (torch.empty(lead, dtype=torch.float32, device=logits.device) for _ in range(2))
+        lse = torch.empty((*lead, 2), dtype=torch.float32, device=logits.device)
+        top_logp = torch.empty((*lead, top), dtype=torch.float32, device=logits.device) if top else None
+        top_tokens = torch.empty((*lead, top), dtype=torch.int32, device=logits.device) if top else None
+        need = lib.ntk_logprobs_workspace(_DTYPES[x.dtype], rows, vocab, top)
+        if need < 0:
+            _lib.check(need)
+        work = torch.empty(need, dtype=torch.uint8, device=logits.device) if need else None
+        _lib.check(lib.ntk_logprobs(_DTYPES[x.dtype], rows, vocab, _ptr(x), stride, _ptr(t), scale, top, _ptr(logp), _ptr(entropy), _ptr(lse),
+                                    _ptr(top_logp), _ptr(top_tokens), _ptr(work), need, call.handle))
+    if _recording() and _wanted(logits):
+        logp, entropy, lse, top_logp = _unrecorded("token_logprobs", "token_logprobs_backward", (logits,), logp, entropy, lse, top_logp)
+    return TokenLogprobs(logp, entropy, lse, top_logp, top_tokens)
+
+
+def token_logprobs_backward(dlogp, dentropy, logits, tokens, lse, entropy, scale=1.0, inplace=False, stream=None):
+    """The gradient of the logits from those of logp and entropy (float32 [...], either may be None), with the lse and entropy that
+    `token_logprobs` returned.  `inplace` writes it over the logits."""
+    lib = _lib.load()
+    _logits(logits)
+    vocab = logits.shape[-1]
+    for name, t in (("tokens", tokens), ("lse", lse), ("entropy", entropy)):
+        if t is None:
+            raise TypeError(f"{name} must be a GPU tensor")
+    if inplace:
+        _written("token_logprobs_backward", (dlogp, dentropy), logits)
+    with _Call(logits, stream, (dlogp, dentropy, logits, tokens, lse, entropy)) as call:
+        x, stride = _rows(logits)
+        if inplace and x.data_ptr() != logits.data_ptr():
+            raise ValueError("inplace needs logits whose rows are evenly spaced and apart")
+        t = _per_row(tokens, "tokens", torch.int32, logits)
+        lse = _per_row(lse, "lse", torch.float32, logits, (2,))
+        entropy, dlogp, dentropy = (_per_row(d, name, torch.float32, logits) for name, d in (
+            ("entropy", entropy), ("dlogp", dlogp), ("dentropy", dentropy)))
+        out, out_stride = (logits, stride) if inplace else (_like(logits), vocab)
+        _lib.check(lib.ntk_logprobs_bwd(_DTYPES[x.dtype], x.shape[0], vocab, _ptr(x), stride, _ptr(t), scale, _ptr(lse), _ptr(entropy),
+                                        _ptr(dlogp), _ptr(dentropy), _ptr(out), out_stride, call.handle))
+    if not inplace and _recording() and _wanted(dlogp, dentropy, logits, lse, entropy):
+        return _unrecorded("token_logprobs_backward", "not defined", (dlogp, dentropy, logits, lse, entropy), out)[0]
+    return out
