@@ -154,7 +154,7 @@ int ntk_attention_bwd(const ntk_attention_desc* desc, const ntk_view* dout, cons
  *                            read in whole lines.
  *   k_scale, v_scale         [pages, kv_heads] fp32 contiguous, NTK_E4M3 only: the cells of a page and head stand for their values
  *                            times it.  Always a power of two from 2^-126 on, as ntk_cache_append leaves it.
- *   page_size                a power of two from 1 to 1024.
+ *   page_size                a power of two from 8 to 1024.
  *   page_table               [batch, max_pages] int32.  Entries past a sequence's places are not used and may hold anything. */
 typedef struct ntk_cache {
     int dtype, pages, page_size, kv_heads, head_dim;

@@ -23,6 +23,7 @@ namespace {
 
 __device__ const uint4 kZeros = {0, 0, 0, 0};
 __device__ const uint4 kNaNs = {~0u, ~0u, ~0u, ~0u};   // NaN in every type, e4m3 among them
+__device__ const float kOne = 1.f;
 
 // What a batch entry's queries see, as AttnScope: its first `queries` rows are the last of its `len` positions.
 struct CachedScope {
@@ -41,6 +42,11 @@ struct CachedScope {
   __device__ __forceinline__ int all(int i0, int i1) const { return min(klim(i0), klim(i1)); }
   __device__ __forceinline__ int any(int i0, int i1) const { return i0 < queries ? klim(min(i1, queries - 1)) : 0; }
 };
+
+// Loads through addresses that were selected: said to be global memory, since a flat load's wait is one for LDS too.
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+__device__ __forceinline__ u32x4 load16(const void* p) { return *(const __attribute__((address_space(1))) u32x4*)p; }
+__device__ __forceinline__ float load_float(const float* p) { return *(const __attribute__((address_space(1))) float*)p; }
 
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
@@ -61,100 +67,113 @@ __device__ __forceinline__ void from_e4m3(uint32_t w, float s, T (&y)[4]) {
   }
 }
 
-// ROWS positions of one head into an LDS tile of AttnTile's layout, by WAVES waves.  A lane's `NI` chunks of 16 bytes (of the cache)
-// lie in rows of the tile that do not change, so their pages are looked up one tile ahead (look).
+// ROWS positions of one head into an LDS tile of AttnTile's layout, by WAVES waves, 64 chunks of 16 bytes an instruction.  Pages
+// hold at least 8 places and tiles start on multiples of 32, so 8 rows from a multiple of 8 lie in one page: a page's number
+// is the same for a whole wave, and addresses are a scalar base and a lane's offset.  Nothing here waits for a load but for the
+// one that look() made a tile before (branches on fresh entries, and flat loads, whose waits are LDS waits too, cost 832 us where this form takes 179: 32 sequences
+// of up to 32768 places in 8 bits, 4 heads of 128).
 template <class T, int DP, int ROWS, int WAVES, bool VEC, bool E4M3>
 struct PageLoad {
   using Tile = AttnTile<T, DP>;
   static constexpr int CE = E4M3 ? 1 : (int)sizeof(T);           // bytes an element of the cache
   static constexpr int CH = DP * CE / 16, EC = 16 / CE;         // chunks a row, elements a chunk
+  static constexpr int RPI = 64 / CH;                           // rows an instruction: at most 16
   static constexpr int BYTES = ROWS * Tile::RB;
   static constexpr int NI = (ROWS * CH + 64 * WAVES - 1) / (64 * WAVES);
-  static constexpr bool EVEN = NI * 64 * WAVES == ROWS * CH;    // else some lanes have none (row >= ROWS)
-  static_assert(EVEN || E4M3, "chunks split over the lanes");
-  struct Where {
-    int page[NI];                          // -1: none, -2: past the end
-  };
-  struct Held {                            // 8 bits: a tile on its way
-    uint4 x[NI];
-    float s[NI];
-  };
-  __device__ static __forceinline__ void place(int i, int wave, int lane, int& row, int& chunk) {
-    const int o = (i * WAVES + wave) * 64 + lane;
-    row = o / CH;
-    chunk = o % CH;
-    if constexpr (!E4M3) chunk ^= Tile::swz(row);               // straight into LDS: lane l's 16 bytes go to place l
+  static constexpr bool EVEN = NI * 64 * WAVES == ROWS * CH;    // else some waves have none (rows >= ROWS)
+  static_assert((EVEN || E4M3) && RPI <= 16, "chunks split over the lanes");
+
+  // lane l: the table's entry for the rows 8 (l % (ROWS / 8)) .. + 7 of a tile
+  __device__ static __forceinline__ int look(const CachedArgs& a, int b, int tile0, int lane) {
+    const int e = min((tile0 + 8 * (lane & (ROWS / 8 - 1))) >> a.pages.shift, a.pages.most - 1);
+    return a.pages.table[(long long)b * a.pages.most + e];
   }
-  __device__ static __forceinline__ void look(const CachedArgs& a, int b, int tile0, int len, int wave, int lane, Where& w) {
+  // instruction i's first row
+  __device__ static __forceinline__ int first(int i, int wave) { return (i * WAVES + wave) * RPI; }
+  // the entry (or its scale) of a lane's row
+  __device__ static __forceinline__ int of_row(int entries, int row0, int lane) {
+    const int lo = __builtin_amdgcn_readlane(entries, row0 / 8);
+    if constexpr (RPI <= 8) return lo;
+    return lane < 32 ? lo : __builtin_amdgcn_readlane(entries, row0 / 8 + 1);
+  }
+  // where a lane's chunk of instruction i is read; `there`: it is the cache's
+  __device__ static __forceinline__ const char* source(const CachedArgs& a, const AttnView& v, int hk, int tile0, int len, int entries, int i,
+                                                       int wave, int lane, int& c, bool& there) {
+    const int row0 = first(i, wave), lr = lane / CH, row = row0 + lr;
+    c = lane % CH;
+    if constexpr (!E4M3) c ^= Tile::swz(row);                   // straight into LDS: lane l's 16 bytes go to place l
+    const int id = of_row(entries, row0, lane);
+    const bool in = (unsigned)id < (unsigned)a.pages.pages;
+    const int group = RPI <= 8 ? row0 : row0 + (lr & 8);
+    const char* base = (const char*)v.p + ((long long)(in ? id : 0) * v.sb + (long long)a.pages.slot(tile0 + group) * v.ss + (long long)hk * v.sh) * CE;
+    const bool live = tile0 + row < len && (EVEN || row < ROWS);
+    there = live && in && c * EC < a.D;
+    const uint32_t off = (uint32_t)(row - group) * (uint32_t)v.ss * CE + (uint32_t)c * 16;   // rows that are not there: unused
+    const char* none = live && !in ? (const char*)&kNaNs : (const char*)&kZeros;
+    if constexpr (VEC) return there ? base + off : none;
+    return there ? base + (long long)(row - group) * v.ss * CE : none;
+  }
+  // 16 bytes of a chunk that need not be aligned
+  __device__ static __forceinline__ u32x4 gather(const char* from, bool there, int c, int D) {
+    if (!there) return load16(from);
+    if constexpr (!E4M3) return __builtin_bit_cast(u32x4, load_chunk_elems((const T*)from, c * EC, D));
+    u32x4 u = {0, 0, 0, 0};
 #pragma unroll
-    for (int i = 0; i < NI; ++i) {
-      int row, c;
-      place(i, wave, lane, row, c);
-      w.page[i] = tile0 + row < len && (EVEN || row < ROWS) ? a.pages.page(b, tile0 + row) : -2;
-    }
-  }
-  __device__ static __forceinline__ const char* at(const AttnView& v, const PageTable& t, int hk, int pos, int page) {
-    return (const char*)v.p + ((long long)page * v.sb + (long long)t.slot(pos) * v.ss + (long long)hk * v.sh) * CE;
+    for (int k = 0; k < 16; ++k)
+      if (c * EC + k < D) u[k / 4] |= (uint32_t)(uint8_t)from[c * EC + k] << (8 * (k % 4));
+    return u;
   }
   // the cache in the queries' type: into LDS
-  __device__ static __forceinline__ void rows(const CachedArgs& a, const AttnView& v, int hk, int tile0, const Where& w, char* lds, int wave,
+  __device__ static __forceinline__ void rows(const CachedArgs& a, const AttnView& v, int hk, int tile0, int len, int entries, char* lds, int wave,
                                               int lane) {
     static_assert(!E4M3, "");
 #pragma unroll
     for (int i = 0; i < NI; ++i) {
-      int row, c;
-      place(i, wave, lane, row, c);
-      const int page = w.page[i];
-      const char* p = at(v, a.pages, hk, tile0 + row, max(page, 0));
+      int c;
+      bool there;
+      const char* from = source(a, v, hk, tile0, len, entries, i, wave, lane, c, there);
+      char* to = lds + __builtin_amdgcn_readfirstlane((i * WAVES + wave) * 1024);
       if constexpr (VEC) {
-        const char* from = page >= 0 && c * EC < a.D ? p + c * 16 : page == -1 ? (const char*)&kNaNs : (const char*)&kZeros;
         typedef const __attribute__((address_space(1))) void G;
         typedef __attribute__((address_space(3))) void L;
-        __builtin_amdgcn_global_load_lds((G*)from, (L*)(lds + __builtin_amdgcn_readfirstlane((i * WAVES + wave) * 1024)), 16, 0, 0);
+        __builtin_amdgcn_global_load_lds((G*)from, (L*)to, 16, 0, 0);
       } else {
-        uint4 u = page == -1 ? kNaNs : kZeros;
-        if (page >= 0) u = load_chunk_elems((const T*)p, c * EC, a.D);
-        *reinterpret_cast<uint4*>(lds + ((i * WAVES + wave) * 64 + lane) * 16) = u;
+        *reinterpret_cast<u32x4*>(to + lane * 16) = gather(from, there, c, a.D);
       }
     }
   }
   // the cache in 8 bits: into registers, and from there into LDS
-  __device__ static __forceinline__ void fetch(const CachedArgs& a, const AttnView& v, const float* scale, int hk, int tile0, const Where& w,
+  struct Held {
+    u32x4 x[NI];
+    float s;                               // lane l: the scale of the rows that look() takes for it
+  };
+  __device__ static __forceinline__ void fetch(const CachedArgs& a, const AttnView& v, const float* scale, int hk, int tile0, int len, int entries,
                                                int wave, int lane, Held& h) {
+    const bool in = (unsigned)entries < (unsigned)a.pages.pages && tile0 + 8 * (lane & (ROWS / 8 - 1)) < len;
+    h.s = load_float(in ? scale + ((long long)entries * a.Hk + hk) : &kOne);
 #pragma unroll
     for (int i = 0; i < NI; ++i) {
-      int row, c;
-      place(i, wave, lane, row, c);
-      const int page = w.page[i];
-      const char* p = at(v, a.pages, hk, tile0 + row, max(page, 0));
-      h.s[i] = page >= 0 ? scale[(long long)page * a.Hk + hk] : 1.f;
-      if constexpr (VEC) {
-        const char* from = page >= 0 && c * EC < a.D ? p + c * 16 : page == -1 ? (const char*)&kNaNs : (const char*)&kZeros;
-        h.x[i] = *reinterpret_cast<const uint4*>(from);
-      } else {
-        uint32_t u[4] = {0, 0, 0, 0};
-        if (page == -1) u[0] = u[1] = u[2] = u[3] = ~0u;
-        if (page >= 0)
-#pragma unroll
-          for (int k = 0; k < 16; ++k)
-            if (c * EC + k < a.D) u[k / 4] |= (uint32_t)(uint8_t)p[c * EC + k] << (8 * (k % 4));
-        h.x[i] = make_uint4(u[0], u[1], u[2], u[3]);
-      }
+      int c;
+      bool there;
+      const char* from = source(a, v, hk, tile0, len, entries, i, wave, lane, c, there);
+      if constexpr (VEC)
+        h.x[i] = load16(from);
+      else
+        h.x[i] = gather(from, there, c, a.D);
     }
   }
   __device__ static __forceinline__ void put(const Held& h, char* lds, int wave, int lane) {
     constexpr int TC = (int)sizeof(T);     // chunks of the tile that a chunk of the cache becomes
 #pragma unroll
     for (int i = 0; i < NI; ++i) {
-      int row, c;
-      place(i, wave, lane, row, c);
+      const int row = first(i, wave) + lane / CH, c = lane % CH;
       if (!EVEN && row >= ROWS) continue;
-      const uint32_t w[4] = {h.x[i].x, h.x[i].y, h.x[i].z, h.x[i].w};
+      const float s = __int_as_float(of_row(__float_as_int(h.s), first(i, wave), lane));
       alignas(16) T e[16];
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
         T y[4];
-        from_e4m3<T>(w[k], h.s[i], y);
+        from_e4m3<T>(h.x[i][k], s, y);
 #pragma unroll
         for (int n = 0; n < 4; ++n) e[4 * k + n] = y[n];
       }
@@ -202,48 +221,42 @@ __device__ __forceinline__ bool cached_body(const CachedArgs& a, char* smem, int
 
   auto pass = [&](auto careful) {
     w.reset();
-    typename Load::Where where;
+    int entries = 0;                           // of the tile that is read next
     if constexpr (!E4M3) {
       auto issue = [&](int t, int st) {
-        Load::rows(a, a.k, hk, t * BN, where, sk + st * Load::BYTES, wave, lane);
-        Load::rows(a, a.v, hk, t * BN, where, sv + st * Load::BYTES, wave, lane);
+        Load::rows(a, a.k, hk, t * BN, sc.len, entries, sk + st * Load::BYTES, wave, lane);
+        Load::rows(a, a.v, hk, t * BN, sc.len, entries, sv + st * Load::BYTES, wave, lane);
+        entries = Load::look(a, b, (t + 1) * BN, lane);
       };
       if (t0 < t1) {
-        Load::look(a, b, t0 * BN, sc.len, wave, lane, where);
+        entries = Load::look(a, b, t0 * BN, lane);
         issue(t0, 0);
-        Load::look(a, b, (t0 + 1) * BN, sc.len, wave, lane, where);
       }
       for (int t = t0, st = 0; t < t1; ++t, st ^= 1) {
         __builtin_amdgcn_s_waitcnt(0x0070);   // this wave's part of the tile has landed, and its LDS reads are done
         __syncthreads();
-        if (t + 1 < t1) {
-          issue(t + 1, st ^ 1);
-          Load::look(a, b, (t + 2) * BN, sc.len, wave, lane, where);
-        }
+        if (t + 1 < t1) issue(t + 1, st ^ 1);
         w.template tile<BN / 32>(a, sk + st * Load::BYTES, sv + st * Load::BYTES, nullptr, t * BN, (t + 1) * BN > all, careful, lane, tl);
       }
     } else {
-      typename Load::Held hk_, hv_;
+      typename Load::Held kt, vt;
       auto fetch = [&](int t) {
-        Load::fetch(a, a.k, a.k_scale, hk, t * BN, where, wave, lane, hk_);
-        Load::fetch(a, a.v, a.v_scale, hk, t * BN, where, wave, lane, hv_);
+        Load::fetch(a, a.k, a.k_scale, hk, t * BN, sc.len, entries, wave, lane, kt);
+        Load::fetch(a, a.v, a.v_scale, hk, t * BN, sc.len, entries, wave, lane, vt);
+        entries = Load::look(a, b, (t + 1) * BN, lane);
       };
       auto put = [&](int st) {
-        Load::put(hk_, sk + st * Load::BYTES, wave, lane);
-        Load::put(hv_, sv + st * Load::BYTES, wave, lane);
+        Load::put(kt, sk + st * Load::BYTES, wave, lane);
+        Load::put(vt, sv + st * Load::BYTES, wave, lane);
       };
       if (t0 < t1) {
-        Load::look(a, b, t0 * BN, sc.len, wave, lane, where);
+        entries = Load::look(a, b, t0 * BN, lane);
         fetch(t0);
-        Load::look(a, b, (t0 + 1) * BN, sc.len, wave, lane, where);
         put(0);
       }
       for (int t = t0, st = 0; t < t1; ++t, st ^= 1) {
         __syncthreads();                       // tile t is written, and tile t - 1 read
-        if (t + 1 < t1) {
-          fetch(t + 1);
-          Load::look(a, b, (t + 2) * BN, sc.len, wave, lane, where);
-        }
+        if (t + 1 < t1) fetch(t + 1);
         w.template tile<BN / 32>(a, sk + st * Load::BYTES, sv + st * Load::BYTES, nullptr, t * BN, (t + 1) * BN > all, careful, lane, tl);
         if (t + 1 < t1) put(st ^ 1);
       }
@@ -297,18 +310,18 @@ __device__ __forceinline__ bool cached_tokens_body(const CachedArgs& a, char* sm
 
   auto pass = [&](auto careful) {
     w.reset();
-    typename Load::Where where;
+    int entries = 0;                           // of the tile that is read next
     int t = t0 + wave;
+    if (t < t1) entries = Load::look(a, b, t * BN, lane);
     if constexpr (!E4M3) {
       auto issue = [&](int t, int st) {
         char* s = mine + st * 2 * Load::BYTES;
-        Load::rows(a, a.k, hk, t * BN, where, s, 0, lane);
-        Load::rows(a, a.v, hk, t * BN, where, s + Load::BYTES, 0, lane);
+        Load::rows(a, a.k, hk, t * BN, sc.len, entries, s, 0, lane);
+        Load::rows(a, a.v, hk, t * BN, sc.len, entries, s + Load::BYTES, 0, lane);
       };
       if (t < t1) {
-        Load::look(a, b, t * BN, sc.len, 0, lane, where);
         issue(t, 0);
-        Load::look(a, b, (t + W) * BN, sc.len, 0, lane, where);
+        entries = Load::look(a, b, (t + W) * BN, lane);
       }
       for (int st = 0; t < t1; t += W, st ^= 1) {
         const bool more = t + W < t1;
@@ -320,7 +333,7 @@ __device__ __forceinline__ bool cached_tokens_body(const CachedArgs& a, char* sm
         }
         __builtin_amdgcn_wave_barrier();
         __builtin_amdgcn_sched_barrier(0);
-        if (VEC && more) Load::look(a, b, (t + 2 * W) * BN, sc.len, 0, lane, where);
+        if (VEC && more) entries = Load::look(a, b, (t + 2 * W) * BN, lane);
         const char* s = mine + st * 2 * Load::BYTES;
         w.template tile<1>(a, s, s + Load::BYTES, nullptr, t * BN, (t + 1) * BN > all, careful, lane, tl);
         __builtin_amdgcn_s_waitcnt(0xC07F);   // this wave's LDS reads are done: the stage may be filled again
@@ -328,26 +341,27 @@ __device__ __forceinline__ bool cached_tokens_body(const CachedArgs& a, char* sm
         __builtin_amdgcn_sched_barrier(0);
         if (!VEC && more) {
           issue(t + W, st ^ 1);
-          Load::look(a, b, (t + 2 * W) * BN, sc.len, 0, lane, where);
+          entries = Load::look(a, b, (t + 2 * W) * BN, lane);
         }
       }
     } else {
-      typename Load::Held kh, vh;
-      auto fetch = [&](int t) {
-        Load::fetch(a, a.k, a.k_scale, hk, t * BN, where, 0, lane, kh);
-        Load::fetch(a, a.v, a.v_scale, hk, t * BN, where, 0, lane, vh);
-      };
+      typename Load::Held kt, vt;
       if (t < t1) {
-        Load::look(a, b, t * BN, sc.len, 0, lane, where);
-        fetch(t);
-        Load::look(a, b, (t + W) * BN, sc.len, 0, lane, where);
+        Load::fetch(a, a.k, a.k_scale, hk, t * BN, sc.len, entries, 0, lane, kt);
+        Load::fetch(a, a.v, a.v_scale, hk, t * BN, sc.len, entries, 0, lane, vt);
+        entries = Load::look(a, b, (t + W) * BN, lane);
       }
       for (; t < t1; t += W) {
-        Load::put(kh, mine, 0, lane);
-        Load::put(vh, mine + Load::BYTES, 0, lane);
-        if (t + W < t1) {
-          fetch(t + W);
-          Load::look(a, b, (t + 2 * W) * BN, sc.len, 0, lane, where);
+        const bool more = t + W < t1;
+        // keys are on their way while values are written, and the other way round
+        Load::put(kt, mine, 0, lane);
+        if (more) {
+          Load::fetch(a, a.k, a.k_scale, hk, (t + W) * BN, sc.len, entries, 0, lane, kt);
+          Load::put(vt, mine + Load::BYTES, 0, lane);
+          Load::fetch(a, a.v, a.v_scale, hk, (t + W) * BN, sc.len, entries, 0, lane, vt);
+          entries = Load::look(a, b, (t + 2 * W) * BN, lane);
+        } else {
+          Load::put(vt, mine + Load::BYTES, 0, lane);
         }
         __builtin_amdgcn_s_waitcnt(0xC07F);   // the tile is written
         __builtin_amdgcn_wave_barrier();
@@ -366,7 +380,7 @@ __device__ __forceinline__ bool cached_tokens_body(const CachedArgs& a, char* sm
   return false;
 }
 template <class T, int DP, bool VEC, bool E4M3>
-__global__ void __launch_bounds__((64 * kCachedWaves<T, DP, E4M3>), 1) k_attn_cached_tokens(const CachedArgs a) {
+__global__ void __launch_bounds__((64 * kCachedWaves<T, DP, E4M3>), (E4M3 && sizeof(T) == 2 ? 2 : 1)) k_attn_cached_tokens(const CachedArgs a) {
   extern __shared__ __align__(1024) char smem[];
   if (cached_tokens_body<T, DP, VEC, E4M3, false>(a, smem)) cached_tokens_body<T, DP, VEC, E4M3, true>(a, smem);
 }

@@ -144,8 +144,8 @@ int cache_args(const ntk_cache* c, int dtype, int batch, const char* what) {
   if (!c) return no(NTK_E_ARG, "the cache is NULL");
   if (c->dtype != NTK_E4M3 && c->dtype != dtype) return no(NTK_E_ARG, "the cache's dtype is the call's or NTK_E4M3");
   if (c->pages < 0 || c->max_pages < 0) return no(NTK_E_ARG, "pages or max_pages < 0");
-  if (c->page_size < 1 || c->page_size > 1024 || (c->page_size & (c->page_size - 1)))
-    return no(NTK_E_UNSUPPORTED, "page_size must be a power of two from 1 to 1024");
+  if (c->page_size < 8 || c->page_size > 1024 || (c->page_size & (c->page_size - 1)))
+    return no(NTK_E_UNSUPPORTED, "page_size must be a power of two from 8 to 1024");
   if (c->kv_heads < 1) return no(NTK_E_SHAPE, "kv_heads < 1");
   if (c->head_dim < 1) return no(NTK_E_ARG, "head_dim < 1");
   if (c->head_dim > 128) return no(NTK_E_UNSUPPORTED, "head_dim over 128");
@@ -520,7 +520,9 @@ extern "C" int ntk_attention_cached(const ntk_attention_desc* desc, const ntk_ca
   if (cache->pages > 0) {
     set_view(a.k, &cache->k);
     set_view(a.v, &cache->v);
-    vec = vec && view_vec(&cache->k, e4m3 ? 1 : e) && view_vec(&cache->v, e4m3 ? 1 : e);
+    // a lane's offset within eight rows of a page is a 32-bit one
+    vec = vec && view_vec(&cache->k, e4m3 ? 1 : e) && view_vec(&cache->v, e4m3 ? 1 : e) && cache->k.stride_position < (1LL << 26) &&
+          cache->v.stride_position < (1LL << 26);
   }
   a.k_scale = cache->k_scale;
   a.v_scale = cache->v_scale;

@@ -399,8 +399,8 @@ def paged_cache(pages, page_size, kv_heads, dim, dtype=torch.bfloat16, device=No
     """A cache of zeros.  Each head's part of a page lies in one piece, which is what `attention_cached` reads in whole lines."""
     if dtype not in _DTYPES and dtype != _E4M3:
         raise TypeError("dtype must be float32, bfloat16, float16 or float8_e4m3fn")
-    if min(pages, kv_heads, dim) < 1 or not 1 <= page_size <= 1024 or page_size & (page_size - 1):
-        raise ValueError("paged_cache: a size is below 1, or page_size is no power of two up to 1024")
+    if min(pages, kv_heads, dim) < 1 or not 8 <= page_size <= 1024 or page_size & (page_size - 1):
+        raise ValueError("paged_cache: a size is below 1, or page_size is no power of two from 8 to 1024")
     dev = _gpu(device)
     k, v = (torch.zeros((pages, kv_heads, page_size, dim), dtype=torch.uint8 if dtype == _E4M3 else dtype, device=dev) for _ in range(2))
     if dtype != _E4M3:

@@ -97,9 +97,9 @@ APPEND = [
     ("bf16", False, 3, [5, 0, 37], [20, 1, 9], 4, 2, 128, 128, 16, {}),
     ("f16", False, 2, [0, 100], [33, 0], 2, 2, 80, 32, 32, {"interleaved": True}),
     ("f32", False, 2, [3, 4], [7, 2], 3, 1, 37, 36, 8, {}),
-    ("f32", False, 2, [3, 9], [7, 2], 4, 1, 48, 48, 4, {"positions": True}),
+    ("f32", False, 2, [3, 9], [7, 2], 4, 1, 48, 48, 8, {"positions": True}),
     ("bf16", False, 2, [7, 15], [4, 4], 0, 2, 96, 0, 8, {}),
-    ("bf16", False, 1, [2], [6], 2, 1, 128, 64, 1, {"layout": "slots"}),
+    ("bf16", False, 1, [2], [36], 2, 1, 128, 64, 8, {"layout": "slots"}),
     ("bf16", True, 1, [0], [1], 1, 1, 64, 64, 16, {}),
     ("bf16", True, 3, [5, 0, 37], [20, 1, 9], 4, 2, 128, 128, 16, {}),
     ("f16", True, 2, [0, 100], [33, 0], 2, 2, 80, 32, 32, {"interleaved": True}),
@@ -107,7 +107,7 @@ APPEND = [
     ("f32", True, 2, [3, 4], [7, 2], 3, 1, 37, 36, 8, {}),
     ("f32", True, 1, [0], [700], 1, 2, 64, 48, 512, {}),
     ("bf16", True, 2, [7, 15], [4, 4], 0, 2, 72, 16, 8, {"positions": True}),
-    ("bf16", True, 1, [2], [6], 2, 1, 128, 0, 1, {"layout": "slots"}),
+    ("bf16", True, 1, [2], [36], 2, 1, 128, 0, 8, {"layout": "slots"}),
     ("bf16", True, 2, [9, 3], [40, 12], 2, 2, 64, 64, 16, {"layout": "odd"}),
     ("bf16", False, 2, [9, 3], [40, 12], 2, 2, 64, 64, 16, {"layout": "odd"}),
 ]
@@ -218,10 +218,10 @@ def test_append_values_at_the_edge():
     from paper_2206_08720_amd import seq
     x = torch.zeros(1, 4, 1, 16)
     x[0, 0, 0, :4] = torch.tensor([math.inf, -math.inf, math.nan, 3.0])
-    cache = _empty(1, 4, 1, 16, "f32", True)
+    cache = _empty(1, 8, 1, 16, "f32", True)
     seq.cache_append(cache, _ints([[0]]), _ints([0]), x.cuda(), torch.zeros_like(x).cuda())
     k, v = _values(cache)
-    assert torch.isnan(k[0, 0, 0, :3]).all() and k[0, 0, 0, 3] == 3.0 and (k[0, 1:] == 0).all() and (v == 0).all()
+    assert torch.isnan(k[0, 0, 0, :3]).all() and k[0, 0, 0, 3] == 3.0 and (k[0, 1:4] == 0).all() and (v[0, :4] == 0).all()
     assert float(cache.k_scale[0, 0]) == 2.0 ** -7 and float(cache.v_scale[0, 0]) == 2.0 ** -126
     # zeros leave no scale behind: what comes next has its own
     y = torch.full((1, 1, 1, 16), 1e-3)
@@ -229,11 +229,11 @@ def test_append_values_at_the_edge():
     v = _values(cache)[1]
     assert ((v[0, 2] - 1e-3).abs() <= 2.0 ** -4 * 1e-3).all() and (v[0, :2] == 0).all()
     top = torch.tensor([65504.0, -65504.0, 61440.0, 63000.0] * 4).half().view(1, 1, 1, 16)
-    cache = _empty(1, 4, 1, 16, "f16", True)
+    cache = _empty(1, 8, 1, 16, "f16", True)
     seq.cache_append(cache, _ints([[0]]), _ints([0]), top.cuda(), top.cuda())
     assert (_values(cache)[0][0, 0, 0] == torch.tensor([61440.0, -61440.0, 61440.0, 61440.0] * 4)).all()
     tiny = torch.full((1, 1, 1, 16), 2.0 ** -140)
-    cache = _empty(1, 4, 1, 16, "f32", True)
+    cache = _empty(1, 8, 1, 16, "f32", True)
     seq.cache_append(cache, _ints([[0]]), _ints([0]), tiny.cuda(), tiny.cuda())
     assert float(cache.k_scale[0, 0]) == 2.0 ** -126 and (_values(cache)[0][0, 0] == 0).all()
 
@@ -272,8 +272,8 @@ CACHED = [
     ("f16", False, 3, 1, 72, 32, 352, [333], 333, None, {"softcap": 30.0, "slopes": True}),
     ("f32", False, 2, 1, 40, 8, 168, [161, 20], 161, [161, 0], {}),
     ("f32", False, 2, 2, 128, 64, 704, [700], 96, [90], {"softcap": 15.0}),
-    ("bf16", False, 2, 1, 37, 4, 100, [100], 100, None, {}),
-    ("bf16", False, 2, 1, 64, 1, 100, [100, 64], 40, None, {"layout": "odd"}),
+    ("bf16", False, 2, 1, 37, 8, 104, [100], 100, None, {}),
+    ("bf16", False, 2, 1, 64, 8, 104, [100, 64], 40, None, {"layout": "odd"}),
     ("bf16", True, 1, 1, 64, 16, 16, [1], 1, None, {}),
     ("bf16", True, 8, 8, 64, 16, 800, [777, 300, 16], 1, None, {}),
     ("f16", True, 8, 2, 128, 8, 1040, [1030, 1, 0], 1, None, {}),
@@ -288,7 +288,9 @@ CACHED = [
     ("f32", True, 2, 1, 40, 8, 168, [161, 20], 161, [161, 0], {}),
     ("f32", True, 2, 2, 64, 64, 704, [700], 96, [90], {"softcap": 15.0}),
     ("f32", True, 2, 2, 128, 64, 704, [700], 96, [90], {}),
-    ("bf16", True, 2, 1, 64, 1, 100, [100, 64], 40, None, {"layout": "odd"}),
+    ("bf16", True, 2, 1, 64, 8, 104, [100, 64], 40, None, {"layout": "odd"}),
+    ("bf16", True, 2, 2, 48, 8, 104, [100, 37], 1, None, {}),
+    ("f16", True, 8, 2, 64, 8, 104, [100, 37], 30, [30, 29], {}),
     ("bf16", True, 2, 1, 128, 16, 64, [64, 5], 4, [9, 5], {"layout": "slots"}),
     ("bf16", True, 4, 1, 128, 16, 9008, [9000], 17, None, {}),
 ]
