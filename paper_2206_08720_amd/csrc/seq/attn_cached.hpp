@@ -113,6 +113,19 @@ struct PageLoad {
     if constexpr (VEC) return there ? base + off : none;
     return there ? base + (long long)(row - group) * v.ss * CE : none;
   }
+  // the same where the whole tile is the cache's (ordinary()): nothing to select
+  __device__ static __forceinline__ const char* inside(const CachedArgs& a, const AttnView& v, int hk, int tile0, int entries, int i, int wave,
+                                                       int lane) {
+    const int row0 = first(i, wave), lr = lane / CH, row = row0 + lr;
+    int c = lane % CH;
+    if constexpr (!E4M3) c ^= Tile::swz(row);
+    const int group = RPI <= 8 ? row0 : row0 + (lr & 8);
+    const char* base = (const char*)v.p + ((long long)of_row(entries, row0, lane) * v.sb + (long long)a.pages.slot(tile0 + group) * v.ss + (long long)hk * v.sh) * CE;
+    return base + ((uint32_t)(row - group) * (uint32_t)v.ss * CE + (uint32_t)c * 16);
+  }
+  __device__ static __forceinline__ bool ordinary(const CachedArgs& a, int tile0, int len, int entries) {
+    return VEC && EVEN && tile0 + ROWS <= len && a.D == DP && __all((unsigned)entries < (unsigned)a.pages.pages);
+  }
   // 16 bytes of a chunk that need not be aligned
   __device__ static __forceinline__ u32x4 gather(const char* from, bool there, int c, int D) {
     if (!there) return load16(from);
@@ -127,6 +140,8 @@ struct PageLoad {
   __device__ static __forceinline__ void rows(const CachedArgs& a, const AttnView& v, int hk, int tile0, int len, int entries, char* lds, int wave,
                                               int lane) {
     static_assert(!E4M3, "");
+    typedef const __attribute__((address_space(1))) void G;
+    typedef __attribute__((address_space(3))) void L;
 #pragma unroll
     for (int i = 0; i < NI; ++i) {
       int c;
@@ -134,8 +149,6 @@ struct PageLoad {
       const char* from = source(a, v, hk, tile0, len, entries, i, wave, lane, c, there);
       char* to = lds + __builtin_amdgcn_readfirstlane((i * WAVES + wave) * 1024);
       if constexpr (VEC) {
-        typedef const __attribute__((address_space(1))) void G;
-        typedef __attribute__((address_space(3))) void L;
         __builtin_amdgcn_global_load_lds((G*)from, (L*)to, 16, 0, 0);
       } else {
         *reinterpret_cast<u32x4*>(to + lane * 16) = gather(from, there, c, a.D);
@@ -149,6 +162,12 @@ struct PageLoad {
   };
   __device__ static __forceinline__ void fetch(const CachedArgs& a, const AttnView& v, const float* scale, int hk, int tile0, int len, int entries,
                                                int wave, int lane, Held& h) {
+    if (ordinary(a, tile0, len, entries)) {
+      h.s = load_float(scale + ((long long)entries * a.Hk + hk));
+#pragma unroll
+      for (int i = 0; i < NI; ++i) h.x[i] = load16(inside(a, v, hk, tile0, entries, i, wave, lane));
+      return;
+    }
     const bool in = (unsigned)entries < (unsigned)a.pages.pages && tile0 + 8 * (lane & (ROWS / 8 - 1)) < len;
     h.s = load_float(in ? scale + ((long long)entries * a.Hk + hk) : &kOne);
 #pragma unroll
@@ -185,12 +204,11 @@ struct PageLoad {
 };
 
 // A lane's query row: r = i * group + g of key/value head hk.
-template <class T, int DP, bool VEC>
-__device__ __forceinline__ void set_row(const CachedArgs& a, const CachedScope& sc, int b, int hk, int r, int lane, FwdRows<T, DP>& w) {
+template <class T, int DP, bool VEC, class Rows>
+__device__ __forceinline__ void set_row(const CachedArgs& a, const CachedScope& sc, int b, int hk, int r, int lane, Rows& w) {
   const int rr = min(r, a.R - 1), i = (int)a.gdiv.div((uint32_t)rr), g = rr - i * a.G;
   w.pos = sc.off + i;
   w.klim = sc.klim(i);
-  w.doc = 0;
   w.slope2 = a.slopes ? a.slopes[hk * a.G + g] * kLog2e : 0.f;
   load_owned<T, DP, VEC>((const T*)a.q.p + b * a.q.sb + i * a.q.ss + (hk * a.G + g) * a.q.sh, r < a.R, a.D, lane, w.q);
 }
@@ -210,7 +228,7 @@ __device__ __forceinline__ bool cached_body(const CachedArgs& a, char* smem, int
   const int hk = bh % a.Hk, b = bh / a.Hk;
   const CachedScope sc(a, b);
   const int r0 = mt * kFwdRows, r = r0 + wave * 32 + (lane & 31);
-  FwdRows<T, DP> w;
+  FwdRows<T, DP, false, E4M3> w;
   typename AttnTile<T, DP>::Lane tl(lane);
   set_row<T, DP, VEC>(a, sc, b, hk, r, lane, w);
 
@@ -228,10 +246,9 @@ __device__ __forceinline__ bool cached_body(const CachedArgs& a, char* smem, int
         Load::rows(a, a.v, hk, t * BN, sc.len, entries, sv + st * Load::BYTES, wave, lane);
         entries = Load::look(a, b, (t + 1) * BN, lane);
       };
-      if (t0 < t1) {
-        entries = Load::look(a, b, t0 * BN, lane);
-        issue(t0, 0);
-      }
+      if (t0 >= t1) return;
+      entries = Load::look(a, b, t0 * BN, lane);
+      issue(t0, 0);
       for (int t = t0, st = 0; t < t1; ++t, st ^= 1) {
         __builtin_amdgcn_s_waitcnt(0x0070);   // this wave's part of the tile has landed, and its LDS reads are done
         __syncthreads();
@@ -249,11 +266,10 @@ __device__ __forceinline__ bool cached_body(const CachedArgs& a, char* smem, int
         Load::put(kt, sk + st * Load::BYTES, wave, lane);
         Load::put(vt, sv + st * Load::BYTES, wave, lane);
       };
-      if (t0 < t1) {
-        entries = Load::look(a, b, t0 * BN, lane);
-        fetch(t0);
-        put(0);
-      }
+      if (t0 >= t1) return;
+      entries = Load::look(a, b, t0 * BN, lane);
+      fetch(t0);
+      put(0);
       for (int t = t0, st = 0; t < t1; ++t, st ^= 1) {
         __syncthreads();                       // tile t is written, and tile t - 1 read
         if (t + 1 < t1) fetch(t + 1);
@@ -300,7 +316,7 @@ __device__ __forceinline__ bool cached_tokens_body(const CachedArgs& a, char* sm
   const int hk = bh % a.Hk, b = bh / a.Hk;
   const CachedScope sc(a, b);
   const int r = lane & 31;
-  FwdRows<T, DP> w;
+  FwdRows<T, DP, false, E4M3> w;
   typename AttnTile<T, DP>::Lane tl(lane);
   set_row<T, DP, VEC>(a, sc, b, hk, r, lane, w);
 
@@ -312,28 +328,28 @@ __device__ __forceinline__ bool cached_tokens_body(const CachedArgs& a, char* sm
     w.reset();
     int entries = 0;                           // of the tile that is read next
     int t = t0 + wave;
-    if (t < t1) entries = Load::look(a, b, t * BN, lane);
+    if (t >= t1) return;
+    entries = Load::look(a, b, t * BN, lane);
     if constexpr (!E4M3) {
       auto issue = [&](int t, int st) {
         char* s = mine + st * 2 * Load::BYTES;
         Load::rows(a, a.k, hk, t * BN, sc.len, entries, s, 0, lane);
         Load::rows(a, a.v, hk, t * BN, sc.len, entries, s + Load::BYTES, 0, lane);
       };
-      if (t < t1) {
-        issue(t, 0);
-        entries = Load::look(a, b, (t + W) * BN, lane);
-      }
+      issue(t, 0);
+      entries = Load::look(a, b, (t + W) * BN, lane);
       for (int st = 0; t < t1; t += W, st ^= 1) {
         const bool more = t + W < t1;
         if (VEC && more) {
+          const int then = Load::look(a, b, (t + 2 * W) * BN, lane);   // in front of the loads that it would wait for
           issue(t + W, st ^ 1);
+          entries = then;
           wait_loads<2 * Load::NI>();    // the current tile has landed; the next stays in flight
         } else {
           __builtin_amdgcn_s_waitcnt(0x0070);
         }
         __builtin_amdgcn_wave_barrier();
         __builtin_amdgcn_sched_barrier(0);
-        if (VEC && more) entries = Load::look(a, b, (t + 2 * W) * BN, lane);
         const char* s = mine + st * 2 * Load::BYTES;
         w.template tile<1>(a, s, s + Load::BYTES, nullptr, t * BN, (t + 1) * BN > all, careful, lane, tl);
         __builtin_amdgcn_s_waitcnt(0xC07F);   // this wave's LDS reads are done: the stage may be filled again
@@ -346,20 +362,19 @@ __device__ __forceinline__ bool cached_tokens_body(const CachedArgs& a, char* sm
       }
     } else {
       typename Load::Held kt, vt;
-      if (t < t1) {
-        Load::fetch(a, a.k, a.k_scale, hk, t * BN, sc.len, entries, 0, lane, kt);
-        Load::fetch(a, a.v, a.v_scale, hk, t * BN, sc.len, entries, 0, lane, vt);
-        entries = Load::look(a, b, (t + W) * BN, lane);
-      }
+      Load::fetch(a, a.k, a.k_scale, hk, t * BN, sc.len, entries, 0, lane, kt);
+      Load::fetch(a, a.v, a.v_scale, hk, t * BN, sc.len, entries, 0, lane, vt);
+      entries = Load::look(a, b, (t + W) * BN, lane);
       for (; t < t1; t += W) {
         const bool more = t + W < t1;
         // keys are on their way while values are written, and the other way round
         Load::put(kt, mine, 0, lane);
         if (more) {
+          const int then = Load::look(a, b, (t + 2 * W) * BN, lane);   // in front of the loads that it would wait for
           Load::fetch(a, a.k, a.k_scale, hk, (t + W) * BN, sc.len, entries, 0, lane, kt);
           Load::put(vt, mine + Load::BYTES, 0, lane);
           Load::fetch(a, a.v, a.v_scale, hk, (t + W) * BN, sc.len, entries, 0, lane, vt);
-          entries = Load::look(a, b, (t + 2 * W) * BN, lane);
+          entries = then;
         } else {
           Load::put(vt, mine + Load::BYTES, 0, lane);
         }

@@ -12,7 +12,8 @@ constexpr int kFwdKeys = sizeof(T) == 2 ? 64 : 32;
 constexpr int kFwdRows = 128;
 
 // One wave's 32 query rows: a lane's row, its limits and its state.
-template <class T, int DP>
+// DOCS: the call may have documents.  EARLY: tiles are written into LDS by the waves.
+template <class T, int DP, bool DOCS = true, bool EARLY = false>
 struct FwdRows {
   using N = Num<T>;
   using Tile = AttnTile<T, DP>;
@@ -39,6 +40,31 @@ struct FwdRows {
     zero16(s);
 #pragma unroll
     for (int t = 0; t < KT; ++t) s = N::template product<Careful::value>(Tile::rows(sk, 32 * nb, t, tl), q[t], s);
+    finish_scores<Careful>(a, nb, key0, ids, masked, lane, s, vis);
+  }
+  // All products of a tile before the first of their scores is used, four operands read ahead.
+  template <int NB>
+  __device__ __forceinline__ void products_early(const char* sk, const typename Tile::Lane& tl, f32x16 (&s)[NB]) const {
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb) zero16(s[nb]);
+#pragma unroll
+    for (int t = 0; t < KT; ++t)
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb) s[nb] = N::template product<false>(Tile::rows(sk, 32 * nb, t, tl), q[t], s[nb]);
+    if constexpr (sizeof(T) == 2) {
+      constexpr int DS = 0x100, MFMA = 8, AHEAD = 4;
+      __builtin_amdgcn_sched_group_barrier(DS, AHEAD, 0);
+#pragma unroll
+      for (int i = 0; i < KT * NB - AHEAD; ++i) {
+        __builtin_amdgcn_sched_group_barrier(MFMA, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(DS, 1, 0);
+      }
+      __builtin_amdgcn_sched_group_barrier(MFMA, AHEAD, 0);
+    }
+  }
+  template <class Careful>
+  __device__ __forceinline__ void finish_scores(const AttnArgs& a, int nb, int key0, const int* ids, bool masked, int lane, f32x16& s,
+                                                unsigned& vis) const {
     const int h4 = 4 * (lane >> 5), base = key0 + 32 * nb + h4;
     if (a.cap_in != 0.f) {
 #pragma unroll
@@ -57,9 +83,9 @@ struct FwdRows {
         vis = 0xffffu;
 #pragma unroll
         for (int v = 0; v < 16; ++v)
-          if (8 * (v >> 2) + (v & 3) >= left || (a.docs && ids[32 * nb + h4 + 8 * (v >> 2) + (v & 3)] != doc)) vis &= ~(1u << v);
+          if (8 * (v >> 2) + (v & 3) >= left || (DOCS && a.docs && ids[32 * nb + h4 + 8 * (v >> 2) + (v & 3)] != doc)) vis &= ~(1u << v);
       }
-      if (a.docs) {
+      if (DOCS && a.docs) {
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
           const i32x4 id = *reinterpret_cast<const i32x4*>(ids + 32 * nb + h4 + 8 * q);
@@ -82,8 +108,14 @@ struct FwdRows {
     tl.fresh();
     f32x16 s[NB];
     unsigned vis[NB];
+    if constexpr (EARLY && !Careful::value) {
+      products_early<NB>(sk, tl, s);
 #pragma unroll
-    for (int nb = 0; nb < NB; ++nb) scores<Careful>(a, sk, nb, key0, ids, masked, lane, tl, s[nb], vis[nb]);
+      for (int nb = 0; nb < NB; ++nb) finish_scores<Careful>(a, nb, key0, ids, masked, lane, s[nb], vis[nb]);
+    } else {
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb) scores<Careful>(a, sk, nb, key0, ids, masked, lane, tl, s[nb], vis[nb]);
+    }
     float top = s[0][0];
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb)
@@ -120,7 +152,10 @@ struct FwdRows {
       const Frag p = to_frag<T>(s[nb], u);
       if constexpr (!Careful::value) {
         Frag vt[DB];
-        vc.template read<16 * X>(vt, tl);
+        if constexpr (EARLY)
+          vc.template read_early<16 * X>(vt, tl);
+        else
+          vc.template read<16 * X>(vt, tl);
 #pragma unroll
         for (int d = 0; d < DB; ++d) acc[d] = N::mma(vt[d], p, acc[d]);
       } else {
@@ -137,8 +172,8 @@ struct FwdRows {
 };
 
 // Row results: o and lse, or a range's partial sums for k_attn_join.
-template <class T, int DP, bool VEC>
-__device__ __forceinline__ void finish_row(const AttnArgs& a, FwdRows<T, DP>& w, int b, int hk, int r, int split, int lane) {
+template <class T, int DP, bool VEC, class Rows>
+__device__ __forceinline__ void finish_row(const AttnArgs& a, Rows& w, int b, int hk, int r, int split, int lane) {
   if (r >= a.R) return;
   const float unit = a.cap_in != 0.f || a.slopes ? 1.f : a.c;
   const float m2 = w.m == -__builtin_inff() ? w.m : w.m * unit;
@@ -161,8 +196,8 @@ __device__ __forceinline__ void finish_row(const AttnArgs& a, FwdRows<T, DP>& w,
 }
 
 // The states of W waves that took keys of the same rows, one after the other, into the first one's; true there.
-template <class T, int DP, int W>
-__device__ __forceinline__ bool join_waves(const AttnArgs& a, FwdRows<T, DP>& w, char* smem, int wave, int lane) {
+template <class T, int DP, int W, class Rows>
+__device__ __forceinline__ bool join_waves(const AttnArgs& a, Rows& w, char* smem, int wave, int lane) {
   __syncthreads();
   float* sacc = reinterpret_cast<float*>(smem);        // [W - 1][DB * 16][64]
   float* sml = sacc + (W - 1) * FwdRows<T, DP>::DB * 16 * 64;   // [W - 1][2][64]
