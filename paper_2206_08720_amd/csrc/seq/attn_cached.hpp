@@ -17,6 +17,8 @@ struct CachedArgs : AttnArgs {             // k, v: sb from page to page, ss fro
   PageTable pages;
   const int* q_lens;                       // [batch] or null
   const float *k_scale, *v_scale;          // [pages, kv_heads]: the cache is e4m3
+  int workers, least;                      // workgroups, tiles that each takes at least; 0: a workgroup a row tile
+  int* heads;                              // [workers][4]: row tiles that a worker begins and others go on with
 };
 
 namespace {
@@ -77,54 +79,70 @@ struct PageLoad {
   using Tile = AttnTile<T, DP>;
   static constexpr int CE = E4M3 ? 1 : (int)sizeof(T);           // bytes an element of the cache
   static constexpr int CH = DP * CE / 16, EC = 16 / CE;         // chunks a row, elements a chunk
-  static constexpr int RPI = 64 / CH;                           // rows an instruction: at most 16
+  using At = TilePlaces<CH, WAVES>;
+  static constexpr int RPI = At::RPI;
   static constexpr int BYTES = ROWS * Tile::RB;
   static constexpr int NI = (ROWS * CH + 64 * WAVES - 1) / (64 * WAVES);
   static constexpr bool EVEN = NI * 64 * WAVES == ROWS * CH;    // else some waves have none (rows >= ROWS)
-  static_assert((EVEN || E4M3) && RPI <= 16, "chunks split over the lanes");
+  static_assert(EVEN || E4M3, "chunks split over the lanes");
 
   // lane l: the table's entry for the rows 8 (l % (ROWS / 8)) .. + 7 of a tile
   __device__ static __forceinline__ int look(const CachedArgs& a, int b, int tile0, int lane) {
     const int e = min((tile0 + 8 * (lane & (ROWS / 8 - 1))) >> a.pages.shift, a.pages.most - 1);
     return a.pages.table[(long long)b * a.pages.most + e];
   }
-  // instruction i's first row
-  __device__ static __forceinline__ int first(int i, int wave) { return (i * WAVES + wave) * RPI; }
-  // the entry (or its scale) of a lane's row
-  __device__ static __forceinline__ int of_row(int entries, int row0, int lane) {
-    const int lo = __builtin_amdgcn_readlane(entries, row0 / 8);
+  // One head's part of a cache's array: bytes.
+  struct Head {
+    const char* base;
+    long long page;                        // from page to page
+    uint32_t slot;                         // from slot to slot
+    __device__ __forceinline__ Head(const AttnView& v, int hk) : base((const char*)v.p + (long long)hk * v.sh * CE), page(v.sb * CE), slot((uint32_t)(v.ss * CE)) {}
+  };
+  // A tile's place, with look()'s entry for it.
+  struct Where {
+    int entry;
+    long long scale;                       // lane l: of the rows 8 (l % (ROWS / 8)) ..; -1: none
+    int tile0, len;
+    bool whole;                            // every row is the cache's
+    __device__ __forceinline__ Where(const CachedArgs& a, int hk, int entry_, int tile0_, int len_, int lane)
+        : entry(entry_), tile0(tile0_), len(len_) {
+      const bool in = (unsigned)entry < (unsigned)a.pages.pages;
+      scale = in && tile0 + 8 * (lane & (ROWS / 8 - 1)) < len ? (long long)entry * a.Hk + hk : -1;
+      whole = VEC && EVEN && tile0 + ROWS <= len && a.D == DP && __all(in);
+    }
+  };
+  // what look() has (or its scale) for a lane's row of the instruction whose first row is row0
+  __device__ static __forceinline__ int of_row(int x, int row0, int lane) {
+    const int lo = __builtin_amdgcn_readlane(x, row0 / 8);
     if constexpr (RPI <= 8) return lo;
-    return lane < 32 ? lo : __builtin_amdgcn_readlane(entries, row0 / 8 + 1);
+    return lane < 32 ? lo : __builtin_amdgcn_readlane(x, row0 / 8 + 1);
   }
+  // a lane's chunk of a row, and where it is within eight rows
+  __device__ static __forceinline__ int chunk(int row, int lane) {
+    if constexpr (E4M3) return lane % CH;
+    return lane % CH ^ Tile::swz(row);                          // straight into LDS: lane l's 16 bytes go to place l
+  }
+  __device__ static __forceinline__ uint32_t within(const Head& h, int row, int c) { return (uint32_t)(row & 7) * h.slot + (uint32_t)c * 16; }
   // where a lane's chunk of instruction i is read; `there`: it is the cache's
-  __device__ static __forceinline__ const char* source(const CachedArgs& a, const AttnView& v, int hk, int tile0, int len, int entries, int i,
-                                                       int wave, int lane, int& c, bool& there) {
-    const int row0 = first(i, wave), lr = lane / CH, row = row0 + lr;
-    c = lane % CH;
-    if constexpr (!E4M3) c ^= Tile::swz(row);                   // straight into LDS: lane l's 16 bytes go to place l
-    const int id = of_row(entries, row0, lane);
+  __device__ static __forceinline__ const char* source(const CachedArgs& a, const Head& h, const Where& w, int i, int wave, int lane, int& c, bool& there) {
+    const int row0 = At::first(i, wave), row = At::row(i, wave, lane), id = of_row(w.entry, row0, lane);
+    c = chunk(row, lane);
     const bool in = (unsigned)id < (unsigned)a.pages.pages;
-    const int group = RPI <= 8 ? row0 : row0 + (lr & 8);
-    const char* base = (const char*)v.p + ((long long)(in ? id : 0) * v.sb + (long long)a.pages.slot(tile0 + group) * v.ss + (long long)hk * v.sh) * CE;
-    const bool live = tile0 + row < len && (EVEN || row < ROWS);
+    const char* base = h.base + (long long)(in ? id : 0) * h.page + (long long)a.pages.slot(w.tile0 + At::group(row0, lane)) * h.slot;
+    const bool live = w.tile0 + row < w.len && (EVEN || row < ROWS);
     there = live && in && c * EC < a.D;
-    const uint32_t off = (uint32_t)(row - group) * (uint32_t)v.ss * CE + (uint32_t)c * 16;   // rows that are not there: unused
     const char* none = live && !in ? (const char*)&kNaNs : (const char*)&kZeros;
-    if constexpr (VEC) return there ? base + off : none;
-    return there ? base + (long long)(row - group) * v.ss * CE : none;
+    if constexpr (VEC) {
+      uint64_t at = (uint64_t)(uintptr_t)(base + within(h, row, c));
+      asm volatile("" : "+v"(at));             // formed in any case: a branch around it would cost more
+      return there ? (const char*)(uintptr_t)at : none;
+    }
+    return there ? base + (long long)(row & 7) * h.slot : none;
   }
-  // the same where the whole tile is the cache's (ordinary()): nothing to select
-  __device__ static __forceinline__ const char* inside(const CachedArgs& a, const AttnView& v, int hk, int tile0, int entries, int i, int wave,
-                                                       int lane) {
-    const int row0 = first(i, wave), lr = lane / CH, row = row0 + lr;
-    int c = lane % CH;
-    if constexpr (!E4M3) c ^= Tile::swz(row);
-    const int group = RPI <= 8 ? row0 : row0 + (lr & 8);
-    const char* base = (const char*)v.p + ((long long)of_row(entries, row0, lane) * v.sb + (long long)a.pages.slot(tile0 + group) * v.ss + (long long)hk * v.sh) * CE;
-    return base + ((uint32_t)(row - group) * (uint32_t)v.ss * CE + (uint32_t)c * 16);
-  }
-  __device__ static __forceinline__ bool ordinary(const CachedArgs& a, int tile0, int len, int entries) {
-    return VEC && EVEN && tile0 + ROWS <= len && a.D == DP && __all((unsigned)entries < (unsigned)a.pages.pages);
+  // The same in a whole tile: a scalar base and 32 bits of a lane, nothing to select.
+  __device__ static __forceinline__ long long offset(const CachedArgs& a, const Head& h, const Where& w, int i, int wave, int lane) {
+    const int row0 = At::first(i, wave);
+    return (long long)of_row(w.entry, row0, lane) * h.page + (uint32_t)a.pages.slot(w.tile0 + At::group(row0, lane)) * h.slot;
   }
   // 16 bytes of a chunk that need not be aligned
   __device__ static __forceinline__ u32x4 gather(const char* from, bool there, int c, int D) {
@@ -137,8 +155,7 @@ struct PageLoad {
     return u;
   }
   // the cache in the queries' type: into LDS
-  __device__ static __forceinline__ void rows(const CachedArgs& a, const AttnView& v, int hk, int tile0, int len, int entries, char* lds, int wave,
-                                              int lane) {
+  __device__ static __forceinline__ void rows(const CachedArgs& a, const Head& h, const Where& w, char* lds, int wave, int lane) {
     static_assert(!E4M3, "");
     typedef const __attribute__((address_space(1))) void G;
     typedef __attribute__((address_space(3))) void L;
@@ -146,13 +163,12 @@ struct PageLoad {
     for (int i = 0; i < NI; ++i) {
       int c;
       bool there;
-      const char* from = source(a, v, hk, tile0, len, entries, i, wave, lane, c, there);
+      const char* from = source(a, h, w, i, wave, lane, c, there);
       char* to = lds + __builtin_amdgcn_readfirstlane((i * WAVES + wave) * 1024);
-      if constexpr (VEC) {
+      if constexpr (VEC)
         __builtin_amdgcn_global_load_lds((G*)from, (L*)to, 16, 0, 0);
-      } else {
+      else
         *reinterpret_cast<u32x4*>(to + lane * 16) = gather(from, there, c, a.D);
-      }
     }
   }
   // the cache in 8 bits: into registers, and from there into LDS
@@ -160,34 +176,34 @@ struct PageLoad {
     u32x4 x[NI];
     float s;                               // lane l: the scale of the rows that look() takes for it
   };
-  __device__ static __forceinline__ void fetch(const CachedArgs& a, const AttnView& v, const float* scale, int hk, int tile0, int len, int entries,
-                                               int wave, int lane, Held& h) {
-    if (ordinary(a, tile0, len, entries)) {
-      h.s = load_float(scale + ((long long)entries * a.Hk + hk));
+  __device__ static __forceinline__ void fetch(const CachedArgs& a, const Head& h, const float* scale, const Where& w, int wave, int lane, Held& to) {
+    to.s = load_float(w.scale >= 0 ? scale + w.scale : &kOne);
+    if (w.whole) {
 #pragma unroll
-      for (int i = 0; i < NI; ++i) h.x[i] = load16(inside(a, v, hk, tile0, entries, i, wave, lane));
+      for (int i = 0; i < NI; ++i) {
+        const int row = At::row(i, wave, lane);
+        to.x[i] = load16(h.base + offset(a, h, w, i, wave, lane) + within(h, row, chunk(row, lane)));
+      }
       return;
     }
-    const bool in = (unsigned)entries < (unsigned)a.pages.pages && tile0 + 8 * (lane & (ROWS / 8 - 1)) < len;
-    h.s = load_float(in ? scale + ((long long)entries * a.Hk + hk) : &kOne);
 #pragma unroll
     for (int i = 0; i < NI; ++i) {
       int c;
       bool there;
-      const char* from = source(a, v, hk, tile0, len, entries, i, wave, lane, c, there);
+      const char* from = source(a, h, w, i, wave, lane, c, there);
       if constexpr (VEC)
-        h.x[i] = load16(from);
+        to.x[i] = load16(from);
       else
-        h.x[i] = gather(from, there, c, a.D);
+        to.x[i] = gather(from, there, c, a.D);
     }
   }
   __device__ static __forceinline__ void put(const Held& h, char* lds, int wave, int lane) {
     constexpr int TC = (int)sizeof(T);     // chunks of the tile that a chunk of the cache becomes
 #pragma unroll
     for (int i = 0; i < NI; ++i) {
-      const int row = first(i, wave) + lane / CH, c = lane % CH;
+      const int row = At::row(i, wave, lane), c = lane % CH;
       if (!EVEN && row >= ROWS) continue;
-      const float s = __int_as_float(of_row(__float_as_int(h.s), first(i, wave), lane));
+      const float s = __int_as_float(of_row(__float_as_int(h.s), At::first(i, wave), lane));
       alignas(16) T e[16];
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
@@ -213,88 +229,306 @@ __device__ __forceinline__ void set_row(const CachedArgs& a, const CachedScope& 
   load_owned<T, DP, VEC>((const T*)a.q.p + b * a.q.sb + i * a.q.ss + (hk * a.G + g) * a.q.sh, r < a.R, a.D, lane, w.q);
 }
 
+// ---- the work, in equal parts ----------------------------------------------------------------------------------------------
+// Sequences have lengths of their own, which the host does not know: with a workgroup a row tile, or ranges of a row's keys cut
+// alike for all, the longest sequence would keep a few workgroups busy after the others have gone (32 sequences of 16 to 32
+// thousand places: 171 us; parts of two prompts: 847 us).  So the workgroups that run at once deal out all tiles of keys, head by head and
+// row tile by row tile, in equal runs.  A row tile whose run ends early is gone on with by the next workers; what each has of it is
+// joined by k_cached_join.  The parts follow from the lengths alone, so that results do not depend on timing.
+//
+// A row tile of no keys counts as one: its rows are written, too.
+template <int BN, int ROWS>
+struct Parts {
+  // tiles of keys that row tile mt of sequence b sees
+  __device__ static __forceinline__ int tiles(const CachedArgs& a, int b, int mt) {
+    const CachedScope sc(a, b);
+    const int i0 = (int)a.gdiv.div((uint32_t)(mt * ROWS)), i1 = (int)a.gdiv.div((uint32_t)(min(mt * ROWS + ROWS, a.R) - 1));
+    return (sc.any(i0, i1) + BN - 1) / BN;
+  }
+  int hk, pair, t, per, left;              // where this worker's run stands: pair = b * row tiles + mt, tile t, tiles left
+  __device__ __forceinline__ int b(const CachedArgs& a) const { return a.tiles == 1 ? pair : pair / a.tiles; }
+  __device__ __forceinline__ int mt(const CachedArgs& a) const { return a.tiles == 1 ? 0 : pair % a.tiles; }
+
+  template <int THREADS>
+  __device__ __forceinline__ void find(const CachedArgs& a, int block) {
+    __shared__ long long sums[THREADS / 64];
+    __shared__ int found[3];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = a.B * a.tiles;
+    if (a.workers == 0) {
+      int bh, item;
+      place(block, a.B * a.Hk, bh, item);
+      hk = bh % a.Hk;
+      pair = bh / a.Hk * a.tiles + a.tiles - 1 - item;          // the rows that see most keys first
+      t = 0;
+      left = per = 0x7fffffff;
+      return;
+    }
+    const bool inside = a.tiles == 1;
+    const int times = inside ? a.Hk : 1;
+    const int chunk = (n + THREADS - 1) / THREADS, p0 = min(n, (int)threadIdx.x * chunk), p1 = min(n, p0 + chunk);
+    long long mine = 0;
+    for (int p = p0; p < p1; ++p) mine += (long long)times * max(1, tiles(a, p / a.tiles, p % a.tiles));
+    long long upto = mine;                                       // inclusive sum
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const long long x = __shfl_up(upto, o);
+      if (lane >= o) upto += x;
+    }
+    if (lane == 63) sums[wave] = upto;
+    __syncthreads();
+    long long total = 0;
+#pragma unroll
+    for (int w = 0; w < THREADS / 64; ++w) {
+      if (w < wave) upto += sums[w];
+      total += sums[w];
+    }
+    // neighbours in the order read the same keys: a die (workgroups are dealt out to the eight in turn) takes a run of workers
+    const int eighth = a.workers / 8, w = a.workers % 8 ? block : (block % 8) * eighth + block / 8;
+    const long long all = inside ? total : total * a.Hk;
+    per = (int)min((long long)0x7fffffff, max((long long)a.least, (all + a.workers - 1) / a.workers));
+    const long long g0 = (long long)w * per;
+    left = (int)max(0LL, min((long long)per, all - g0));
+    hk = inside ? 0 : (int)(g0 / total);
+    const long long at = g0 - hk * total;
+    if (at >= upto - mine && at < upto) {
+      long long x = upto - mine;
+      int p = p0;
+      for (;; ++p) {
+        const int c = max(1, tiles(a, p / a.tiles, p % a.tiles));
+        if (at < x + (long long)times * c) {
+          found[0] = p;
+          found[1] = (int)((at - x) % c);
+          found[2] = inside ? (int)((at - x) / c) : hk;
+          break;
+        }
+        x += (long long)times * c;
+      }
+    }
+    __syncthreads();
+    pair = __builtin_amdgcn_readfirstlane(found[0]);
+    t = __builtin_amdgcn_readfirstlane(found[1]);
+    hk = __builtin_amdgcn_readfirstlane(found[2]);
+    left = __builtin_amdgcn_readfirstlane(left);
+    per = __builtin_amdgcn_readfirstlane(per);
+  }
+  // the row tile behind: a sequence's heads in turn, whose parts of a page are neighbours, or, where many rows read the same keys,
+  // all of a head's rows
+  __device__ __forceinline__ void next(const CachedArgs& a) {
+    if (a.tiles == 1) {
+      if (++hk < a.Hk) return;
+      hk = 0;
+      ++pair;
+    } else if (++pair == a.B * a.tiles) {
+      pair = 0;
+      ++hk;
+    }
+  }
+  // this worker's number in the order of the work
+  __device__ static __forceinline__ int number(const CachedArgs& a, int block) {
+    return a.workers % 8 ? block : (block % 8) * (a.workers / 8) + block / 8;
+  }
+};
+
+// A stretch [t0, t1) of a row tile's `nt` tiles of keys.
+struct Stretch {
+  int b, hk, mt, t0, t1, nt, slot;         // slot: where its partial results go, -1: it is all of them
+};
+
+// Calls f(stretch) for a worker's stretches and notes the row tile that it begins and does not end.  What it goes on with for another
+// comes last: the workers of a head then begin at its first key together, and read the same keys at about the same time.
+template <class P, int THREADS, class F>
+__device__ __forceinline__ void each_stretch(const CachedArgs& a, int block, F f) {
+  P p;
+  p.template find<THREADS>(a, block);
+  const int w = P::number(a, block);
+  if (a.workers && threadIdx.x == 0) a.heads[4 * w + 2] = 0;
+  if (p.left <= 0) return;
+  P late = p;
+  late.left = 0;
+  for (;;) {
+    const bool end = p.left <= 0;
+    if (end) {
+      if (late.left <= 0) return;
+      p = late;
+      late.left = 0;
+    }
+    Stretch s;
+    s.b = p.b(a);
+    s.mt = p.mt(a);
+    s.hk = p.hk;
+    s.nt = P::tiles(a, s.b, s.mt);
+    const int count = max(1, s.nt), take = min(count - p.t, p.left);
+    const bool first = p.t == 0, last = p.t + take == count;
+    if (!first && !end && take < p.left) {
+      late = p;
+      late.left = take;
+    } else {
+      s.t0 = p.t;
+      s.t1 = min(s.nt, p.t + take);
+      s.slot = first && last ? -1 : first ? 2 * w + 1 : 2 * w;
+      f(s);
+      if (a.workers == 0) return;
+      if (first && !last && threadIdx.x == 0) {
+        a.heads[4 * w] = p.pair;
+        a.heads[4 * w + 1] = p.hk;
+        a.heads[4 * w + 2] = (count - take + p.per - 1) / p.per;   // workers behind this one
+      }
+    }
+    p.left -= take;
+    p.t = 0;
+    p.next(a);
+  }
+}
+
+// The rows' results, or their partial sums: [slot][ROWS] rows of DP, behind them maximum (in units of log2) and sum.
+template <class T, int DP, int ROWS, bool VEC, class Rows>
+__device__ __forceinline__ void finish_stretch(const CachedArgs& a, Rows& w, const Stretch& s, int row, int lane) {
+  if (s.slot < 0) {
+    finish_row<T, DP, VEC>(a, w, s.b, s.hk, s.mt * ROWS + row, 0, lane);
+    return;
+  }
+  const long long at = (long long)s.slot * ROWS + row;
+  store_owned<float, DP, true>(a.part + at * DP, DP, lane, w.acc, 1.f);
+  if (lane < 32) {
+    float* ml = a.part + (long long)a.workers * 2 * ROWS * DP + at * 2;
+    ml[0] = w.m == -__builtin_inff() ? w.m : w.m * (a.cap_in != 0.f || a.slopes ? 1.f : a.c);
+    ml[1] = w.l;
+  }
+}
+
+// 32 rows of a row tile that one worker began: its sums and those of the workers behind it.
+template <class T, int DP, int ROWS>
+__global__ void __launch_bounds__(256) k_cached_join(const CachedArgs a) {
+  constexpr int LANES = DP / 4, AT_ONCE = 256 / LANES;
+  const int w = blockIdx.x / (ROWS / 32), part = blockIdx.x % (ROWS / 32);
+  const int pair = a.heads[4 * w], hk = a.heads[4 * w + 1], behind = a.heads[4 * w + 2];
+  if (behind == 0) return;
+  const int b = pair / a.tiles, mt = pair - b * a.tiles, d = threadIdx.x % LANES * 4;
+  const float* ml = a.part + (long long)a.workers * 2 * ROWS * DP;
+#pragma unroll 1
+  for (int row = part * 32 + threadIdx.x / LANES; row < part * 32 + 32; row += AT_ONCE) {
+    const int r = mt * ROWS + row;
+    if (r >= a.R) return;
+    float m = -__builtin_inff(), l = 0.f;
+    f32x4 o = {0.f, 0.f, 0.f, 0.f};
+    for (int s0 = 0; s0 <= behind; s0 += 4) {                    // four stretches' numbers in flight at a time
+      float ms[4], ls[4];
+      f32x4 os[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const int x = min(s0 + u, behind), slot = x == 0 ? 2 * w + 1 : 2 * (w + x);
+        const long long at = (long long)slot * ROWS + row;
+        ms[u] = s0 + u <= behind ? ml[at * 2] : -__builtin_inff();
+        ls[u] = ml[at * 2 + 1];
+        os[u] = *reinterpret_cast<const f32x4*>(a.part + at * DP + d);
+      }
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        if (s0 + u > behind) break;
+        const float mn = fmaxf(m, ms[u]);
+        const float f = m == mn ? 1.f : exp2_hw(m - mn), g = ms[u] == mn ? 1.f : exp2_hw(ms[u] - mn);
+        l = l * f + ls[u] * g;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) o[k] = o[k] * f + os[u][k] * g;
+        m = mn;
+      }
+    }
+    const int i = (int)a.gdiv.div((uint32_t)r), head = hk * a.G + r - i * a.G;
+    T* out = (T*)a.o.p + b * a.o.sb + i * a.o.ss + head * a.o.sh;
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+      if (d + k < a.D) out[d + k] = (T)(l == 0.f ? 0.f : o[k] / l);
+    if (a.lse && d == 0)
+      a.lse[((long long)b * a.H + head) * a.Sq + i] = l == 0.f ? -__builtin_inff() : m * kLn2 + logf(l * kWeightOne<T>);
+  }
+}
+
 // ---- many rows: four waves of 32 rows share the key tiles in two LDS stages -------------------------------------------------
 template <class T, int DP, bool VEC, bool E4M3, bool CAREFUL>
-__device__ __forceinline__ bool cached_body(const CachedArgs& a, char* smem, int block) {
+__device__ __forceinline__ bool cached_stretch(const CachedArgs& a, char* smem, const Stretch& x) {
   constexpr int BN = kFwdKeys<T>;
   using Load = PageLoad<T, DP, BN, 4, VEC, E4M3>;
   char* sk = smem;                                  // [2][BN][DP]
   char* sv = smem + 2 * Load::BYTES;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-
-  int bh, item;
-  place(block, a.B * a.Hk, bh, item);
-  const int split = item % a.splits, mt = a.tiles - 1 - item / a.splits;   // the rows that see most keys first
-  const int hk = bh % a.Hk, b = bh / a.Hk;
+  const int b = x.b, hk = x.hk, t0 = x.t0, t1 = x.t1;
   const CachedScope sc(a, b);
-  const int r0 = mt * kFwdRows, r = r0 + wave * 32 + (lane & 31);
+  const int row = wave * 32 + (lane & 31), r0 = x.mt * kFwdRows + wave * 32;
   FwdRows<T, DP, false, E4M3> w;
   typename AttnTile<T, DP>::Lane tl(lane);
-  set_row<T, DP, VEC>(a, sc, b, hk, r, lane, w);
+  set_row<T, DP, VEC>(a, sc, b, hk, x.mt * kFwdRows + row, lane, w);
 
-  const int i_lo = (int)a.gdiv.div((uint32_t)r0), i_hi = (int)a.gdiv.div((uint32_t)(min(r0 + kFwdRows, a.R) - 1));
-  const int all = sc.all(i_lo, i_hi), any = sc.any(i_lo, i_hi);
-  const int nt = (any + BN - 1) / BN, per = (nt + a.splits - 1) / a.splits;
-  const int t0 = split * per, t1 = min(nt, t0 + per);
+  // keys that all of this wave's rows see, that some row sees
+  const int i_lo = (int)a.gdiv.div((uint32_t)min(r0, a.R - 1)), i_hi = (int)a.gdiv.div((uint32_t)(min(r0 + 32, a.R) - 1));
+  const int all = sc.all(i_lo, i_hi), any = r0 < a.R ? sc.any(i_lo, i_hi) : 0;
+
+  const typename Load::Head keys(a.k, hk), values(a.v, hk);
 
   auto pass = [&](auto careful) {
     w.reset();
-    int entries = 0;                           // of the tile that is read next
+    auto multiply = [&](int t, int st) {
+      if (t * BN < any)
+        w.template tile<BN / 32>(a, sk + st * Load::BYTES, sv + st * Load::BYTES, nullptr, t * BN, (t + 1) * BN > all, careful, lane, tl);
+    };
+    if (t0 >= t1) return;
+    int entry = Load::look(a, b, t0 * BN, lane);                 // of the tile that is read next
     if constexpr (!E4M3) {
       auto issue = [&](int t, int st) {
-        Load::rows(a, a.k, hk, t * BN, sc.len, entries, sk + st * Load::BYTES, wave, lane);
-        Load::rows(a, a.v, hk, t * BN, sc.len, entries, sv + st * Load::BYTES, wave, lane);
-        entries = Load::look(a, b, (t + 1) * BN, lane);
+        const typename Load::Where at(a, hk, entry, t * BN, sc.len, lane);
+        entry = Load::look(a, b, (t + 1) * BN, lane);
+        Load::rows(a, keys, at, sk + st * Load::BYTES, wave, lane);
+        Load::rows(a, values, at, sv + st * Load::BYTES, wave, lane);
       };
-      if (t0 >= t1) return;
-      entries = Load::look(a, b, t0 * BN, lane);
       issue(t0, 0);
       for (int t = t0, st = 0; t < t1; ++t, st ^= 1) {
         __builtin_amdgcn_s_waitcnt(0x0070);   // this wave's part of the tile has landed, and its LDS reads are done
         __syncthreads();
         if (t + 1 < t1) issue(t + 1, st ^ 1);
-        w.template tile<BN / 32>(a, sk + st * Load::BYTES, sv + st * Load::BYTES, nullptr, t * BN, (t + 1) * BN > all, careful, lane, tl);
+        multiply(t, st);
       }
     } else {
       typename Load::Held kt, vt;
       auto fetch = [&](int t) {
-        Load::fetch(a, a.k, a.k_scale, hk, t * BN, sc.len, entries, wave, lane, kt);
-        Load::fetch(a, a.v, a.v_scale, hk, t * BN, sc.len, entries, wave, lane, vt);
-        entries = Load::look(a, b, (t + 1) * BN, lane);
+        const typename Load::Where at(a, hk, entry, t * BN, sc.len, lane);
+        entry = Load::look(a, b, (t + 1) * BN, lane);
+        Load::fetch(a, keys, a.k_scale, at, wave, lane, kt);
+        Load::fetch(a, values, a.v_scale, at, wave, lane, vt);
       };
       auto put = [&](int st) {
         Load::put(kt, sk + st * Load::BYTES, wave, lane);
         Load::put(vt, sv + st * Load::BYTES, wave, lane);
       };
-      if (t0 >= t1) return;
-      entries = Load::look(a, b, t0 * BN, lane);
       fetch(t0);
       put(0);
       for (int t = t0, st = 0; t < t1; ++t, st ^= 1) {
         __syncthreads();                       // tile t is written, and tile t - 1 read
         if (t + 1 < t1) fetch(t + 1);
-        w.template tile<BN / 32>(a, sk + st * Load::BYTES, sv + st * Load::BYTES, nullptr, t * BN, (t + 1) * BN > all, careful, lane, tl);
+        multiply(t, st);
         if (t + 1 < t1) put(st ^ 1);
       }
     }
   };
   pass(std::integral_constant<bool, CAREFUL>{});
   // 0 * inf of a hidden pair (or a visible one): once more, with the product that tells them apart
-  if (!CAREFUL && __syncthreads_or(not_finite(w.acc))) return true;
+  const bool bad = !CAREFUL && not_finite(w.acc);
   w.l = half_sum(w.l);
-  finish_row<T, DP, VEC>(a, w, b, hk, r, split, lane);
-  return false;
+  finish_stretch<T, DP, kFwdRows, VEC>(a, w, x, row, lane);
+  return __syncthreads_or(bad);                // and the next stretch fills the same LDS
 }
 template <class T, int DP, bool VEC, bool E4M3>
 __global__ void __launch_bounds__(256, (sizeof(T) * DP <= 256 ? 2 : 1)) k_attn_cached(const CachedArgs a) {
   extern __shared__ __align__(1024) char smem[];
-  const bool bad = cached_body<T, DP, VEC, E4M3, false>(a, smem, blockIdx.x);
+  bool bad = false;
+  each_stretch<Parts<kFwdKeys<T>, kFwdRows>, 256>(
+      a, blockIdx.x, [&](const Stretch& x) { bad |= cached_stretch<T, DP, VEC, E4M3, false>(a, smem, x); });
   if (threadIdx.x == 0) a.flags[blockIdx.x] = bad;
 }
 template <class T, int DP, bool VEC, bool E4M3>
 __global__ void __launch_bounds__(256, 1) k_attn_cached_again(const CachedArgs a, int blocks) {
   extern __shared__ __align__(1024) char smem[];
-  again(a.flags, blocks, [&](int id) { cached_body<T, DP, VEC, E4M3, true>(a, smem, id); });
+  again(a.flags, blocks, [&](int id) {
+    each_stretch<Parts<kFwdKeys<T>, kFwdRows>, 256>(a, id, [&](const Stretch& x) { cached_stretch<T, DP, VEC, E4M3, true>(a, smem, x); });
+  });
 }
 
 // ---- few rows (at most 32 a key/value head): each wave takes every W-th tile of 32 keys through LDS of its own ------------------
@@ -303,47 +537,49 @@ template <class T, int DP, bool E4M3>
 constexpr int kCachedStages = E4M3 ? 1 : 2;     // 8 bits: the next tile is on its way in registers
 template <class T, int DP, bool E4M3>
 constexpr int kCachedWaves = kCachedKeys * DP * (int)sizeof(T) * 2 * kCachedStages<T, DP, E4M3> * 4 <= 128 * 1024 ? 4 : 2;
+template <class T, int DP, bool E4M3>
+constexpr int kCachedBytes = std::max(2 * kCachedWaves<T, DP, E4M3> * kCachedStages<T, DP, E4M3> * kCachedKeys * AttnTile<T, DP>::RB,
+                                      kJoinBytes<T, DP, kCachedWaves<T, DP, E4M3>>);
 
 template <class T, int DP, bool VEC, bool E4M3, bool CAREFUL>
-__device__ __forceinline__ bool cached_tokens_body(const CachedArgs& a, char* smem) {
+__device__ __forceinline__ bool tokens_stretch(const CachedArgs& a, char* smem, const Stretch& x) {
   constexpr int BN = kCachedKeys, W = kCachedWaves<T, DP, E4M3>, S = kCachedStages<T, DP, E4M3>;
   using Load = PageLoad<T, DP, BN, 1, VEC, E4M3>;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   char* mine = smem + wave * 2 * S * Load::BYTES;          // [S][k, v]
-
-  int bh, split;
-  place(blockIdx.x, a.B * a.Hk, bh, split);
-  const int hk = bh % a.Hk, b = bh / a.Hk;
+  const int b = x.b, hk = x.hk, t1 = x.t1;
   const CachedScope sc(a, b);
   const int r = lane & 31;
   FwdRows<T, DP, false, E4M3> w;
   typename AttnTile<T, DP>::Lane tl(lane);
   set_row<T, DP, VEC>(a, sc, b, hk, r, lane, w);
+  const int all = sc.all(0, (a.R - 1) / a.G);
 
-  const int i_hi = (a.R - 1) / a.G, all = sc.all(0, i_hi), any = sc.any(0, i_hi);
-  const int nt = (any + BN - 1) / BN, per = (nt + a.splits - 1) / a.splits;
-  const int t0 = split * per, t1 = min(nt, t0 + per);
+  const typename Load::Head keys(a.k, hk), values(a.v, hk);
 
   auto pass = [&](auto careful) {
     w.reset();
-    int entries = 0;                           // of the tile that is read next
-    int t = t0 + wave;
+    int t = x.t0 + wave;
     if (t >= t1) return;
-    entries = Load::look(a, b, t * BN, lane);
+    // Every step brings in the wave's next tile, past its last one zeros from one address: the loads in flight are the same
+    // ones every time, and no wait is for more than it needs.  Entries are looked up a step ahead, in front of the loads that are
+    // still on their way when they are used.
+    typedef typename Load::Where Where;
+    int entry = Load::look(a, b, t * BN, lane);
+    const Where at0(a, hk, entry, t * BN, sc.len, lane);
+    entry = Load::look(a, b, (t + W) * BN, lane);
     if constexpr (!E4M3) {
-      auto issue = [&](int t, int st) {
+      auto issue = [&](const Where& at, int st) {
         char* s = mine + st * 2 * Load::BYTES;
-        Load::rows(a, a.k, hk, t * BN, sc.len, entries, s, 0, lane);
-        Load::rows(a, a.v, hk, t * BN, sc.len, entries, s + Load::BYTES, 0, lane);
+        Load::rows(a, keys, at, s, 0, lane);
+        Load::rows(a, values, at, s + Load::BYTES, 0, lane);
       };
-      issue(t, 0);
-      entries = Load::look(a, b, (t + W) * BN, lane);
+      issue(at0, 0);
       for (int st = 0; t < t1; t += W, st ^= 1) {
-        const bool more = t + W < t1;
-        if (VEC && more) {
-          const int then = Load::look(a, b, (t + 2 * W) * BN, lane);   // in front of the loads that it would wait for
-          issue(t + W, st ^ 1);
-          entries = then;
+        const Where at(a, hk, entry, (t + W) * BN, t + W < t1 ? sc.len : 0, lane);
+        entry = Load::look(a, b, (t + 2 * W) * BN, lane);
+        if constexpr (VEC) {
+          issue(at, st ^ 1);
           wait_loads<2 * Load::NI>();    // the current tile has landed; the next stays in flight
         } else {
           __builtin_amdgcn_s_waitcnt(0x0070);
@@ -355,29 +591,20 @@ __device__ __forceinline__ bool cached_tokens_body(const CachedArgs& a, char* sm
         __builtin_amdgcn_s_waitcnt(0xC07F);   // this wave's LDS reads are done: the stage may be filled again
         __builtin_amdgcn_wave_barrier();
         __builtin_amdgcn_sched_barrier(0);
-        if (!VEC && more) {
-          issue(t + W, st ^ 1);
-          entries = Load::look(a, b, (t + 2 * W) * BN, lane);
-        }
+        if constexpr (!VEC) issue(at, st ^ 1);
       }
     } else {
       typename Load::Held kt, vt;
-      Load::fetch(a, a.k, a.k_scale, hk, t * BN, sc.len, entries, 0, lane, kt);
-      Load::fetch(a, a.v, a.v_scale, hk, t * BN, sc.len, entries, 0, lane, vt);
-      entries = Load::look(a, b, (t + W) * BN, lane);
+      Load::fetch(a, keys, a.k_scale, at0, 0, lane, kt);
+      Load::fetch(a, values, a.v_scale, at0, 0, lane, vt);
       for (; t < t1; t += W) {
-        const bool more = t + W < t1;
+        const Where at(a, hk, entry, (t + W) * BN, t + W < t1 ? sc.len : 0, lane);
         // keys are on their way while values are written, and the other way round
         Load::put(kt, mine, 0, lane);
-        if (more) {
-          const int then = Load::look(a, b, (t + 2 * W) * BN, lane);   // in front of the loads that it would wait for
-          Load::fetch(a, a.k, a.k_scale, hk, (t + W) * BN, sc.len, entries, 0, lane, kt);
-          Load::put(vt, mine + Load::BYTES, 0, lane);
-          Load::fetch(a, a.v, a.v_scale, hk, (t + W) * BN, sc.len, entries, 0, lane, vt);
-          entries = then;
-        } else {
-          Load::put(vt, mine + Load::BYTES, 0, lane);
-        }
+        entry = Load::look(a, b, (t + 2 * W) * BN, lane);
+        Load::fetch(a, keys, a.k_scale, at, 0, lane, kt);
+        Load::put(vt, mine + Load::BYTES, 0, lane);
+        Load::fetch(a, values, a.v_scale, at, 0, lane, vt);
         __builtin_amdgcn_s_waitcnt(0xC07F);   // the tile is written
         __builtin_amdgcn_wave_barrier();
         __builtin_amdgcn_sched_barrier(0);
@@ -387,33 +614,37 @@ __device__ __forceinline__ bool cached_tokens_body(const CachedArgs& a, char* sm
         __builtin_amdgcn_sched_barrier(0);
       }
     }
+    // what was brought in past the end goes where the waves' states are joined: it has to have landed before
+    __builtin_amdgcn_s_waitcnt(0x0070);
   };
   pass(std::integral_constant<bool, CAREFUL>{});
   if (!CAREFUL && __syncthreads_or(not_finite(w.acc))) return true;
   w.l = half_sum(w.l);
-  if (join_waves<T, DP, W>(a, w, smem, wave, lane)) finish_row<T, DP, VEC>(a, w, b, hk, r, split, lane);
+  if (join_waves<T, DP, W>(a, w, smem, wave, lane)) finish_stretch<T, DP, 32, VEC>(a, w, x, r, lane);
+  __syncthreads();                             // the next stretch fills the same LDS
   return false;
 }
 template <class T, int DP, bool VEC, bool E4M3>
 __global__ void __launch_bounds__((64 * kCachedWaves<T, DP, E4M3>), (E4M3 && sizeof(T) == 2 ? 2 : 1)) k_attn_cached_tokens(const CachedArgs a) {
   extern __shared__ __align__(1024) char smem[];
-  if (cached_tokens_body<T, DP, VEC, E4M3, false>(a, smem)) cached_tokens_body<T, DP, VEC, E4M3, true>(a, smem);
+  each_stretch<Parts<kCachedKeys, 32>, 64 * kCachedWaves<T, DP, E4M3>>(a, blockIdx.x, [&](const Stretch& x) {
+    if (tokens_stretch<T, DP, VEC, E4M3, false>(a, smem, x)) tokens_stretch<T, DP, VEC, E4M3, true>(a, smem, x);
+  });
 }
 
 template <class T, int DP, bool VEC, bool E4M3>
 hipError_t run_cached(hipStream_t s, const CachedArgs& a, bool tokens) {
   hipError_t e;
+  const int blocks = a.workers ? a.workers : a.B * a.Hk * a.tiles;
   if (tokens) {
-    constexpr int W = kCachedWaves<T, DP, E4M3>;
-    constexpr int bytes = std::max(2 * W * kCachedStages<T, DP, E4M3> * kCachedKeys * AttnTile<T, DP>::RB, kJoinBytes<T, DP, W>);
+    constexpr int bytes = kCachedBytes<T, DP, E4M3>;
     e = hipFuncSetAttribute((const void*)k_attn_cached_tokens<T, DP, VEC, E4M3>, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
     if (e != hipSuccess) return e;
-    k_attn_cached_tokens<T, DP, VEC, E4M3><<<dim3(a.B * a.Hk * a.splits), dim3(64 * W), bytes, s>>>(a);
+    k_attn_cached_tokens<T, DP, VEC, E4M3><<<dim3(blocks), dim3(64 * kCachedWaves<T, DP, E4M3>), bytes, s>>>(a);
   } else {
     constexpr int bytes = 4 * kFwdKeys<T> * AttnTile<T, DP>::RB;
     e = hipFuncSetAttribute((const void*)k_attn_cached<T, DP, VEC, E4M3>, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
     if (e != hipSuccess) return e;
-    const int blocks = a.B * a.Hk * a.tiles * a.splits;
     k_attn_cached<T, DP, VEC, E4M3><<<dim3(blocks), dim3(256), bytes, s>>>(a);
     e = hipGetLastError();
     if (e != hipSuccess) return e;
@@ -422,8 +653,11 @@ hipError_t run_cached(hipStream_t s, const CachedArgs& a, bool tokens) {
     k_attn_cached_again<T, DP, VEC, E4M3><<<dim3(std::min(blocks, kAgainBlocks)), dim3(256), bytes, s>>>(a, blocks);
   }
   e = hipGetLastError();
-  if (e == hipSuccess && a.splits > 1) {
-    k_attn_join<T, DP><<<dim3(a.B * a.Hk * a.R), dim3(DP), 0, s>>>(a);
+  if (e == hipSuccess && a.workers) {
+    if (tokens)
+      k_cached_join<T, DP, 32><<<dim3(a.workers), dim3(256), 0, s>>>(a);
+    else
+      k_cached_join<T, DP, kFwdRows><<<dim3(a.workers * (kFwdRows / 32)), dim3(256), 0, s>>>(a);
     e = hipGetLastError();
   }
   return e;

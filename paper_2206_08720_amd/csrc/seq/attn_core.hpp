@@ -254,8 +254,8 @@ struct AttnTile {
         typedef __attribute__((address_space(3))) s16x4 L;
 #pragma unroll
         for (int db = 0; db < DP / 32; ++db) {
-          const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((L*)(a[db][0] + ROW * RB));
-          const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((L*)(a[db][1] + ROW * RB));
+          const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((L*)(uintptr_t)(a[db][0] + ROW * RB));
+          const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((L*)(uintptr_t)(a[db][1] + ROW * RB));
           typedef short s16x8 __attribute__((ext_vector_type(8)));
           const s16x8 w = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
           f[db] = __builtin_bit_cast(Frag, w);

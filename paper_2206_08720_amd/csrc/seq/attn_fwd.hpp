@@ -42,25 +42,23 @@ struct FwdRows {
     for (int t = 0; t < KT; ++t) s = N::template product<Careful::value>(Tile::rows(sk, 32 * nb, t, tl), q[t], s);
     finish_scores<Careful>(a, nb, key0, ids, masked, lane, s, vis);
   }
-  // All products of a tile before the first of their scores is used, four operands read ahead.
+  // All products of a tile before the first of their scores is used, four operands read ahead (left to itself the compiler
+  // waits for each operand where it is used: 16 trips to LDS in a row).
   template <int NB>
   __device__ __forceinline__ void products_early(const char* sk, const typename Tile::Lane& tl, f32x16 (&s)[NB]) const {
+    constexpr int N_OPS = KT * NB, AHEAD = sizeof(T) == 2 ? 4 : 1;
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb) zero16(s[nb]);
+    Frag f[AHEAD];
 #pragma unroll
-    for (int t = 0; t < KT; ++t)
+    for (int i = 0; i < AHEAD; ++i) f[i] = Tile::rows(sk, 32 * (i % NB), i / NB, tl);
 #pragma unroll
-      for (int nb = 0; nb < NB; ++nb) s[nb] = N::template product<false>(Tile::rows(sk, 32 * nb, t, tl), q[t], s[nb]);
-    if constexpr (sizeof(T) == 2) {
-      constexpr int DS = 0x100, MFMA = 8, AHEAD = 4;
-      __builtin_amdgcn_sched_group_barrier(DS, AHEAD, 0);
-#pragma unroll
-      for (int i = 0; i < KT * NB - AHEAD; ++i) {
-        __builtin_amdgcn_sched_group_barrier(MFMA, 1, 0);
-        __builtin_amdgcn_sched_group_barrier(DS, 1, 0);
-      }
-      __builtin_amdgcn_sched_group_barrier(MFMA, AHEAD, 0);
+    for (int i = 0; i < N_OPS; ++i) {
+      __builtin_amdgcn_sched_barrier(6);       // arithmetic may pass, reads and products not
+      s[i % NB] = N::template product<false>(f[i % AHEAD], q[i / NB], s[i % NB]);
+      if (i + AHEAD < N_OPS) f[i % AHEAD] = Tile::rows(sk, 32 * ((i + AHEAD) % NB), (i + AHEAD) / NB, tl);
     }
+    __builtin_amdgcn_sched_barrier(6);
   }
   template <class Careful>
   __device__ __forceinline__ void finish_scores(const AttnArgs& a, int nb, int key0, const int* ids, bool masked, int lane, f32x16& s,

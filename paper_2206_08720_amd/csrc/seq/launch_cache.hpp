@@ -32,7 +32,14 @@ hipError_t launch_append(hipStream_t s, int dtype, const AppendArgs& a, bool vec
 
 // Attention over a cache (kernels_cached.hip; kernels_cached_e4m3.hip for a cache in 8 bits).
 struct CachedArgs;
-AttnPlan attn_plan_cached(int dtype, bool e4m3, int B, int Hk, int R, int places, int D);
+// `tokens`: the few-row kernel; `tiles` row tiles a key/value head; the tiles of keys are dealt out to `workers` workgroups, each at least
+// `least` of them (0: a workgroup a row tile, `blocks` in all).  Workspace: part_floats, then 4 ints a worker, then a flag a workgroup.
+struct CachedPlan {
+  bool tokens;
+  int tiles, workers, least;
+  long long blocks, part_floats, ints;
+};
+CachedPlan attn_plan_cached(int dtype, bool e4m3, int B, int Hk, int R, int places, int D);
 hipError_t launch_attn_cached(hipStream_t s, int dtype, const CachedArgs& a, bool tokens, bool vec);
 hipError_t launch_attn_cached_e4m3(hipStream_t s, int dtype, const CachedArgs& a, bool tokens, bool vec);
 

@@ -19,6 +19,18 @@ struct PageTable {
   }
 };
 
+// How WAVES waves bring a tile of rows of CH 16-byte chunks in, 64 chunks an instruction: instruction i of a wave takes the rows from
+// first() on.  Pages hold at least 8 places and tiles start on multiples of 32, so that the eight rows from a multiple of 8 lie side by
+// side in one page: a row is `row % 8` slots behind the one that group() names.
+template <int CH, int WAVES>
+struct TilePlaces {
+  static constexpr int RPI = 64 / CH;                           // rows an instruction: at most 16
+  static_assert(RPI >= 1 && RPI <= 16, "an instruction takes rows of two groups at most");
+  __host__ __device__ static __forceinline__ int first(int i, int wave) { return (i * WAVES + wave) * RPI; }
+  __host__ __device__ static __forceinline__ int row(int i, int wave, int lane) { return first(i, wave) + lane / CH; }
+  __host__ __device__ static __forceinline__ int group(int row0, int lane) { return (row0 & ~7) + (RPI == 16 ? lane / CH & 8 : 0); }
+};
+
 // The tokens that an append adds to one sequence: positions first .. first + count - 1.
 struct AppendSpan {
   int first, count;

@@ -53,8 +53,8 @@ bool apart(const ntk_view* v, int batch, int positions, int heads, int dim) {
 }
 bool same_place(const ntk_view* a, const ntk_view* b) { return a->data == b->data; }
 
-// Checks a descriptor for the pass asked for; `plan` as the forward pass runs it.  cells: the type of a cache in pages, or -1.
-int attn_args(const ntk_attention_desc* d, AttnPlan* plan, bool backward, int cells = -1) {
+// Checks a descriptor for the pass asked for; `plan` as the forward pass runs it.  `cached`: over pages, which has a plan of its own.
+int attn_args(const ntk_attention_desc* d, AttnPlan* plan, bool backward, bool cached = false) {
   if (!d) return bad(NTK_E_ARG, "attention: the descriptor is NULL");
   if (!type_ok(d->dtype)) return bad(NTK_E_ARG, "attention: dtype");
   if (d->batch < 0 || d->q_len < 0 || d->k_len < 0) return bad(NTK_E_ARG, "attention: batch, q_len or k_len < 0");
@@ -72,9 +72,9 @@ int attn_args(const ntk_attention_desc* d, AttnPlan* plan, bool backward, int ce
   const long long G = d->heads / d->kv_heads, R = (long long)d->q_len * G, bh = (long long)d->batch * d->kv_heads;
   if (R >= (1LL << 29) - 1024 || d->k_len >= (1LL << 31) - 1024 || bh >= (1LL << 31))
     return bad(NTK_E_UNSUPPORTED, "attention: q_len * group reaches 2^29 or k_len 2^31");
+  if (cached) return NTK_OK;
   if (R > 0 && bh > 0) {
-    *plan = cells < 0 ? attn_plan_fwd(d->dtype, d->batch, d->kv_heads, (int)R, d->k_len, d->head_dim)
-                      : attn_plan_cached(d->dtype, cells == NTK_E4M3, d->batch, d->kv_heads, (int)R, d->k_len, d->head_dim);
+    *plan = attn_plan_fwd(d->dtype, d->batch, d->kv_heads, (int)R, d->k_len, d->head_dim);
     const int dp = d->head_dim <= 64 ? 64 : 128;
     const long long rows = bh * R, keys = bh * d->k_len, spr = 256 / (dp / 4);   // rows a workgroup of the ranges' sums
     bool fits;
@@ -477,24 +477,29 @@ extern "C" int ntk_cache_append(int dtype, int batch, int length, int q_heads, c
 
 namespace {
 
-int cached_args(const ntk_attention_desc* d, int cells, AttnPlan* plan) {
+int cached_args(const ntk_attention_desc* d, int cells, CachedPlan* plan) {
   if (!d) return bad(NTK_E_ARG, "attention_cached: the descriptor is NULL");
   if (cells != NTK_E4M3 && cells != d->dtype) return bad(NTK_E_ARG, "attention_cached: the cache's dtype is the call's or NTK_E4M3");
   if (d->prefix || d->docs) return bad(NTK_E_ARG, "attention_cached: prefix and docs must be NULL");
-  return attn_args(d, plan, false, cells);
+  if (int rc = attn_args(d, nullptr, false, true)) return rc;
+  *plan = CachedPlan{};
+  if (d->batch == 0 || d->q_len == 0) return NTK_OK;
+  *plan = attn_plan_cached(d->dtype, cells == NTK_E4M3, d->batch, d->kv_heads, d->q_len * (d->heads / d->kv_heads), d->k_len, d->head_dim);
+  if (!grid_ok(plan->blocks, 256)) return bad(NTK_E_UNSUPPORTED, "attention_cached: too many rows for one launch");
+  return NTK_OK;
 }
 
 }  // namespace
 
 extern "C" long long ntk_attention_cached_workspace(const ntk_attention_desc* desc, int cache_dtype) {
-  AttnPlan plan;
+  CachedPlan plan;
   if (int rc = cached_args(desc, cache_dtype, &plan)) return rc;
-  return (plan.part_floats + plan.flag_ints) * 4;
+  return (plan.part_floats + plan.ints) * 4;
 }
 
 extern "C" int ntk_attention_cached(const ntk_attention_desc* desc, const ntk_cache* cache, const int* q_lens, const ntk_view* q,
                                     const ntk_view* o, float* lse, void* workspace, long long workspace_bytes, void* hip_stream) {
-  AttnPlan plan;
+  CachedPlan plan;
   if (!cache) return bad(NTK_E_ARG, "attention_cached: the cache is NULL");
   if (int rc = cached_args(desc, cache->dtype, &plan)) return rc;
   if (int rc = cache_args(cache, desc->dtype, desc->batch, "attention_cached")) return rc;
@@ -506,7 +511,7 @@ extern "C" int ntk_attention_cached(const ntk_attention_desc* desc, const ntk_ca
   if (!view_ok(q, e) || !view_ok(o, e)) return bad(NTK_E_ARG, "attention_cached: a view is missing, unaligned or has a negative stride");
   if (!desc->k_lens || !aligned(desc->k_lens, 4) || !aligned(q_lens, 4) || !aligned(lse, 4) || !aligned(desc->slopes, 4))
     return bad(NTK_E_ARG, "attention_cached: k_lens is NULL, or a pointer is not aligned to its type");
-  const long long need = (plan.part_floats + plan.flag_ints) * 4;
+  const long long need = (plan.part_floats + plan.ints) * 4;
   if (need && (!workspace || !whole16(workspace) || workspace_bytes < need))
     return bad(NTK_E_ARG, "attention_cached: the workspace is missing, unaligned or too small");
   if (!apart(o, desc->batch, desc->q_len, desc->heads, desc->head_dim) || same_place(o, q) ||
@@ -520,9 +525,9 @@ extern "C" int ntk_attention_cached(const ntk_attention_desc* desc, const ntk_ca
   if (cache->pages > 0) {
     set_view(a.k, &cache->k);
     set_view(a.v, &cache->v);
-    // a lane's offset within eight rows of a page is a 32-bit one
-    vec = vec && view_vec(&cache->k, e4m3 ? 1 : e) && view_vec(&cache->v, e4m3 ? 1 : e) && cache->k.stride_position < (1LL << 26) &&
-          cache->v.stride_position < (1LL << 26);
+    const long long wide = (1LL << 31) / (e4m3 ? 1 : e) / cache->page_size;   // offsets within a page have 32 bits
+    vec = vec && view_vec(&cache->k, e4m3 ? 1 : e) && view_vec(&cache->v, e4m3 ? 1 : e) && cache->k.stride_position < wide &&
+          cache->v.stride_position < wide;
   }
   a.k_scale = cache->k_scale;
   a.v_scale = cache->v_scale;
@@ -530,9 +535,11 @@ extern "C" int ntk_attention_cached(const ntk_attention_desc* desc, const ntk_ca
   a.pages = page_table(cache);
   a.lse = lse;
   a.part = (float*)workspace;
-  a.flags = (int*)workspace + plan.part_floats;
+  a.heads = (int*)workspace + plan.part_floats;
+  a.flags = a.heads + 4LL * plan.workers;
   a.tiles = plan.tiles;
-  a.splits = plan.splits;
+  a.workers = plan.workers;
+  a.least = plan.least;
   const hipError_t err = e4m3 ? launch_attn_cached_e4m3((hipStream_t)hip_stream, desc->dtype, a, plan.tokens, vec)
                               : launch_attn_cached((hipStream_t)hip_stream, desc->dtype, a, plan.tokens, vec);
   return err == hipSuccess ? NTK_OK : hip_bad(err);

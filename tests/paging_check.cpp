@@ -16,7 +16,39 @@ static int fail(const char* what, long long x) {
   return 1;
 }
 
+// Every row of a tile once, at its own slot and in its group's page.
+template <int CH, int WAVES>
+static int check_tile(int rows) {
+  using At = TilePlaces<CH, WAVES>;
+  const int ni = (rows * CH + 64 * WAVES - 1) / (64 * WAVES);
+  for (int shift = 3; shift <= 10; ++shift) {
+    PageTable t;
+    t.shift = shift;
+    for (int tile0 = 0; tile0 < 4096; tile0 += 32) {
+      std::vector<int> seen((size_t)ni * 64 * WAVES / CH, 0);
+      for (int i = 0; i < ni; ++i)
+        for (int wave = 0; wave < WAVES; ++wave)
+          for (int lane = 0; lane < 64; ++lane) {
+            const int row = At::row(i, wave, lane), g = At::group(At::first(i, wave), lane);
+            if (g % 8 || row < g || row >= g + 8) return fail("group", row);
+            if ((tile0 + g) >> shift != (tile0 + row) >> shift) return fail("two pages", row);
+            if (t.slot(tile0 + g) + row % 8 != t.slot(tile0 + row)) return fail("slot of a row", row);
+            // the lane whose look() has the group, and what an instruction reads it by
+            const int by = At::RPI <= 8 || lane < 32 ? At::first(i, wave) / 8 : At::first(i, wave) / 8 + 1;
+            if (by * 8 != g) return fail("entry of a row", row);
+            ++seen[row];
+          }
+      for (int n : seen)
+        if (n != CH) return fail("chunks of a row", n);
+    }
+  }
+  return 0;
+}
+
 int main() {
+  if (check_tile<4, 1>(32) || check_tile<4, 4>(64) || check_tile<4, 4>(32) || check_tile<8, 1>(32) || check_tile<8, 4>(64) || check_tile<8, 4>(32) ||
+      check_tile<16, 1>(32) || check_tile<16, 4>(64) || check_tile<16, 4>(32) || check_tile<32, 1>(32) || check_tile<32, 4>(32))
+    return 1;
   std::mt19937 rng(7);
   for (int trial = 0; trial < 4000; ++trial) {
     PageTable t;
