@@ -1,0 +1,10 @@
+// kernels_cached_f16.hip -- attention over a cache of pages for queries in fp16, the cache in fp16 or in 8 bits.
+#include "seq/attn_cached.hpp"
+
+namespace ntk {
+
+hipError_t launch_attn_cached_f16(hipStream_t s, const CachedArgs& a, bool e4m3, int waves, bool vec) {
+  return run_cached_type<_Float16>(s, a, e4m3, waves, vec);
+}
+
+}  // namespace ntk

@@ -1,4 +1,4 @@
-// attn_cached.hpp -- attention over a cache of pages (kernels_cached.hip, kernels_cached_e4m3.hip).
+// attn_cached.hpp -- attention over a cache of pages (kernels_cached_bf16.hip, _f16, _f32).
 //
 // The forward pass of kernels_attn.hip, o = softmax(mask(score(q k^T))) v with a running maximum, with keys and values read through
 // a table of pages.  What differs is how a tile comes into LDS: a row's place follows from its page, read one tile ahead, and is
@@ -396,67 +396,70 @@ __device__ __forceinline__ void finish_stretch(const CachedArgs& a, Rows& w, con
   }
 }
 
-// 32 rows of a row tile that one worker began: its sums and those of the workers behind it.
+// Rows of a row tile that one worker began: its sums and those of the workers behind it.  A thread takes four elements of a row, with
+// those of four workers in flight (a row at a time it took 18 us where 16 workers have parts of 40 rows each, and takes 8 this way).
+template <int DP, int ROWS>
+struct JoinShape {
+  static constexpr int LANES = DP / 4, BLOCK_ROWS = 256 / LANES, PARTS = ROWS / BLOCK_ROWS, DEPTH = 4;
+};
 template <class T, int DP, int ROWS>
 __global__ void __launch_bounds__(256) k_cached_join(const CachedArgs a) {
-  constexpr int LANES = DP / 4, AT_ONCE = 256 / LANES;
-  const int w = blockIdx.x / (ROWS / 32), part = blockIdx.x % (ROWS / 32);
+  using S = JoinShape<DP, ROWS>;
+  const int w = blockIdx.x / S::PARTS, row = blockIdx.x % S::PARTS * S::BLOCK_ROWS + threadIdx.x / S::LANES;
   const int pair = a.heads[4 * w], hk = a.heads[4 * w + 1], behind = a.heads[4 * w + 2];
   if (behind == 0) return;
-  const int b = pair / a.tiles, mt = pair - b * a.tiles, d = threadIdx.x % LANES * 4;
+  const int b = pair / a.tiles, mt = pair - b * a.tiles, d = threadIdx.x % S::LANES * 4, r = mt * ROWS + row;
+  if (r >= a.R) return;
   const float* ml = a.part + (long long)a.workers * 2 * ROWS * DP;
-#pragma unroll 1
-  for (int row = part * 32 + threadIdx.x / LANES; row < part * 32 + 32; row += AT_ONCE) {
-    const int r = mt * ROWS + row;
-    if (r >= a.R) return;
-    float m = -__builtin_inff(), l = 0.f;
-    f32x4 o = {0.f, 0.f, 0.f, 0.f};
-    for (int s0 = 0; s0 <= behind; s0 += 4) {                    // four stretches' numbers in flight at a time
-      float ms[4], ls[4];
-      f32x4 os[4];
+  float m = -__builtin_inff(), l = 0.f;
+  f32x4 o = {0.f, 0.f, 0.f, 0.f};
+  for (int s0 = 0; s0 <= behind; s0 += S::DEPTH) {
+    float ms[S::DEPTH], ls[S::DEPTH];
+    f32x4 os[S::DEPTH];
 #pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        const int x = min(s0 + u, behind), slot = x == 0 ? 2 * w + 1 : 2 * (w + x);
-        const long long at = (long long)slot * ROWS + row;
-        ms[u] = s0 + u <= behind ? ml[at * 2] : -__builtin_inff();
-        ls[u] = ml[at * 2 + 1];
-        os[u] = *reinterpret_cast<const f32x4*>(a.part + at * DP + d);
-      }
-#pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        if (s0 + u > behind) break;
-        const float mn = fmaxf(m, ms[u]);
-        const float f = m == mn ? 1.f : exp2_hw(m - mn), g = ms[u] == mn ? 1.f : exp2_hw(ms[u] - mn);
-        l = l * f + ls[u] * g;
-#pragma unroll
-        for (int k = 0; k < 4; ++k) o[k] = o[k] * f + os[u][k] * g;
-        m = mn;
-      }
+    for (int u = 0; u < S::DEPTH; ++u) {
+      const int x = min(s0 + u, behind), slot = x == 0 ? 2 * w + 1 : 2 * (w + x);
+      const long long at = (long long)slot * ROWS + row;
+      ms[u] = s0 + u <= behind ? ml[at * 2] : -__builtin_inff();
+      ls[u] = ml[at * 2 + 1];
+      os[u] = *reinterpret_cast<const f32x4*>(a.part + at * DP + d);
     }
-    const int i = (int)a.gdiv.div((uint32_t)r), head = hk * a.G + r - i * a.G;
-    T* out = (T*)a.o.p + b * a.o.sb + i * a.o.ss + head * a.o.sh;
 #pragma unroll
-    for (int k = 0; k < 4; ++k)
-      if (d + k < a.D) out[d + k] = (T)(l == 0.f ? 0.f : o[k] / l);
-    if (a.lse && d == 0)
-      a.lse[((long long)b * a.H + head) * a.Sq + i] = l == 0.f ? -__builtin_inff() : m * kLn2 + logf(l * kWeightOne<T>);
+    for (int u = 0; u < S::DEPTH; ++u) {                         // no branch: it would have the loads behind it wait
+      const float mn = fmaxf(m, ms[u]), there = s0 + u <= behind ? 1.f : 0.f;
+      const float f = m == mn ? 1.f : exp2_hw(m - mn), g = there * (ms[u] == mn ? 1.f : exp2_hw(ms[u] - mn));
+      l = l * f + ls[u] * g;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) o[k] = o[k] * f + os[u][k] * g;
+      m = mn;
+    }
   }
+  const int i = (int)a.gdiv.div((uint32_t)r), head = hk * a.G + r - i * a.G;
+  T* out = (T*)a.o.p + b * a.o.sb + i * a.o.ss + head * a.o.sh;
+#pragma unroll
+  for (int k = 0; k < 4; ++k)
+    if (d + k < a.D) out[d + k] = (T)(l == 0.f ? 0.f : o[k] / l);
+  if (a.lse && d == 0)
+    a.lse[((long long)b * a.H + head) * a.Sq + i] = l == 0.f ? -__builtin_inff() : m * kLn2 + logf(l * kWeightOne<T>);
 }
 
-// ---- many rows: four waves of 32 rows share the key tiles in two LDS stages -------------------------------------------------
-template <class T, int DP, bool VEC, bool E4M3, bool CAREFUL>
+// ---- many rows: NW waves of 32 rows share the key tiles in two LDS stages ----------------------------------------------------
+// Bound by two waves a SIMD that take turns at the matrix cores and at the exponentials, as in kernels_attn.hip; in 8 bits with eight waves a
+// workgroup, so that what a tile takes to bring in and to convert is shared by 256 rows (bf16, parts of 1212 and 1839 queries over 14187 and
+// 8463 places, 32 heads over 8 of 128: 691 us, 720 TFLOP/s; 750 with four waves, of which bringing in takes 110 and converting 70).
+template <class T, int DP, int NW, bool VEC, bool E4M3, bool CAREFUL>
 __device__ __forceinline__ bool cached_stretch(const CachedArgs& a, char* smem, const Stretch& x) {
   constexpr int BN = kFwdKeys<T>;
-  using Load = PageLoad<T, DP, BN, 4, VEC, E4M3>;
+  using Load = PageLoad<T, DP, BN, NW, VEC, E4M3>;
   char* sk = smem;                                  // [2][BN][DP]
   char* sv = smem + 2 * Load::BYTES;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int b = x.b, hk = x.hk, t0 = x.t0, t1 = x.t1;
   const CachedScope sc(a, b);
-  const int row = wave * 32 + (lane & 31), r0 = x.mt * kFwdRows + wave * 32;
+  const int row = wave * 32 + (lane & 31), r0 = x.mt * (32 * NW) + wave * 32;
   FwdRows<T, DP, false, E4M3> w;
   typename AttnTile<T, DP>::Lane tl(lane);
-  set_row<T, DP, VEC>(a, sc, b, hk, x.mt * kFwdRows + row, lane, w);
+  set_row<T, DP, VEC>(a, sc, b, hk, x.mt * (32 * NW) + row, lane, w);
 
   // keys that all of this wave's rows see, that some row sees
   const int i_lo = (int)a.gdiv.div((uint32_t)min(r0, a.R - 1)), i_hi = (int)a.gdiv.div((uint32_t)(min(r0 + 32, a.R) - 1));
@@ -512,22 +515,22 @@ __device__ __forceinline__ bool cached_stretch(const CachedArgs& a, char* smem, 
   // 0 * inf of a hidden pair (or a visible one): once more, with the product that tells them apart
   const bool bad = !CAREFUL && not_finite(w.acc);
   w.l = half_sum(w.l);
-  finish_stretch<T, DP, kFwdRows, VEC>(a, w, x, row, lane);
+  finish_stretch<T, DP, 32 * NW, VEC>(a, w, x, row, lane);
   return __syncthreads_or(bad);                // and the next stretch fills the same LDS
 }
-template <class T, int DP, bool VEC, bool E4M3>
-__global__ void __launch_bounds__(256, (sizeof(T) * DP <= 256 ? 2 : 1)) k_attn_cached(const CachedArgs a) {
+template <class T, int DP, int NW, bool VEC, bool E4M3>
+__global__ void __launch_bounds__(64 * NW, (sizeof(T) * DP <= 256 ? 2 : 1)) k_attn_cached(const CachedArgs a) {
   extern __shared__ __align__(1024) char smem[];
   bool bad = false;
-  each_stretch<Parts<kFwdKeys<T>, kFwdRows>, 256>(
-      a, blockIdx.x, [&](const Stretch& x) { bad |= cached_stretch<T, DP, VEC, E4M3, false>(a, smem, x); });
+  each_stretch<Parts<kFwdKeys<T>, 32 * NW>, 64 * NW>(
+      a, blockIdx.x, [&](const Stretch& x) { bad |= cached_stretch<T, DP, NW, VEC, E4M3, false>(a, smem, x); });
   if (threadIdx.x == 0) a.flags[blockIdx.x] = bad;
 }
-template <class T, int DP, bool VEC, bool E4M3>
-__global__ void __launch_bounds__(256, 1) k_attn_cached_again(const CachedArgs a, int blocks) {
+template <class T, int DP, int NW, bool VEC, bool E4M3>
+__global__ void __launch_bounds__(64 * NW, 1) k_attn_cached_again(const CachedArgs a, int blocks) {
   extern __shared__ __align__(1024) char smem[];
   again(a.flags, blocks, [&](int id) {
-    each_stretch<Parts<kFwdKeys<T>, kFwdRows>, 256>(a, id, [&](const Stretch& x) { cached_stretch<T, DP, VEC, E4M3, true>(a, smem, x); });
+    each_stretch<Parts<kFwdKeys<T>, 32 * NW>, 64 * NW>(a, id, [&](const Stretch& x) { cached_stretch<T, DP, NW, VEC, E4M3, true>(a, smem, x); });
   });
 }
 
@@ -632,47 +635,52 @@ __global__ void __launch_bounds__((64 * kCachedWaves<T, DP, E4M3>), (E4M3 && siz
   });
 }
 
-template <class T, int DP, bool VEC, bool E4M3>
-hipError_t run_cached(hipStream_t s, const CachedArgs& a, bool tokens) {
-  hipError_t e;
-  const int blocks = a.workers ? a.workers : a.B * a.Hk * a.tiles;
-  if (tokens) {
-    constexpr int bytes = kCachedBytes<T, DP, E4M3>;
-    e = hipFuncSetAttribute((const void*)k_attn_cached_tokens<T, DP, VEC, E4M3>, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+template <class T, int DP, int NW, bool VEC, bool E4M3>
+hipError_t run_cached_tiles(hipStream_t s, const CachedArgs& a, int blocks) {
+  constexpr int bytes = 4 * kFwdKeys<T> * AttnTile<T, DP>::RB;
+  const void* kernels[2] = {(const void*)k_attn_cached<T, DP, NW, VEC, E4M3>, (const void*)k_attn_cached_again<T, DP, NW, VEC, E4M3>};
+  for (const void* k : kernels) {
+    const hipError_t e = hipFuncSetAttribute(k, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
     if (e != hipSuccess) return e;
-    k_attn_cached_tokens<T, DP, VEC, E4M3><<<dim3(blocks), dim3(64 * kCachedWaves<T, DP, E4M3>), bytes, s>>>(a);
-  } else {
-    constexpr int bytes = 4 * kFwdKeys<T> * AttnTile<T, DP>::RB;
-    e = hipFuncSetAttribute((const void*)k_attn_cached<T, DP, VEC, E4M3>, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
-    if (e != hipSuccess) return e;
-    k_attn_cached<T, DP, VEC, E4M3><<<dim3(blocks), dim3(256), bytes, s>>>(a);
-    e = hipGetLastError();
-    if (e != hipSuccess) return e;
-    e = hipFuncSetAttribute((const void*)k_attn_cached_again<T, DP, VEC, E4M3>, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
-    if (e != hipSuccess) return e;
-    k_attn_cached_again<T, DP, VEC, E4M3><<<dim3(std::min(blocks, kAgainBlocks)), dim3(256), bytes, s>>>(a, blocks);
   }
+  k_attn_cached<T, DP, NW, VEC, E4M3><<<dim3(blocks), dim3(64 * NW), bytes, s>>>(a);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  k_attn_cached_again<T, DP, NW, VEC, E4M3><<<dim3(std::min(blocks, kAgainBlocks)), dim3(64 * NW), bytes, s>>>(a, blocks);
   e = hipGetLastError();
   if (e == hipSuccess && a.workers) {
-    if (tokens)
-      k_cached_join<T, DP, 32><<<dim3(a.workers), dim3(256), 0, s>>>(a);
-    else
-      k_cached_join<T, DP, kFwdRows><<<dim3(a.workers * (kFwdRows / 32)), dim3(256), 0, s>>>(a);
+    k_cached_join<T, DP, 32 * NW><<<dim3(a.workers * JoinShape<DP, 32 * NW>::PARTS), dim3(256), 0, s>>>(a);
+    e = hipGetLastError();
+  }
+  return e;
+}
+
+template <class T, int DP, bool VEC, bool E4M3>
+hipError_t run_cached(hipStream_t s, const CachedArgs& a, int waves) {
+  const int blocks = a.workers ? a.workers : a.B * a.Hk * a.tiles;
+  if constexpr (cached_wide(sizeof(T), E4M3))
+    if (waves == 8) return run_cached_tiles<T, DP, 8, VEC, E4M3>(s, a, blocks);
+  if (waves) return run_cached_tiles<T, DP, 4, VEC, E4M3>(s, a, blocks);
+  constexpr int bytes = kCachedBytes<T, DP, E4M3>;
+  hipError_t e = hipFuncSetAttribute((const void*)k_attn_cached_tokens<T, DP, VEC, E4M3>, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+  if (e != hipSuccess) return e;
+  k_attn_cached_tokens<T, DP, VEC, E4M3><<<dim3(blocks), dim3(64 * kCachedWaves<T, DP, E4M3>), bytes, s>>>(a);
+  e = hipGetLastError();
+  if (e == hipSuccess && a.workers) {
+    k_cached_join<T, DP, 32><<<dim3(a.workers * JoinShape<DP, 32>::PARTS), dim3(256), 0, s>>>(a);
     e = hipGetLastError();
   }
   return e;
 }
 
 template <class T, bool E4M3>
-hipError_t run_cached_dim(hipStream_t s, const CachedArgs& a, bool tokens, bool vec) {
-  if (a.D <= 64) return vec ? run_cached<T, 64, true, E4M3>(s, a, tokens) : run_cached<T, 64, false, E4M3>(s, a, tokens);
-  return vec ? run_cached<T, 128, true, E4M3>(s, a, tokens) : run_cached<T, 128, false, E4M3>(s, a, tokens);
+hipError_t run_cached_dim(hipStream_t s, const CachedArgs& a, int waves, bool vec) {
+  if (a.D <= 64) return vec ? run_cached<T, 64, true, E4M3>(s, a, waves) : run_cached<T, 64, false, E4M3>(s, a, waves);
+  return vec ? run_cached<T, 128, true, E4M3>(s, a, waves) : run_cached<T, 128, false, E4M3>(s, a, waves);
 }
-template <bool E4M3>
-hipError_t run_cached_type(hipStream_t s, int dtype, const CachedArgs& a, bool tokens, bool vec) {
-  if (dtype == 1) return run_cached_dim<__bf16, E4M3>(s, a, tokens, vec);
-  if (dtype == 2) return run_cached_dim<_Float16, E4M3>(s, a, tokens, vec);
-  return run_cached_dim<float, E4M3>(s, a, tokens, vec);
+template <class T>
+hipError_t run_cached_type(hipStream_t s, const CachedArgs& a, bool e4m3, int waves, bool vec) {
+  return e4m3 ? run_cached_dim<T, true>(s, a, waves, vec) : run_cached_dim<T, false>(s, a, waves, vec);
 }
 
 }  // namespace

@@ -143,6 +143,7 @@ struct FwdRows {
         sum += s[nb][v];
       }
     l += sum;
+    if constexpr (EARLY) __builtin_amdgcn_s_setprio(1);   // the wave that multiplies goes first
     typename Tile::Cols vc;
     vc.set(sv, tl);
     unrolled<2 * NB>([&](auto step) {
@@ -166,6 +167,7 @@ struct FwdRows {
         });
       }
     });
+    if constexpr (EARLY) __builtin_amdgcn_s_setprio(0);
   }
 };
 

@@ -30,18 +30,21 @@ struct AppendArgs {
 long long append_blocks(const AppendArgs& a);   // workgroups, of 256 threads
 hipError_t launch_append(hipStream_t s, int dtype, const AppendArgs& a, bool vec);
 
-// Attention over a cache (kernels_cached.hip; kernels_cached_e4m3.hip for a cache in 8 bits).
+// Attention over a cache (kernels_cached.hip, the kernels in a file for each type).
 struct CachedArgs;
-// `tokens`: the few-row kernel; `tiles` row tiles a key/value head; the tiles of keys are dealt out to `workers` workgroups, each at least
+// `waves` of 32 rows a workgroup, 0: the few-row kernel; `tiles` row tiles a key/value head; the tiles of keys are dealt out to `workers` workgroups, each at least
 // `least` of them (0: a workgroup a row tile, `blocks` in all).  Workspace: part_floats, then 4 ints a worker, then a flag a workgroup.
 struct CachedPlan {
-  bool tokens;
-  int tiles, workers, least;
+  int waves, tiles, workers, least;
   long long blocks, part_floats, ints;
 };
+// whether there is a form of eight waves: what a tile of 8 bits takes to convert is then shared by 256 rows
+constexpr bool cached_wide(int type_bytes, bool e4m3) { return e4m3 && type_bytes == 2; }
 CachedPlan attn_plan_cached(int dtype, bool e4m3, int B, int Hk, int R, int places, int D);
-hipError_t launch_attn_cached(hipStream_t s, int dtype, const CachedArgs& a, bool tokens, bool vec);
-hipError_t launch_attn_cached_e4m3(hipStream_t s, int dtype, const CachedArgs& a, bool tokens, bool vec);
+hipError_t launch_attn_cached(hipStream_t s, int dtype, const CachedArgs& a, bool e4m3, int waves, bool vec);
+hipError_t launch_attn_cached_bf16(hipStream_t s, const CachedArgs& a, bool e4m3, int waves, bool vec);   // one file each
+hipError_t launch_attn_cached_f16(hipStream_t s, const CachedArgs& a, bool e4m3, int waves, bool vec);
+hipError_t launch_attn_cached_f32(hipStream_t s, const CachedArgs& a, bool e4m3, int waves, bool vec);
 
 // Log probabilities of given tokens (kernels_logprob.hip).
 struct LogprobArgs {

@@ -540,8 +540,7 @@ extern "C" int ntk_attention_cached(const ntk_attention_desc* desc, const ntk_ca
   a.tiles = plan.tiles;
   a.workers = plan.workers;
   a.least = plan.least;
-  const hipError_t err = e4m3 ? launch_attn_cached_e4m3((hipStream_t)hip_stream, desc->dtype, a, plan.tokens, vec)
-                              : launch_attn_cached((hipStream_t)hip_stream, desc->dtype, a, plan.tokens, vec);
+  const hipError_t err = launch_attn_cached((hipStream_t)hip_stream, desc->dtype, a, e4m3, plan.waves, vec);
   return err == hipSuccess ? NTK_OK : hip_bad(err);
 }
 
