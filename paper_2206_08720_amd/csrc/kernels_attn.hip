@@ -213,6 +213,39 @@ __global__ void __launch_bounds__((64 * kTokWaves<T, DP>), 1) k_attn_tokens(cons
   if (tokens_body<T, DP, VEC, false>(a, smem)) tokens_body<T, DP, VEC, true>(a, smem);
 }
 
+// ---- the ranges of a row, joined -----------------------------------------------------------------------
+template <class T, int DP>
+__global__ void __launch_bounds__(DP) k_attn_join(const AttnArgs a) {
+  const int d = threadIdx.x, r = blockIdx.x % a.R, bh = blockIdx.x / a.R, hk = bh % a.Hk, b = bh / a.Hk;
+  const long long rows = (long long)a.B * a.Hk * a.R, row = (long long)bh * a.R + r;
+  const float* ml = a.part + (long long)a.splits * rows * DP;
+  // online, eight ranges' numbers in flight at a time
+  float m = -__builtin_inff(), l = 0.f, o = 0.f;
+  for (int s0 = 0; s0 < a.splits; s0 += 8) {
+    float ms[8], ls[8], os[8];
+#pragma unroll
+    for (int u = 0; u < 8; ++u) {
+      const long long at = (long long)min(s0 + u, a.splits - 1) * rows + row;
+      ms[u] = s0 + u < a.splits ? ml[at * 2] : -__builtin_inff();
+      ls[u] = ml[at * 2 + 1];
+      os[u] = a.part[at * DP + d];
+    }
+#pragma unroll
+    for (int u = 0; u < 8; ++u) {
+      if (s0 + u >= a.splits) break;
+      const float mn = fmaxf(m, ms[u]);
+      const float f = m == mn ? 1.f : exp2_hw(m - mn), g = ms[u] == mn ? 1.f : exp2_hw(ms[u] - mn);
+      l = l * f + ls[u] * g;
+      o = o * f + os[u] * g;
+      m = mn;
+    }
+  }
+  const int i = (int)a.gdiv.div((uint32_t)r), head = hk * a.G + r - i * a.G;
+  if (d < a.D) ((T*)a.o.p)[b * a.o.sb + i * a.o.ss + head * a.o.sh + d] = (T)(l == 0.f ? 0.f : o / l);
+  if (a.lse && d == 0)
+    a.lse[((long long)b * a.H + head) * a.Sq + i] = l == 0.f ? -__builtin_inff() : m * kLn2 + logf(l * kWeightOne<T>);
+}
+
 template <class T, int DP, bool VEC>
 hipError_t run_fwd(hipStream_t s, const AttnArgs& a, bool tokens) {
   if (tokens) {

@@ -61,6 +61,20 @@ __device__ __forceinline__ u64 lane_of(u64 x, int lane) {
   return ((u64)hi << 32) | lo;
 }
 
+// x of the lane below
+__device__ __forceinline__ u64 from_below(u64 x) {
+  constexpr int WAVE_SHR1 = 0x138;
+  const uint32_t lo = __builtin_amdgcn_update_dpp(0, (int)(uint32_t)x, WAVE_SHR1, 0xf, 0xf, true);
+  const uint32_t hi = __builtin_amdgcn_update_dpp(0, (int)(uint32_t)(x >> 32), WAVE_SHR1, 0xf, 0xf, true);
+  return ((u64)hi << 32) | lo;
+}
+// how many of the first n lanes hold more than x (different numbers but for zeros)
+__device__ __forceinline__ int rank_among(u64 x, int n) {
+  int r = 0;
+  for (int j = 0; j < n; ++j) r += lane_of(x, j) > x;
+  return r;
+}
+
 // The best so far of a wave, in order: lane j holds the j-th (0: none yet).
 struct Best {
   u64 mine, last;                              // last: the one at `top` - 1, which a candidate has to beat
@@ -72,10 +86,44 @@ struct Best {
       const u64 got = lane_of(x, from);
       if (lane == from) x = 0;
       const int at = __popcll(__ballot(mine > got));
-      const u64 up = __shfl_up(mine, 1);
+      const u64 up = from_below(mine);
       mine = lane < at ? mine : lane == at ? got : up;
       last = lane_of(mine, top - 1);
     }
+  }
+  // The first candidates, U a lane (0: none).  Offered one by one, a hundred of two thousand would take a place for a while.  So the
+  // `top`-th of the lanes' own largest is found first, which is at most the `top`-th of all: mostly fewer than 64 reach it, and those
+  // are put in order at once, by how many are larger.
+  template <int U>
+  __device__ __forceinline__ void begin(const u64 (&x)[U], int top, int lane, u64* lds) {
+    u64 most = x[0];
+#pragma unroll
+    for (int u = 1; u < U; ++u) most = x[u] > most ? x[u] : most;
+    const u64 cut = lane_of(most, (int)__builtin_ctzll(__ballot(most == 0 || rank_among(most, 64) == top - 1) | 1ull << 63));
+    int n = 0;
+#pragma unroll
+    for (int u = 0; u < U; ++u) n += __popcll(__ballot(x[u] != 0 && x[u] >= cut));
+    if (n > 64) {
+#pragma unroll
+      for (int u = 0; u < U; ++u) offer(x[u], top, lane);
+      return;
+    }
+    int at = 0;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const bool in = x[u] != 0 && x[u] >= cut;
+      const u64 all = __ballot(in);
+      if (in) lds[at + __popcll(all & ((1ull << lane) - 1))] = x[u];
+      at += __popcll(all);
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    const u64 got = lane < n ? lds[lane] : 0;
+    const int place = rank_among(got, n);
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    if (lane < n) lds[place] = got;
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    mine = lane < n ? lds[lane] : 0;
+    last = lane_of(mine, top - 1);
   }
   __device__ __forceinline__ float floor_logit() const { return last ? logit_of(last) : -__builtin_inff(); }
 };
@@ -190,7 +238,17 @@ __global__ void __launch_bounds__(kThreads) k_logprobs(const LogprobArgs a) {
     sum.l += l;
     sum.s += s;
     if constexpr (TOP) {
-      if (__any(!(top < best.floor_logit()) || l != l)) {
+      if (base == g0) {
+        u64 x[kUnroll * EC];
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u) {
+          const int g = base + u * kThreads + (int)threadIdx.x, e0 = r.first(g);
+#pragma unroll
+          for (int i = 0; i < EC; ++i)
+            x[u * EC + i] = g < g1 && (unsigned)(e0 + i) < (unsigned)a.vocab ? rank_of(f[u][i], e0 + i) : 0;
+        }
+        best.begin(x, a.top, lane, bests[wave]);
+      } else if (__any(!(top < best.floor_logit()) || l != l)) {
 #pragma unroll
         for (int u = 0; u < kUnroll; ++u) {
           const int g = base + u * kThreads + (int)threadIdx.x, e0 = r.first(g);
@@ -208,9 +266,17 @@ __global__ void __launch_bounds__(kThreads) k_logprobs(const LogprobArgs a) {
   __syncthreads();
   if (wave) return;
 #pragma unroll
-  for (int w = 1; w < kWaves; ++w) {
-    sum = add(sum, sums[w], c);
-    if constexpr (TOP) best.offer(lane < a.top ? bests[w][lane] : 0, a.top, lane);
+  for (int w = 1; w < kWaves; ++w) sum = add(sum, sums[w], c);
+  if constexpr (TOP) {
+    u64 x[kWaves];
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+      const int i = w * 64 + lane, from = i / a.top;               // the waves' lists, one behind the other
+      x[w] = from < kWaves ? bests[from][i - from * a.top] : 0;
+    }
+    __shared__ u64 lds[64];
+    best = Best();
+    best.begin(x, a.top, lane, lds);
   }
   if (a.splits == 1) {
     finish<T>(a, row, sum, best.mine, lane);
@@ -240,8 +306,16 @@ __global__ void __launch_bounds__(64) k_logprobs_join(const LogprobArgs a) {
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1) sum = add(sum, Sum{__shfl_xor(sum.m, o), __shfl_xor(sum.l, o), __shfl_xor(sum.s, o)}, c);
   Best best;
-  if (a.top)
-    for (int i = 0; i < a.splits * a.top; i += 64) best.offer(i + lane < a.splits * a.top ? lists[i + lane] : 0, a.top, lane);
+  if (a.top) {
+    constexpr int U = 8;
+    __shared__ u64 lds[64];
+    const int n = a.splits * a.top;
+    u64 x[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) x[u] = u * 64 + lane < n ? lists[u * 64 + lane] : 0;
+    best.begin(x, a.top, lane, lds);
+    for (int i = U * 64; i < n; i += 64) best.offer(i + lane < n ? lists[i + lane] : 0, a.top, lane);
+  }
   finish<T>(a, row, sum, best.mine, lane);
 }
 

@@ -1,5 +1,5 @@
 // attn_fwd.hpp -- what the forward attention kernels share (kernels_attn.hip, kernels_cached.hip): a wave's 32 query rows
-// and their running softmax, the rows' results, and the sum over the ranges that a row's keys are cut into.
+// and their running softmax, the rows' results, and the sum of the states that waves have of the same rows.
 #pragma once
 #include "attn_core.hpp"
 
@@ -230,39 +230,6 @@ __device__ __forceinline__ bool join_waves(const AttnArgs& a, Rows& w, char* sme
 }
 template <class T, int DP, int W>
 constexpr int kJoinBytes = (W - 1) * (DP / 32 * 16 * 64 + 128) * 4;   // LDS it takes
-
-// ---- the ranges of a row, joined -----------------------------------------------------------------------
-template <class T, int DP>
-__global__ void __launch_bounds__(DP) k_attn_join(const AttnArgs a) {
-  const int d = threadIdx.x, r = blockIdx.x % a.R, bh = blockIdx.x / a.R, hk = bh % a.Hk, b = bh / a.Hk;
-  const long long rows = (long long)a.B * a.Hk * a.R, row = (long long)bh * a.R + r;
-  const float* ml = a.part + (long long)a.splits * rows * DP;
-  // online, eight ranges' numbers in flight at a time
-  float m = -__builtin_inff(), l = 0.f, o = 0.f;
-  for (int s0 = 0; s0 < a.splits; s0 += 8) {
-    float ms[8], ls[8], os[8];
-#pragma unroll
-    for (int u = 0; u < 8; ++u) {
-      const long long at = (long long)min(s0 + u, a.splits - 1) * rows + row;
-      ms[u] = s0 + u < a.splits ? ml[at * 2] : -__builtin_inff();
-      ls[u] = ml[at * 2 + 1];
-      os[u] = a.part[at * DP + d];
-    }
-#pragma unroll
-    for (int u = 0; u < 8; ++u) {
-      if (s0 + u >= a.splits) break;
-      const float mn = fmaxf(m, ms[u]);
-      const float f = m == mn ? 1.f : exp2_hw(m - mn), g = ms[u] == mn ? 1.f : exp2_hw(ms[u] - mn);
-      l = l * f + ls[u] * g;
-      o = o * f + os[u] * g;
-      m = mn;
-    }
-  }
-  const int i = (int)a.gdiv.div((uint32_t)r), head = hk * a.G + r - i * a.G;
-  if (d < a.D) ((T*)a.o.p)[b * a.o.sb + i * a.o.ss + head * a.o.sh + d] = (T)(l == 0.f ? 0.f : o / l);
-  if (a.lse && d == 0)
-    a.lse[((long long)b * a.H + head) * a.Sq + i] = l == 0.f ? -__builtin_inff() : m * kLn2 + logf(l * kWeightOne<T>);
-}
 
 }  // namespace
 }  // namespace ntk
