@@ -87,9 +87,7 @@ def _written(name, inputs, *outs):
     """Before arrays of the caller's are written: refused where a gradient would have to pass, and counted as a change."""
     if _recording() and _wanted(*inputs, *outs):
         raise RuntimeError(f"seq.{name} writes into its argument, which autograd does not record: an argument requires a gradient")
-    for t in outs:
-        if t is not None:
-            torch.autograd.graph.increment_version(t)
+    torch.autograd.graph.increment_version([t for t in outs if t is not None])
 
 
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda i: torch.cuda.current_stream(i).cuda_stream)
@@ -417,31 +415,40 @@ def _ints(t, name, device, shape):
 
 
 def _cache(cache, page_table, dtype, device, batch):
-    """The cache and its table as an ntk_cache."""
+    """(An ntk_cache in one array of 64-bit numbers, which is quicker than the struct; its dtype; the shape of cache.k; places of a
+    sequence.)"""
     k, v, k_scale, v_scale = cache
     cells = k.dtype if isinstance(k, torch.Tensor) else None
     if cells not in (dtype, _E4M3):
         raise TypeError(f"the cache must be of type {dtype} or {_E4M3}")
     _check(k, "cache.k", cells, ndim=4, device=device)
-    _check(v, "cache.v", cells, device=device, shape=k.shape)
-    pages, size, heads, dim = k.shape
+    shape = k.shape
+    _check(v, "cache.v", cells, device=device, shape=shape)
+    pages, size, heads, dim = shape
     if cells == _E4M3:
+        code = _lib.NTK_E4M3
         for name, t in (("cache.k_scale", k_scale), ("cache.v_scale", v_scale)):
             _check(t, name, torch.float32, device=device, shape=(pages, heads))
             if not t.is_contiguous():
                 raise ValueError(f"{name} must be contiguous")
+        scales = k_scale.data_ptr(), v_scale.data_ptr()
     elif k_scale is not None or v_scale is not None:
         raise ValueError(f"a cache of type {dtype} has no scales")
+    else:
+        code, scales = _DTYPES[cells], (0, 0)
     _check(page_table, "page_table", torch.int32, ndim=2, device=device)
-    if page_table.shape[0] != batch or not page_table.is_contiguous():
+    rows, most = page_table.shape
+    if rows != batch or not page_table.is_contiguous():
         raise ValueError(f"page_table must be a contiguous [{batch}, max_pages] tensor")
-    _sizes(pages, size, heads, dim, page_table.shape[1])
-
-    def view(t):
-        return _lib.ntk_view(t.data_ptr(), *(t.stride(i) if t.shape[i] > 1 else 0 for i in range(3)))
-
-    return _lib.ntk_cache(_lib.NTK_E4M3 if cells == _E4M3 else _DTYPES[cells], pages, size, heads, dim, view(k), view(v),
-                          _ptr(k_scale), _ptr(v_scale), page_table.data_ptr(), page_table.shape[1])
+    if pages > _MOST or most > _MOST:
+        _sizes(pages, most)
+    _sizes(size, heads, dim, most * size)
+    (kp, ks, kh, _), (vp, vs, vh, _) = k.stride(), v.stride()
+    array = (ctypes.c_longlong * 15)(
+        code | pages << 32, size | heads << 32, dim,
+        k.data_ptr(), kp if pages > 1 else 0, ks if size > 1 else 0, kh if heads > 1 else 0,
+        v.data_ptr(), vp if pages > 1 else 0, vs if size > 1 else 0, vh if heads > 1 else 0, *scales, page_table.data_ptr(), most)
+    return array, code, shape, most * size
 
 
 def cache_append(cache, page_table, lens, k, v, q=None, table=None, positions=None, new_lens=None, interleaved=False, stream=None):
@@ -470,9 +477,9 @@ def cache_append(cache, page_table, lens, k, v, q=None, table=None, positions=No
         raise TypeError("lens must be a GPU tensor of type int32")
     _ints(new_lens, "new_lens", dev, (b,))
     _ints(positions, "positions", dev, (b, n))
-    desc = _cache(cache, page_table, k.dtype, dev, b)
-    if (desc.kv_heads, desc.head_dim) != (heads, dim):
-        raise ValueError(f"the cache holds {desc.kv_heads} heads of {desc.head_dim}, k has {heads} of {dim}")
+    desc, _, held, _ = _cache(cache, page_table, k.dtype, dev, b)
+    if held[2] != heads or held[3] != dim:
+        raise ValueError(f"the cache holds {held[2]} heads of {held[3]}, k has {heads} of {dim}")
     _written("cache_append", (k, v, table), *cache)
     with _Call(k, stream, (k, v, q, table, positions, lens, new_lens, page_table, *cache)) as call:
         qo = None if q is None else _like(q)
@@ -494,10 +501,10 @@ def attention_cached(q, cache, page_table, k_lens, q_lens=None, causal=True, sof
     _check(q, "q", ndim=4)
     b, sq, heads, dim = q.shape
     dev = q.device
-    desc = _cache(cache, page_table, q.dtype, dev, b)
-    if desc.head_dim != dim:
-        raise ValueError(f"the cache holds heads of {desc.head_dim}, q has heads of {dim}")
-    _sizes(b, sq, heads, desc.max_pages * desc.page_size)
+    desc, cells, held, places = _cache(cache, page_table, q.dtype, dev, b)
+    if held[3] != dim:
+        raise ValueError(f"the cache holds heads of {held[3]}, q has heads of {dim}")
+    _sizes(b, sq, heads)
     if k_lens is None:
         raise TypeError("k_lens must be a GPU tensor of type int32")
     _ints(k_lens, "k_lens", dev, (b,))
@@ -509,12 +516,12 @@ def attention_cached(q, cache, page_table, k_lens, q_lens=None, causal=True, sof
     if out is not None:
         _check(out, "out", q.dtype, device=dev, shape=q.shape)
         _written("attention_cached(out=)", (q, slopes, *cache), out)
-    scores = _lib.ntk_attention_desc(_DTYPES[q.dtype], b, sq, desc.max_pages * desc.page_size, heads, desc.kv_heads, dim, 1 if causal else 0,
+    scores = _lib.ntk_attention_desc(_DTYPES[q.dtype], b, sq, places, heads, held[2], dim, 1 if causal else 0,
                                      1.0 / math.sqrt(max(dim, 1)) if scale is None else scale, softcap, _ptr(k_lens), None, None, _ptr(slopes))
     with _Call(q, stream, (q, k_lens, q_lens, slopes, out, page_table, *cache)) as call:
         o = _like(q) if out is None else out
         lse = torch.empty((b, heads, sq), dtype=torch.float32, device=dev) if return_lse else None
-        need = lib.ntk_attention_cached_workspace(ctypes.byref(scores), desc.dtype)
+        need = lib.ntk_attention_cached_workspace(ctypes.byref(scores), cells)
         if need < 0:
             _lib.check(need)
         work = torch.empty(need, dtype=torch.uint8, device=dev) if need else None
