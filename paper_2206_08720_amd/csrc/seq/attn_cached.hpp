@@ -30,11 +30,19 @@ __device__ const float kOne = 1.f;
 // What a batch entry's queries see, as AttnScope: its first `queries` rows are the last of its `len` positions.
 struct CachedScope {
   int len, off, queries, causal;
-  __device__ __forceinline__ CachedScope(const CachedArgs& a, int b) {
+  CachedScope() = default;
+  __device__ __forceinline__ void set(const CachedArgs& a, int b) {
     len = min(max(a.lens[b], 0), a.Sk);
     queries = a.q_lens ? min(max(a.q_lens[b], 0), a.Sq) : a.Sq;
     off = len - queries;
     causal = a.causal;
+  }
+  // of a sequence that all lanes work on, which the compiler cannot know of what it loads: scalars, and branches without masks
+  __device__ __forceinline__ CachedScope(const CachedArgs& a, int b) {
+    set(a, b);
+    len = __builtin_amdgcn_readfirstlane(len);
+    queries = __builtin_amdgcn_readfirstlane(queries);
+    off = len - queries;
   }
   __device__ __forceinline__ int klim(int i) const {     // keys below it are seen by query i
     const int pos = off + i;
@@ -239,9 +247,13 @@ __device__ __forceinline__ void set_row(const CachedArgs& a, const CachedScope& 
 // A row tile of no keys counts as one: its rows are written, too.
 template <int BN, int ROWS>
 struct Parts {
-  // tiles of keys that row tile mt of sequence b sees
+  // tiles of keys that row tile mt of sequence b sees (each lane its own)
   __device__ static __forceinline__ int tiles(const CachedArgs& a, int b, int mt) {
-    const CachedScope sc(a, b);
+    CachedScope sc;
+    sc.set(a, b);
+    return tiles(a, sc, mt);
+  }
+  __device__ static __forceinline__ int tiles(const CachedArgs& a, const CachedScope& sc, int mt) {
     const int i0 = (int)a.gdiv.div((uint32_t)(mt * ROWS)), i1 = (int)a.gdiv.div((uint32_t)(min(mt * ROWS + ROWS, a.R) - 1));
     return (sc.any(i0, i1) + BN - 1) / BN;
   }
@@ -356,7 +368,7 @@ __device__ __forceinline__ void each_stretch(const CachedArgs& a, int block, F f
     s.b = p.b(a);
     s.mt = p.mt(a);
     s.hk = p.hk;
-    s.nt = P::tiles(a, s.b, s.mt);
+    s.nt = P::tiles(a, CachedScope(a, s.b), s.mt);
     const int count = max(1, s.nt), take = min(count - p.t, p.left);
     const bool first = p.t == 0, last = p.t + take == count;
     if (!first && !end && take < p.left) {
