@@ -3,8 +3,8 @@
 A trunk of one block (norm, attention with rotary positions, residual, norm) reads packed token embeddings; the
 features of each sequence's last position are the inputs X of a small fully-connected head, whose
 Theta(X, X) the library computes.  Between two NTKs the trunk takes gradient steps towards target
-features, its backward pass made of the operators' own; at the end it reads the sequences token by token
-over a cache of keys and values.
+features, its backward pass made of the operators' own; at the end it reads the sequences again, a part at once and the rest token by token,
+over a cache of keys and values in pages.
 
     python examples/sequence_ntk.py        # on an MI355X, after the library is built
 """
@@ -64,16 +64,13 @@ class Trunk:
         _, d_norm_in = seq.rms_norm_backward(dqkv @ self.qkv, x, self.norm_in)
         return [d_norm_in, d_qkv, d_out, d_norm_out]
 
-    def token(self, x, cache, lens):
-        """z of the next position of every sequence: x [batch, 1, width]; cache [2, batch, capacity, kv_heads, dim] holds
-        lens[b] positions and gets one more."""
+    def token(self, x, cache, pages, lens):
+        """z of the next positions of every sequence: x [batch, length, width]; sequence b holds lens[b] positions in its pages of the
+        cache and gets `length` more."""
         y = seq.rms_norm(x, self.norm_in)
         q, k, v = self._split(y)
-        at = lens[:, None].contiguous()
-        q, k = seq.rotary(q, self.table, at, k=k)
-        rows = torch.arange(len(lens), device="cuda")
-        cache[0][rows, lens.long()], cache[1][rows, lens.long()] = k[:, 0], v[:, 0]
-        a = seq.attention(q, cache[0], cache[1], causal=True, softcap=self.softcap, k_lens=lens + 1)
+        q = seq.cache_append(cache, pages, lens, k, v, q=q, table=self.table)
+        a = seq.attention_cached(q, cache, pages, lens + x.shape[1], softcap=self.softcap)
         return seq.rms_norm(a.flatten(2) @ self.out.T, self.norm_out, residual=x)[0]
 
 
@@ -105,13 +102,17 @@ def main(batch=16, length=200, width=256, heads=8, kv_heads=2, dim=64, steps=3, 
                     w.sub_((0.1 * dw.float()).to(dtype))
     finally:
         ntk.close()
-    # the second document again, token by token; its positions start over, which rotary's relative angles do not see
-    first = length // 3
-    cache = torch.zeros(2, batch, length - first, kv_heads, dim, device="cuda", dtype=dtype)
+    # the second document again, half of it at once and the rest token by token; its positions start over, which rotary's relative
+    # angles do not see
+    first, size = length // 3, 16
+    per = -(-(length - first) // size)
+    cache = seq.paged_cache(batch * per, size, kv_heads, dim, dtype)
+    pages = torch.randperm(batch * per, device="cuda", generator=g).int().view(batch, per)
     lens = torch.zeros(batch, dtype=torch.int32, device="cuda")
-    for t in range(first, length):
-        out = trunk.token(x[:, t:t + 1], cache, lens)
-        lens += 1
+    half = (length - first) // 2
+    for t0, t1 in [(first, first + half)] + [(t, t + 1) for t in range(first + half, length)]:
+        out = trunk.token(x[:, t0:t1], cache, pages, lens)
+        lens += t1 - t0
     answer = out[:, 0].float()
     if not quiet:
         print(f"token by token against the whole pass: largest difference {float((answer - features).abs().max()):.2e}")

@@ -109,8 +109,8 @@ __device__ __forceinline__ void read_run(const AppendArgs& a, const T* x, const 
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
     const float c = in ? t[2 * i] : __builtin_nanf(""), s = t[2 * i + 1], u = f[i], v = f[8 + i];
-    f[i] = u * c - v * s;
-    f[8 + i] = v * c + u * s;
+    f[i] = fmaf(u, c, -(v * s));                          // rounded where kernels_rotary.hip rounds
+    f[8 + i] = fmaf(v, c, u * s);
   }
 }
 
