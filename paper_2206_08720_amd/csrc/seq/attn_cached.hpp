@@ -442,7 +442,7 @@ __global__ void __launch_bounds__(256) k_cached_join(const CachedArgs a) {
       const float f = m == mn ? 1.f : exp2_hw(m - mn), g = there * (ms[u] == mn ? 1.f : exp2_hw(ms[u] - mn));
       l = l * f + ls[u] * g;
 #pragma unroll
-      for (int k = 0; k < 4; ++k) o[k] = o[k] * f + os[u][k] * g;
+      for (int k = 0; k < 4; ++k) o[k] = o[k] * f + (s0 + u <= behind ? os[u][k] : 0.f) * g;   // the last one's may be infinite
       m = mn;
     }
   }

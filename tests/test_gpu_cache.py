@@ -369,6 +369,29 @@ def test_hidden_values_that_are_not_finite(e4m3):
     assert not torch.isfinite(o[0, 100:, 2:].float()).all(-1).any()
 
 
+@pytest.mark.parametrize("sq", [1, 40])
+def test_an_infinite_value_passes_the_join(sq):
+    """A sequence cut into parts for many workgroups: +inf among the values of one channel is +inf there, and nothing elsewhere."""
+    import torch
+    from paper_2206_08720_amd import seq
+    n, size = 9000, 16
+    cache = _empty(570, size, 1, 64, "bf16", False)
+    pages = _tables(1, 570, 570, 11)
+    _fill(cache, pages, [n], "bf16", 12)
+    q = _rand((1, sq, 4, 64), 13, "bf16")
+    k, v = (_sequence(x, pages, 0, n, size)[None] for x in _values(cache))
+    want, tol = _oracle(q, k, v, "bf16", causal=True)["o"]
+    others = [d for d in range(64) if d != 1]
+    for at in (0, 4500, n - sq):            # in the first part, in between, in the last one
+        page, slot = int(pages[0, at // size]), at % size
+        kept = cache.v[page, slot, 0, 1].clone()
+        cache.v[page, slot, 0, 1] = math.inf
+        o = seq.attention_cached(q.cuda(), cache, pages.cuda(), _ints([n]))
+        cache.v[page, slot, 0, 1] = kept
+        assert (o[..., 1] == math.inf).all()
+        _close("o", o[..., others], want[..., others], tol[..., others])
+
+
 def test_large_offsets():
     """A cache of 6 GiB: pages past 2^32 bytes, and strides past 2^31 elements."""
     import torch
