@@ -171,7 +171,8 @@ typedef struct ntk_cache {
  *   NTK_E4M3      the scale s of a page and head is the least power of two (from 2^-126 on) under which no new finite
  *                 value is above 448 s; on a page whose first slots hold older tokens it is at least what it was, and where it grows, those
  *                 slots are rounded again under it (exactly but for the type's subnormals).  Values that are not finite become NaN.
- *                 Values of fp16 over 61440 become 61440, so that no query in fp16 reads them as infinity.
+ *                 The type's last values, over 15/16 of 2^16 in fp16 and of 2^128 in fp32 and bf16, become 15/16 of it: rounded up, a
+ *                 query of the type would read them as infinity.
  *   table         [max_pos, rot / 2, 2] fp32 of ntk_rotary_table, or NULL with rot = 0: nothing turns.  A position that it lacks
  *                 gives NaN.
  *   lens, new_lens  [batch] int32 (values are clamped to 0 .. max_pages page_size and 0 .. length).

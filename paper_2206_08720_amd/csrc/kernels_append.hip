@@ -175,15 +175,16 @@ __device__ __forceinline__ float most_of(const float (&f)[kRun]) {
   return m;
 }
 
-// The type has no infinity: what is not finite becomes NaN.  A query in fp16 reads 2^16 as infinity, which is where fp16's last
-// values would round to: they stay one step below.
+// The type has no infinity: what is not finite becomes NaN.  The last values of the arrays' type would round to a power of two that
+// it reads as infinity: they stay one step below, 15/16 of it.  (A sum that a turn takes past fp16's range is no such value.)
 template <class T>
 __device__ __forceinline__ void to_units(float (&f)[kRun], float inv) {
+  constexpr bool HALF = std::is_same_v<T, _Float16>;
+  constexpr float most = HALF ? 61440.f : 0x1.ep127f, end = HALF ? 65520.f : __builtin_inff();
 #pragma unroll
   for (int k = 0; k < kRun; ++k) {
     float v = f[k];
-    if constexpr (std::is_same_v<T, _Float16>)
-      if (fabsf(v) > 61440.f && fabsf(v) < 65520.f) v = copysignf(61440.f, v);
+    if (fabsf(v) > most && fabsf(v) < end) v = copysignf(most, v);
     f[k] = fabsf(v) < __builtin_inff() ? v * inv : __builtin_nanf("");
   }
 }

@@ -232,6 +232,13 @@ def test_append_values_at_the_edge():
     cache = _empty(1, 8, 1, 16, "f16", True)
     seq.cache_append(cache, _ints([[0]]), _ints([0]), top.cuda(), top.cuda())
     assert (_values(cache)[0][0, 0, 0] == torch.tensor([61440.0, -61440.0, 61440.0, 61440.0] * 4)).all()
+    for type in ("f32", "bf16"):            # 2^128 would be the next one up
+        most = torch.finfo(_types()[type]).max
+        top = torch.tensor([most, -most, 1.875 * 2.0 ** 127, 1.5 * 2.0 ** 127] * 4).to(_types()[type]).view(1, 1, 1, 16)
+        cache = _empty(1, 8, 1, 16, type, True)
+        seq.cache_append(cache, _ints([[0]]), _ints([0]), top.cuda(), top.cuda())
+        want = torch.tensor([1.875, -1.875, 1.875, 1.5] * 4).double() * 2.0 ** 127
+        assert (_values(cache)[0][0, 0, 0] == want).all() and (_values(cache)[1][0, 0, 0] == want).all()
     tiny = torch.full((1, 1, 1, 16), 2.0 ** -140)
     cache = _empty(1, 8, 1, 16, "f32", True)
     seq.cache_append(cache, _ints([[0]]), _ints([0]), tiny.cuda(), tiny.cuda())
