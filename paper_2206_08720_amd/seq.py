@@ -545,14 +545,13 @@ class TokenLogprobs(NamedTuple):
 
 
 def _per_row(t, name, dtype, logits, each=()):
-    """One number (or `each` of them) a row, at any strides: contiguous, or None."""
+    """Checks one number (or `each` of them) a row, at any strides, or None."""
     if t is None:
-        return None
+        return
     if not isinstance(t, torch.Tensor) or t.dtype != dtype or not t.is_cuda:
         raise TypeError(f"{name} must be a GPU tensor of type {dtype}")
     if t.device != logits.device or t.shape != logits.shape[:-1] + each:
         raise ValueError(f"{name} is {tuple(t.shape)} on {t.device}, expected {tuple(logits.shape[:-1] + each)} on {logits.device}")
-    return t.contiguous()
 
 
 def _logits(logits):
@@ -571,12 +570,13 @@ def token_logprobs(logits, tokens, top=0, scale=1.0, stream=None):
     lead, vocab = logits.shape[:-1], logits.shape[-1]
     if tokens is None:
         raise TypeError("tokens must be a GPU tensor of type int32")
+    _per_row(tokens, "tokens", torch.int32, logits)
     if not 0 <= top <= min(vocab, 64):
         raise ValueError(f"top must be between 0 and {min(vocab, 64)}")
     with _Call(logits, stream, (logits, tokens)) as call:
         x, stride = _rows(logits)
         rows = x.shape[0]
-        t = _per_row(tokens, "tokens", torch.int32, logits)
+        t = tokens.contiguous()
         logp, entropy = (torch.empty(lead, dtype=torch.float32, device=logits.device) for _ in range(2))
         lse = torch.empty((*lead, 2), dtype=torch.float32, device=logits.device)
         top_logp = torch.empty((*lead, top), dtype=torch.float32, device=logits.device) if top else None
@@ -601,16 +601,17 @@ def token_logprobs_backward(dlogp, dentropy, logits, tokens, lse, entropy, scale
     for name, t in (("tokens", tokens), ("lse", lse), ("entropy", entropy)):
         if t is None:
             raise TypeError(f"{name} must be a GPU tensor")
+    _per_row(tokens, "tokens", torch.int32, logits)
+    _per_row(lse, "lse", torch.float32, logits, (2,))
+    for name, t in (("entropy", entropy), ("dlogp", dlogp), ("dentropy", dentropy)):
+        _per_row(t, name, torch.float32, logits)
     if inplace:
         _written("token_logprobs_backward", (dlogp, dentropy), logits)
     with _Call(logits, stream, (dlogp, dentropy, logits, tokens, lse, entropy)) as call:
         x, stride = _rows(logits)
         if inplace and x.data_ptr() != logits.data_ptr():
             raise ValueError("inplace needs logits whose rows are evenly spaced and apart")
-        t = _per_row(tokens, "tokens", torch.int32, logits)
-        lse = _per_row(lse, "lse", torch.float32, logits, (2,))
-        entropy, dlogp, dentropy = (_per_row(d, name, torch.float32, logits) for name, d in (
-            ("entropy", entropy), ("dlogp", dlogp), ("dentropy", dentropy)))
+        t, lse, entropy, dlogp, dentropy = (d if d is None else d.contiguous() for d in (tokens, lse, entropy, dlogp, dentropy))
         out, out_stride = (logits, stride) if inplace else (_like(logits), vocab)
         _lib.check(lib.ntk_logprobs_bwd(_DTYPES[x.dtype], x.shape[0], vocab, _ptr(x), stride, _ptr(t), scale, _ptr(lse), _ptr(entropy),
                                         _ptr(dlogp), _ptr(dentropy), _ptr(out), out_stride, call.handle))

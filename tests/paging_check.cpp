@@ -56,7 +56,7 @@ int main() {
     t.most = rng() % 9;
     t.pages = 1 + rng() % 40;
     const int batch = 1 + rng() % 3, size = 1 << t.shift;
-    // exactly the table's entries: a read past them is one that the checker (and its allocation) would miss at its peril
+    // one entry to spare on either side, which names no page
     std::vector<int> table((size_t)batch * t.most + 2, 12345);
     for (int i = 0; i < batch * t.most; ++i) {
       const int kind = rng() % 8;

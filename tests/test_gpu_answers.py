@@ -235,6 +235,8 @@ def test_refusals():
                  lambda: seq.attention_cached(q, cache, pages, lens, q_lens=lens[:1]), lambda: seq.attention_cached(q, cache, pages, lens, slopes=torch.zeros(3, device="cuda")),
                  lambda: seq.attention_cached(q, cache, pages.long(), lens), lambda: seq.attention_cached(q, cache, pages, lens, out=q[:1]),
                  lambda: seq.token_logprobs(logits, None), lambda: seq.token_logprobs(logits, tokens.long()), lambda: seq.token_logprobs(logits, tokens[:3]),
+                 lambda: seq.token_logprobs(logits, tokens.cpu(), stream=torch.cuda.Stream()), lambda: seq.token_logprobs(logits, [1, 2, 3, 4], stream=torch.cuda.Stream()),
+                 lambda: seq.token_logprobs_backward(tokens.cpu().float(), None, logits, tokens, torch.zeros(4, 2, device="cuda"), tokens.float(), stream=torch.cuda.Stream()),
                  lambda: seq.token_logprobs(logits, tokens, top=101), lambda: seq.token_logprobs(logits, tokens, top=-1), lambda: seq.token_logprobs(logits.double(), tokens),
                  lambda: seq.token_logprobs(logits.cpu(), tokens), lambda: seq.token_logprobs(logits[:, :0], tokens),
                  lambda: seq.token_logprobs_backward(tokens.float(), None, logits, tokens, torch.zeros(4, device="cuda"), tokens.float()),
