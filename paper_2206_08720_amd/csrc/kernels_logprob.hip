@@ -6,6 +6,10 @@
 // One pass with the running maximum; the sums carry x - m, not x, and m and log l are handed to the gradient apart, so that
 // nothing large cancels (a row that a mask fills with the type's lowest value is a uniform one).  Logits of -inf (tokens that
 // are ruled out) have p = 0 and add nothing.  Sums are fp32.
+//
+// Bound by memory: of 4096 rows of 65536 in bf16 the forward pass takes 140 us (3.8 TB/s of reads), the gradient 181 (5.9 TB/s of
+// reads and writes, some of them from the last-level cache); with 8 rows of 131072 by the launches and the best candidates' order
+// (14 us and 6 for the join, with top = 20).  Results are given off in fp32, the gradient in the logits' type.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -386,7 +390,8 @@ int elem(int dtype) { return dtype == 0 ? 4 : 2; }
 
 }  // namespace
 
-// Ranges of a row: 1024 workgroups, four a compute unit, each with at least 16 KB.
+// Ranges of a row: 1024 workgroups, four a compute unit, each with at least 16 KB.  (One row of 131072 in bf16 takes 8.8 us, with
+// ranges of 8 KB 12.7, of 32 KB 11.9; eight with top = 20 21.7, 22.6 and 26.8; 300 of 50000 16.4, with 2048 workgroups 19.3.)
 int logprob_splits(int dtype, long long rows, int vocab) {
   const long long bytes = (long long)vocab * elem(dtype);
   return rows < 1 ? 1 : (int)std::max(1LL, std::min((1024 + rows - 1) / rows, bytes / 16384));

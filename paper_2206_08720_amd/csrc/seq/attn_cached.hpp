@@ -80,8 +80,8 @@ __device__ __forceinline__ void from_e4m3(uint32_t w, float s, T (&y)[4]) {
 // ROWS positions of one head into an LDS tile of AttnTile's layout, by WAVES waves, 64 chunks of 16 bytes an instruction.  Pages
 // hold at least 8 places and tiles start on multiples of 32, so 8 rows from a multiple of 8 lie in one page: a page's number
 // is the same for a whole wave, and addresses are a scalar base and a lane's offset.  Nothing here waits for a load but for the
-// one that look() made a tile before (branches on fresh entries, and flat loads, whose waits are LDS waits too, cost 832 us where this form takes 179: 32 sequences
-// of up to 32768 places in 8 bits, 4 heads of 128).
+// one that look() made a tile before (branches on fresh entries, and flat loads, whose waits are LDS waits too, cost 832 us where this
+// form took 179: 32 sequences of 24 thousand places on average in 8 bits, 4 heads of 128).
 template <class T, int DP, int ROWS, int WAVES, bool VEC, bool E4M3>
 struct PageLoad {
   using Tile = AttnTile<T, DP>;
@@ -239,10 +239,18 @@ __device__ __forceinline__ void set_row(const CachedArgs& a, const CachedScope& 
 
 // ---- the work, in equal parts ----------------------------------------------------------------------------------------------
 // Sequences have lengths of their own, which the host does not know: with a workgroup a row tile, or ranges of a row's keys cut
-// alike for all, the longest sequence would keep a few workgroups busy after the others have gone (32 sequences of 16 to 32
-// thousand places: 171 us; parts of two prompts: 847 us).  So the workgroups that run at once deal out all tiles of keys, head by head and
-// row tile by row tile, in equal runs.  A row tile whose run ends early is gone on with by the next workers; what each has of it is
-// joined by k_cached_join.  The parts follow from the lengths alone, so that results do not depend on timing.
+// alike for all, the longest sequence would keep a few workgroups busy after the others have gone.  So the workgroups that run at once
+// deal out all tiles of keys, head by head and row tile by row tile, in equal runs.  A row tile whose run ends early is gone on with
+// by the next workers; what each has of it is joined by k_cached_join.  The parts follow from the lengths alone, so that results do
+// not depend on timing.  In us, a workgroup a row tile / alike for all / equal runs (tokens of 32 query over 4 key/value heads in
+// 8 bits, the parts' over 8, all of 128): 32 sequences of 24 thousand places 359 / 171 / 182, one of 131 thousand and 31 of one
+// thousand 1581 / 543 / 71, parts of 1200 queries at the ends of 14 and 2 thousand places 887 / 782 / 373.  What a worker loses by it is
+// the look at all lengths, about 5 us.
+//
+// A stretch costs 7 to 8 us whatever its length (its state, the first loads, the partial results).  So where few rows have fewer row
+// tiles than there are workers, and runs get not much longer by it, a worker takes one part of one row tile, and nothing more: one
+// token over 8000 places, 8 key/value heads in bf16, 29 us where runs that go on into the next head take 35; four of 1500 places 25
+// and 31.  Tiles of many rows cost more than that saves (3 parts of 380 queries, 12 heads of 80: 60 us, this way 66).
 //
 // A row tile of no keys counts as one: its rows are written, too.
 template <int BN, int ROWS>
@@ -263,8 +271,8 @@ struct Parts {
 
   template <int THREADS>
   __device__ __forceinline__ void find(const CachedArgs& a, int block) {
-    __shared__ long long sums[THREADS / 64];
-    __shared__ int found[3];
+    constexpr int TRIES = 6;
+    __shared__ int counts[1 + TRIES], sums[THREADS / 64], found[5];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = a.B * a.tiles;
     if (a.workers == 0) {
       int bh, item;
@@ -275,53 +283,80 @@ struct Parts {
       left = per = 0x7fffffff;
       return;
     }
+    // The plan sees to it that there are fewer than 2^30 tiles in all.
     const bool inside = a.tiles == 1;
-    const int times = inside ? a.Hk : 1;
+    const int times = inside ? a.Hk : 1, heads = inside ? 1 : a.Hk;
     const int chunk = (n + THREADS - 1) / THREADS, p0 = min(n, (int)threadIdx.x * chunk), p1 = min(n, p0 + chunk);
-    long long mine = 0;
-    for (int p = p0; p < p1; ++p) mine += (long long)times * max(1, tiles(a, p / a.tiles, p % a.tiles));
-    long long upto = mine;                                       // inclusive sum
+    auto tiles_of = [&](int p) { return max(1, inside ? tiles(a, p, 0) : tiles(a, p / a.tiles, p % a.tiles)); };
+    auto sum = [&](auto f) {                                     // of this thread's row tiles
+      int x = 0;
+      for (int p = p0; p < p1; ++p) x += times * f(tiles_of(p));
+      return x;
+    };
+    if (threadIdx.x <= TRIES) counts[threadIdx.x] = 0;
+    __syncthreads();
+    if (p0 < p1) atomicAdd(&counts[0], sum([](int c) { return c; }));
+    __syncthreads();
+    const int all = counts[0] * heads;
+    per = max(a.least, (all + a.workers - 1) / a.workers);
+    // the least of a few lengths under which parts that end with their row tile need no more workers than there are
+    int share = 0, total = counts[0];
+    if (ROWS == 32 && n * a.Hk < a.workers) {
+      const int spare = a.workers - n * a.Hk, top = min(max(a.least, (all + spare - 1) / spare), per + per / 4 + 8);
+      auto length = [&](int k) { return per + (top - per) * ((1 << k) >> 1) / 16; };
+#pragma unroll
+      for (int k = 0; k < TRIES; ++k)
+        if (p0 < p1) atomicAdd(&counts[1 + k], sum([&](int c) { return (c + length(k) - 1) / length(k); }));
+      __syncthreads();
+#pragma unroll
+      for (int k = TRIES - 1; k >= 0; --k)
+        if (counts[1 + k] * heads <= a.workers) {
+          share = length(k);
+          total = counts[1 + k];
+        }
+    }
+    auto units = [&](int c) { return share ? (c + share - 1) / share : c; };   // parts of a row tile, or tiles
+    // neighbours in the order read the same keys: a die (workgroups are dealt out to the eight in turn) takes a run of workers
+    const int g0 = number(a, block) * (share ? 1 : per), used = total * heads;
+    hk = inside ? 0 : g0 / total;
+    const int at = g0 - hk * total;
+    const int mine = sum(units);
+    int upto = mine;                                             // inclusive sum
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) {
-      const long long x = __shfl_up(upto, o);
+      const int x = __shfl_up(upto, o);
       if (lane >= o) upto += x;
     }
     if (lane == 63) sums[wave] = upto;
     __syncthreads();
-    long long total = 0;
 #pragma unroll
-    for (int w = 0; w < THREADS / 64; ++w) {
+    for (int w = 0; w < THREADS / 64; ++w)
       if (w < wave) upto += sums[w];
-      total += sums[w];
-    }
-    // neighbours in the order read the same keys: a die (workgroups are dealt out to the eight in turn) takes a run of workers
-    const int eighth = a.workers / 8, w = a.workers % 8 ? block : (block % 8) * eighth + block / 8;
-    const long long all = inside ? total : total * a.Hk;
-    per = (int)min((long long)0x7fffffff, max((long long)a.least, (all + a.workers - 1) / a.workers));
-    const long long g0 = (long long)w * per;
-    left = (int)max(0LL, min((long long)per, all - g0));
-    hk = inside ? 0 : (int)(g0 / total);
-    const long long at = g0 - hk * total;
     if (at >= upto - mine && at < upto) {
-      long long x = upto - mine;
-      int p = p0;
+      int x = upto - mine, p = p0;
       for (;; ++p) {
-        const int c = max(1, tiles(a, p / a.tiles, p % a.tiles));
-        if (at < x + (long long)times * c) {
+        const int c = tiles_of(p), u = units(c);
+        if (at < x + times * u) {
+          const int i = (at - x) % u, equal = (c + u - 1) / u;   // a row tile's parts are equal ones
           found[0] = p;
-          found[1] = (int)((at - x) % c);
-          found[2] = inside ? (int)((at - x) / c) : hk;
+          found[1] = share ? i * equal : i;
+          found[2] = inside ? (at - x) / u : hk;
+          if (share) {
+            found[3] = min(equal, c - i * equal);
+            found[4] = equal;
+          }
           break;
         }
-        x += (long long)times * c;
+        x += times * u;
       }
     }
     __syncthreads();
     pair = __builtin_amdgcn_readfirstlane(found[0]);
     t = __builtin_amdgcn_readfirstlane(found[1]);
     hk = __builtin_amdgcn_readfirstlane(found[2]);
+    left = g0 >= used ? 0 : share ? found[3] : min(per, used - g0);
     left = __builtin_amdgcn_readfirstlane(left);
-    per = __builtin_amdgcn_readfirstlane(per);
+    per = __builtin_amdgcn_readfirstlane(share ? found[4] : per);
   }
   // the row tile behind: a sequence's heads in turn, whose parts of a page are neighbours, or, where many rows read the same keys,
   // all of a head's rows
@@ -456,9 +491,11 @@ __global__ void __launch_bounds__(256) k_cached_join(const CachedArgs a) {
 }
 
 // ---- many rows: NW waves of 32 rows share the key tiles in two LDS stages ----------------------------------------------------
-// Bound by two waves a SIMD that take turns at the matrix cores and at the exponentials, as in kernels_attn.hip; in 8 bits with eight waves a
-// workgroup, so that what a tile takes to bring in and to convert is shared by 256 rows (bf16, parts of 1212 and 1839 queries over 14187 and
-// 8463 places, 32 heads over 8 of 128: 691 us, 720 TFLOP/s; 750 with four waves, of which bringing in takes 110 and converting 70).
+// Bound by two waves a SIMD that take turns at the matrix cores (34 % of the cycles) and at the exponentials (vector 45 %), as in
+// kernels_attn.hip; in 8 bits with eight waves a workgroup, so that what a tile takes to bring in and to convert is shared by 256 rows
+// (bf16, parts of 1212 and 1839 queries over 14187 and 8463 places, 32 heads over 8 of 128: 691 us, 720 TFLOP/s; 750 with four waves, of
+// which bringing in takes 110 and converting 70).  Results that are not finite are formed again by a kernel of its own: within this
+// one its registers cost long parts 2 to 7 %, which is more than the launch.
 template <class T, int DP, int NW, bool VEC, bool E4M3, bool CAREFUL>
 __device__ __forceinline__ bool cached_stretch(const CachedArgs& a, char* smem, const Stretch& x) {
   constexpr int BN = kFwdKeys<T>;
@@ -547,6 +584,10 @@ __global__ void __launch_bounds__(64 * NW, 1) k_attn_cached_again(const CachedAr
 }
 
 // ---- few rows (at most 32 a key/value head): each wave takes every W-th tile of 32 keys through LDS of its own ------------------
+// Bound by memory where there is enough to read: 96 sequences of 3 thousand places on average, 8 heads of 128 in bf16, 239 us, 5.1 TB/s (a
+// large copy reaches 4.9); in 8 bits 32 sequences of 24 thousand, 4 heads, 183 us, 4.3 TB/s, where a wave's conversions and products
+// take turns with its loads (vector 29 %, LDS 29 %, matrix 11 % of the cycles).  The careful pass comes after the loop over the
+// stretches: inside it, its registers would be spilled with theirs.
 constexpr int kCachedKeys = 32;
 template <class T, int DP, bool E4M3>
 constexpr int kCachedStages = E4M3 ? 1 : 2;     // 8 bits: the next tile is on its way in registers
@@ -642,9 +683,11 @@ __device__ __forceinline__ bool tokens_stretch(const CachedArgs& a, char* smem, 
 template <class T, int DP, bool VEC, bool E4M3>
 __global__ void __launch_bounds__((64 * kCachedWaves<T, DP, E4M3>), (E4M3 && sizeof(T) == 2 ? 2 : 1)) k_attn_cached_tokens(const CachedArgs a) {
   extern __shared__ __align__(1024) char smem[];
-  each_stretch<Parts<kCachedKeys, 32>, 64 * kCachedWaves<T, DP, E4M3>>(a, blockIdx.x, [&](const Stretch& x) {
-    if (tokens_stretch<T, DP, VEC, E4M3, false>(a, smem, x)) tokens_stretch<T, DP, VEC, E4M3, true>(a, smem, x);
-  });
+  typedef Parts<kCachedKeys, 32> P;
+  constexpr int THREADS = 64 * kCachedWaves<T, DP, E4M3>;
+  bool bad = false;
+  each_stretch<P, THREADS>(a, blockIdx.x, [&](const Stretch& x) { bad |= tokens_stretch<T, DP, VEC, E4M3, false>(a, smem, x); });
+  if (bad) each_stretch<P, THREADS>(a, blockIdx.x, [&](const Stretch& x) { tokens_stretch<T, DP, VEC, E4M3, true>(a, smem, x); });
 }
 
 template <class T, int DP, int NW, bool VEC, bool E4M3>

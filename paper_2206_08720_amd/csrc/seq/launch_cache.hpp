@@ -32,8 +32,9 @@ hipError_t launch_append(hipStream_t s, int dtype, const AppendArgs& a, bool vec
 
 // Attention over a cache (kernels_cached.hip, the kernels in a file for each type).
 struct CachedArgs;
-// `waves` of 32 rows a workgroup, 0: the few-row kernel; `tiles` row tiles a key/value head; the tiles of keys are dealt out to `workers` workgroups, each at least
-// `least` of them (0: a workgroup a row tile, `blocks` in all).  Workspace: part_floats, then 4 ints a worker, then a flag a workgroup.
+// `waves` of 32 rows a workgroup, 0: the few-row kernel; `tiles` row tiles a key/value head; the tiles of keys are dealt out to
+// `workers` workgroups, each at least `least` of them (0: a workgroup a row tile, `blocks` in all).  Workspace: part_floats, then 4 ints
+// a worker, then a flag a workgroup.
 struct CachedPlan {
   int waves, tiles, workers, least;
   long long blocks, part_floats, ints;
