@@ -585,8 +585,8 @@ __global__ void __launch_bounds__(64 * NW, 1) k_attn_cached_again(const CachedAr
 
 // ---- few rows (at most 32 a key/value head): each wave takes every W-th tile of 32 keys through LDS of its own ------------------
 // Bound by memory where there is enough to read: 96 sequences of 3 thousand places on average, 8 heads of 128 in bf16, 239 us, 5.1 TB/s (a
-// large copy reaches 4.9); in 8 bits 32 sequences of 24 thousand, 4 heads, 183 us, 4.3 TB/s, where a wave's conversions and products
-// take turns with its loads (vector 29 %, LDS 29 %, matrix 11 % of the cycles).  The careful pass comes after the loop over the
+// large copy reaches 4.9); in 8 bits 32 sequences of 24 thousand, 4 heads, 168 us, 4.7 TB/s, where a wave's conversions and products
+// take turns with its loads (vector 31 %, LDS 31 %, matrix 12 % of the cycles).  The careful pass comes after the loop over the
 // stretches: inside it, its registers would be spilled with theirs.
 constexpr int kCachedKeys = 32;
 template <class T, int DP, bool E4M3>
