@@ -88,7 +88,7 @@ def test_the_cache_gives_what_the_whole_sequence_gives():
 
 UNEVEN = [
     # type, e4m3, H, Hk, D, page, capacity, k_lens, q_len, q_lens: one long sequence among short ones, empty ones, more sequences than threads,
-    # row tiles of all lengths, queries that run past the keys
+    # row tiles of all lengths, queries that run past the keys, nearly as many sequences and heads as workgroups
     ("bf16", False, 8, 2, 128, 16, 6016, [6000, 1, 0, 33, 700, 32, 31, 2], 1, None, {}),
     ("bf16", True, 8, 2, 128, 64, 6016, [6000, 1, 0, 33, 700, 32, 31, 2], 1, None, {}),
     ("f16", True, 4, 4, 64, 16, 9600, [3, 9555, 0, 0, 9599], 2, [2, 1, 1, 0, 2], {}),
@@ -99,6 +99,8 @@ UNEVEN = [
     ("f16", True, 2, 1, 80, 16, 1040, [1040, 200, 31], 300, [300, 200, 100], {"slopes": True}),
     ("f32", False, 2, 1, 64, 16, 800, [800, 100], 200, [133, 200], {}),
     ("bf16", True, 1, 1, 64, 128, 12800, [12800], 1, None, {}),
+    ("bf16", False, 8, 8, 128, 16, 1024, [i * 397 % 1025 for i in range(31)], 1, None, {}),
+    ("bf16", True, 8, 8, 128, 16, 2048, [i * 797 % 2049 for i in range(31)], 1, None, {}),
 ]
 
 
