@@ -99,12 +99,8 @@ struct PageLoad {
     const int e = min((tile0 + 8 * (lane & (ROWS / 8 - 1))) >> a.pages.shift, a.pages.most - 1);
     return a.pages.table[(long long)b * a.pages.most + e];
   }
-  // One head's part of a cache's array: bytes.
-  struct Head {
-    const char* base;
-    long long page;                        // from page to page
-    uint32_t slot;                         // from slot to slot
-    __device__ __forceinline__ Head(const AttnView& v, int hk) : base((const char*)v.p + (long long)hk * v.sh * CE), page(v.sb * CE), slot((uint32_t)(v.ss * CE)) {}
+  struct Head : HeadCells<VEC> {
+    __device__ __forceinline__ Head(const AttnView& v, int hk) : HeadCells<VEC>(v.p, v.sb, v.ss, v.sh, hk, CE) {}
   };
   // A tile's place, with look()'s entry for it.
   struct Where {
@@ -125,32 +121,31 @@ struct PageLoad {
     if constexpr (RPI <= 8) return lo;
     return lane < 32 ? lo : __builtin_amdgcn_readlane(x, row0 / 8 + 1);
   }
-  // a lane's chunk of a row, and where it is within eight rows
+  // a lane's chunk of a row
   __device__ static __forceinline__ int chunk(int row, int lane) {
     if constexpr (E4M3) return lane % CH;
     return lane % CH ^ Tile::swz(row);                          // straight into LDS: lane l's 16 bytes go to place l
   }
-  __device__ static __forceinline__ uint32_t within(const Head& h, int row, int c) { return (uint32_t)(row & 7) * h.slot + (uint32_t)c * 16; }
   // where a lane's chunk of instruction i is read; `there`: it is the cache's
   __device__ static __forceinline__ const char* source(const CachedArgs& a, const Head& h, const Where& w, int i, int wave, int lane, int& c, bool& there) {
     const int row0 = At::first(i, wave), row = At::row(i, wave, lane), id = of_row(w.entry, row0, lane);
     c = chunk(row, lane);
     const bool in = (unsigned)id < (unsigned)a.pages.pages;
-    const char* base = h.base + (long long)(in ? id : 0) * h.page + (long long)a.pages.slot(w.tile0 + At::group(row0, lane)) * h.slot;
+    const char* base = h.base + h.offset(in ? id : 0, a.pages.slot(w.tile0 + At::group(row0, lane)));
     const bool live = w.tile0 + row < w.len && (EVEN || row < ROWS);
     there = live && in && c * EC < a.D;
     const char* none = live && !in ? (const char*)&kNaNs : (const char*)&kZeros;
     if constexpr (VEC) {
-      uint64_t at = (uint64_t)(uintptr_t)(base + within(h, row, c));
+      uint64_t at = (uint64_t)(uintptr_t)(base + (h.within(row) + (uint32_t)c * 16));
       asm volatile("" : "+v"(at));             // formed in any case: a branch around it would cost more
       return there ? (const char*)(uintptr_t)at : none;
     }
-    return there ? base + (long long)(row & 7) * h.slot : none;
+    return there ? base + h.within(row) : none;
   }
   // The same in a whole tile: a scalar base and 32 bits of a lane, nothing to select.
-  __device__ static __forceinline__ long long offset(const CachedArgs& a, const Head& h, const Where& w, int i, int wave, int lane) {
-    const int row0 = At::first(i, wave);
-    return (long long)of_row(w.entry, row0, lane) * h.page + (uint32_t)a.pages.slot(w.tile0 + At::group(row0, lane)) * h.slot;
+  __device__ static __forceinline__ const char* whole(const CachedArgs& a, const Head& h, const Where& w, int i, int wave, int lane) {
+    const int row0 = At::first(i, wave), row = At::row(i, wave, lane);
+    return h.base + h.offset(of_row(w.entry, row0, lane), a.pages.slot(w.tile0 + At::group(row0, lane))) + (h.within(row) + (uint32_t)chunk(row, lane) * 16);
   }
   // 16 bytes of a chunk that need not be aligned
   __device__ static __forceinline__ u32x4 gather(const char* from, bool there, int c, int D) {
@@ -188,10 +183,7 @@ struct PageLoad {
     to.s = load_float(w.scale >= 0 ? scale + w.scale : &kOne);
     if (w.whole) {
 #pragma unroll
-      for (int i = 0; i < NI; ++i) {
-        const int row = At::row(i, wave, lane);
-        to.x[i] = load16(h.base + offset(a, h, w, i, wave, lane) + within(h, row, chunk(row, lane)));
-      }
+      for (int i = 0; i < NI; ++i) to.x[i] = load16(whole(a, h, w, i, wave, lane));
       return;
     }
 #pragma unroll

@@ -3,6 +3,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 namespace ntk {
 
 // A sequence's place `pos` is slot pos % 2^shift of the page that entry pos / 2^shift of its row of the table names.
@@ -29,6 +31,25 @@ struct TilePlaces {
   __host__ __device__ static __forceinline__ int first(int i, int wave) { return (i * WAVES + wave) * RPI; }
   __host__ __device__ static __forceinline__ int row(int i, int wave, int lane) { return first(i, wave) + lane / CH; }
   __host__ __device__ static __forceinline__ int group(int row0, int lane) { return (row0 & ~7) + (RPI == 16 ? lane / CH & 8 : 0); }
+};
+
+// Whether offsets within a page of a cache fit 32 bits, its slots `stride` elements of `bytes` apart.
+inline bool narrow_slots(long long stride, int bytes, int page_size) { return stride < (1LL << 31) / bytes / page_size; }
+
+// One head's part of a cache's array, in bytes.  NARROW: narrow_slots() holds.  Where it does not, slots may lie any distance apart
+// (the slots outermost, in a cache of tens of GB), and their offsets have 64 bits.
+template <bool NARROW>
+struct HeadCells {
+  using Offset = std::conditional_t<NARROW, uint32_t, long long>;
+  const char* base;
+  long long page;                          // from page to page
+  Offset slot;                             // from slot to slot
+  __host__ __device__ __forceinline__ HeadCells(const void* p, long long pages, long long slots, long long heads, int head, int bytes)
+      : base((const char*)p + (long long)head * heads * bytes), page(pages * bytes), slot((Offset)(slots * bytes)) {}
+  // where page `id` has its slot `s`
+  __host__ __device__ __forceinline__ long long offset(int id, int s) const { return (long long)id * page + (Offset)s * slot; }
+  // a row's place behind the first one of its eight
+  __host__ __device__ __forceinline__ Offset within(int row) const { return (Offset)(row & 7) * slot; }
 };
 
 // The tokens that an append adds to one sequence: positions first .. first + count - 1.

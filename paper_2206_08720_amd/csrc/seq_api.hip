@@ -525,9 +525,8 @@ extern "C" int ntk_attention_cached(const ntk_attention_desc* desc, const ntk_ca
   if (cache->pages > 0) {
     set_view(a.k, &cache->k);
     set_view(a.v, &cache->v);
-    const long long wide = (1LL << 31) / (e4m3 ? 1 : e) / cache->page_size;   // offsets within a page have 32 bits
-    vec = vec && view_vec(&cache->k, e4m3 ? 1 : e) && view_vec(&cache->v, e4m3 ? 1 : e) && cache->k.stride_position < wide &&
-          cache->v.stride_position < wide;
+    const int ce = e4m3 ? 1 : e;
+    for (const ntk_view* c : {&cache->k, &cache->v}) vec = vec && view_vec(c, ce) && narrow_slots(c->stride_position, ce, cache->page_size);
   }
   a.k_scale = cache->k_scale;
   a.v_scale = cache->v_scale;
