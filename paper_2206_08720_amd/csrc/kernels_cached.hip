@@ -13,8 +13,10 @@ CachedPlan attn_plan_cached(int dtype, bool e4m3, int B, int Hk, int R, int plac
   p.blocks = (long long)B * Hk * p.tiles;
   const int keys = p.waves == 0 ? kCachedKeys : size == 2 ? 64 : 32;
   const long long most = ((long long)places + keys - 1) / keys;   // tiles of keys that a row tile can see
-  // Workgroups that run at once: two a compute unit, one where registers or LDS leave room for one.
-  const bool two = p.waves == 0 ? dp == 64 || (e4m3 && size == 2) : p.waves == 4 && size * dp <= 256;
+  // Workgroups that run at once: two a compute unit, one where registers or LDS leave room for one.  Tokens: two where a workgroup's
+  // tiles (kCachedBytes) take 64 KB, not 128.  (With two counted where one fits, runs go in two rounds: fp32, heads of 64, one sequence of
+  // 131 thousand places 91 us, counted right 63; 32 of six thousand 194 and 164; 350 of 1600 662 and 557.)
+  const bool two = p.waves == 0 ? size * dp <= (e4m3 ? 256 : 128) : p.waves == 4 && size * dp <= 256;
   const int slots = two ? 512 : 256;
   // Tokens: 64 KB of keys a workgroup at least (four sequences of 1500 places, 8 heads of 128 in bf16: 31 us, with 128 KB 36, with 32 KB
   // 32).  Many rows: 256 keys, 64 in fp32, whose products take several times as long (3 by 380 queries at the end of 2100 places, fp16,
