@@ -9,6 +9,7 @@
 // two values of the queries' type), and written into the same tiles, so that the products are the same ones.
 #pragma once
 #include "attn_fwd.hpp"
+#include "dealing.hpp"
 #include "launch_cache.hpp"
 
 namespace ntk {
@@ -263,8 +264,8 @@ struct Parts {
 
   template <int THREADS>
   __device__ __forceinline__ void find(const CachedArgs& a, int block) {
-    constexpr int TRIES = 6;
-    __shared__ int counts[1 + TRIES], sums[THREADS / 64], found[5];
+    __shared__ int counts[1 + Deal::TRIES], sums[THREADS / 64];
+    __shared__ Deal::Part found;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = a.B * a.tiles;
     if (a.workers == 0) {
       int bh, item;
@@ -285,34 +286,22 @@ struct Parts {
       for (int p = p0; p < p1; ++p) x += times * f(tiles_of(p));
       return x;
     };
-    if (threadIdx.x <= TRIES) counts[threadIdx.x] = 0;
+    if (threadIdx.x <= Deal::TRIES) counts[threadIdx.x] = 0;
     __syncthreads();
     if (p0 < p1) atomicAdd(&counts[0], sum([](int c) { return c; }));
     __syncthreads();
-    const int all = counts[0] * heads;
-    per = max(a.least, (all + a.workers - 1) / a.workers);
+    Deal d(n, times, heads, a.workers, a.least, counts[0]);
     // the least of a few lengths under which parts that end with their row tile need no more workers than there are
-    int share = 0, total = counts[0];
-    if (ROWS == 32 && n * a.Hk < a.workers) {
-      const int spare = a.workers - n * a.Hk, top = min(max(a.least, (all + spare - 1) / spare), per + per / 4 + 8);
-      auto length = [&](int k) { return per + (top - per) * ((1 << k) >> 1) / 16; };
+    if (ROWS == 32 && d.may_share()) {
 #pragma unroll
-      for (int k = 0; k < TRIES; ++k)
-        if (p0 < p1) atomicAdd(&counts[1 + k], sum([&](int c) { return (c + length(k) - 1) / length(k); }));
+      for (int k = 0; k < Deal::TRIES; ++k)
+        if (p0 < p1) atomicAdd(&counts[1 + k], sum([&](int c) { return (c + d.length(k) - 1) / d.length(k); }));
       __syncthreads();
-#pragma unroll
-      for (int k = TRIES - 1; k >= 0; --k)
-        if (counts[1 + k] * heads <= a.workers) {
-          share = length(k);
-          total = counts[1 + k];
-        }
+      d.choose(counts + 1);
     }
-    auto units = [&](int c) { return share ? (c + share - 1) / share : c; };   // parts of a row tile, or tiles
     // neighbours in the order read the same keys: a die (workgroups are dealt out to the eight in turn) takes a run of workers
-    const int g0 = number(a, block) * (share ? 1 : per), used = total * heads;
-    hk = inside ? 0 : g0 / total;
-    const int at = g0 - hk * total;
-    const int mine = sum(units);
+    const int w = number(a, block), at = d.at(w);
+    const int mine = sum([&](int c) { return d.units(c); });
     int upto = mine;                                             // inclusive sum
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) {
@@ -322,33 +311,27 @@ struct Parts {
     if (lane == 63) sums[wave] = upto;
     __syncthreads();
 #pragma unroll
-    for (int w = 0; w < THREADS / 64; ++w)
-      if (w < wave) upto += sums[w];
+    for (int i = 0; i < THREADS / 64; ++i)
+      if (i < wave) upto += sums[i];
     if (at >= upto - mine && at < upto) {
       int x = upto - mine, p = p0;
       for (;; ++p) {
-        const int c = tiles_of(p), u = units(c);
-        if (at < x + times * u) {
-          const int i = (at - x) % u, equal = (c + u - 1) / u;   // a row tile's parts are equal ones
-          found[0] = p;
-          found[1] = share ? i * equal : i;
-          found[2] = inside ? (at - x) / u : hk;
-          if (share) {
-            found[3] = min(equal, c - i * equal);
-            found[4] = equal;
-          }
+        const int c = tiles_of(p), u = times * d.units(c);
+        if (at < x + u) {
+          found = d.within(p, c, x, w);
           break;
         }
-        x += times * u;
+        x += u;
       }
     }
     __syncthreads();
-    pair = __builtin_amdgcn_readfirstlane(found[0]);
-    t = __builtin_amdgcn_readfirstlane(found[1]);
-    hk = __builtin_amdgcn_readfirstlane(found[2]);
-    left = g0 >= used ? 0 : share ? found[3] : min(per, used - g0);
+    const Deal::Part part = d.taken(found, w);
+    pair = part.pair, t = part.t, hk = part.hk, left = part.left, per = part.per;
+    pair = __builtin_amdgcn_readfirstlane(pair);                 // (from `part` itself, 25 more vector registers)
+    t = __builtin_amdgcn_readfirstlane(t);
+    hk = __builtin_amdgcn_readfirstlane(hk);
     left = __builtin_amdgcn_readfirstlane(left);
-    per = __builtin_amdgcn_readfirstlane(share ? found[4] : per);
+    per = __builtin_amdgcn_readfirstlane(per);
   }
   // the row tile behind: a sequence's heads in turn, whose parts of a page are neighbours, or, where many rows read the same keys,
   // all of a head's rows
