@@ -6,11 +6,12 @@
 // the subnormals alone), and because the matrix kernels apply it within the conversion.  A page that holds older tokens
 // keeps at least the s it has; where s grows, the older cells are multiplied by s_old / s.
 //
-// Everything moves once: bound by memory where there is much of it (12 thousand tokens of 32 query and 8 key/value heads of 128 in
-// bf16: 80 us for 302 MB, 3.8 TB/s, where a copy reaches 4.9; the rest goes to the table's rows, which come from the caches, and to the
-// look-ups of page after length that each run of 16 waits for), by the launch where there is little (64 tokens: 6 us).  In 8 bits
+// Everything moves once: bound by memory where there is much of it (13.8 thousand tokens of 32 query and 8 key/value heads of 128 in
+// bf16: 91 us for 339 MB, 3.7 TB/s, where a copy reaches 4.9; the rest goes to the table's rows, which come from the caches, and to the
+// look-ups of page after length that each run of 16 waits for), by the launch where there is little (64 tokens: 7 us).  In 8 bits
 // a wave owns the part of a page that one head gets, so that no two write a scale; it reads the new tokens twice, the second time
-// from the caches.
+// from the caches: the same tokens 91 us with pages of 64 places, 311 MB.  Large pages leave few waves with much each: 348 us with pages of
+// 1024; one prompt of 8192 tokens 40 us with pages of 64, 96 of 256, 303 of 1024.
 #include <hip/hip_runtime.h>
 
 #include <type_traits>

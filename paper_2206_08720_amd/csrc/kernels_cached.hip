@@ -19,8 +19,10 @@ CachedPlan attn_plan_cached(int dtype, bool e4m3, int B, int Hk, int R, int plac
   const bool two = p.waves == 0 ? size * dp <= (e4m3 ? 256 : 128) : p.waves == 4 && size * dp <= 256;
   const int slots = two ? 512 : 256;
   // Tokens: 64 KB of keys a workgroup at least (four sequences of 1500 places, 8 heads of 128 in bf16: 31 us, with 128 KB 36, with 32 KB
-  // 32).  Many rows: 256 keys, 64 in fp32, whose products take several times as long (3 by 380 queries at the end of 2100 places, fp16,
-  // 12 heads of 80: 50 us, with 512 keys 53, with 128 50; a workgroup a row tile 91).
+  // 32; in fp32 40, 48 and 40).  Many rows: 256 keys, 64 in fp32, whose products take several times as long (3 by 380 queries at the end of
+  // 2100 places, fp16, 12 heads of 80: 50 us, with 512 keys 53, with 128 50; a workgroup a row tile 91.  fp32, up to 40 queries at the end
+  // of up to 400, 4 sequences of 8 heads of 64: 24 us, with 128 keys 27; one of 8 heads of 128: 29 and 36; 64 at the end of 4000, 8 heads of
+  // 64: 40 and 35, with 32 keys 41, with 256 43).
   p.least = p.waves == 0 ? std::max(4, 65536 / (keys * dp * cell)) : size == 2 ? 4 : 2;
   // A workgroup a row tile where parts would be short, or row tiles are enough to even out.  Parts are counted in 32 bits.
   const bool whole = most < 2 * p.least || p.blocks >= 8 * slots || p.blocks * most >= (1LL << 30);

@@ -7,6 +7,11 @@
 //
 // A cache in 8 bits is read into registers, converted there (one instruction takes two e4m3 values and their page's power of two to
 // two values of the queries' type), and written into the same tiles, so that the products are the same ones.
+//
+// Fewer bits than fp32, by choice: p is rounded to the queries' type for its product (its sum l is not), as in kernels_attn.hip, which
+// leaves bf16 results 0.0022 from 64 bits in norm and fp16 ones 0.00024, where rounding the result alone leaves 0.0017 and 0.00021.  p in
+// two parts of 16 bits, whose products are added, reaches the latter, and costs as many products of values again: tokens 1 to 5 %, five
+// drafted tokens 7, long parts of prompts 21 to 27 (the case below 604 -> 768 us).
 #pragma once
 #include "attn_fwd.hpp"
 #include "dealing.hpp"
@@ -468,8 +473,9 @@ __global__ void __launch_bounds__(256) k_cached_join(const CachedArgs a) {
 // ---- many rows: NW waves of 32 rows share the key tiles in two LDS stages ----------------------------------------------------
 // Bound by two waves a SIMD that take turns at the matrix cores (34 % of the cycles) and at the exponentials (vector 45 %), as in
 // kernels_attn.hip; in 8 bits with eight waves a workgroup, so that what a tile takes to bring in and to convert is shared by 256 rows
-// (bf16, parts of 1212 and 1839 queries over 14187 and 8463 places, 32 heads over 8 of 128: 691 us, 720 TFLOP/s; 750 with four waves, of
-// which bringing in takes 110 and converting 70).  Results that are not finite are formed again by a kernel of its own: within this
+// (bf16, parts of 1212 and 1839 queries over 14187 and 8463 places, 32 heads over 8 of 128: 578 us in a long run, 860 TFLOP/s; in a short
+// one, at the clock that it begins with, 691, and 750 with four waves, of which bringing in takes 110 and converting 70; a cache in bf16,
+// with four waves, 691 in a long run; in fp32, parts half as long over half as many places, 16 heads over 8, 587).  Results that are not finite are formed again by a kernel of its own: within this
 // one its registers cost long parts 2 to 7 %, which is more than the launch.
 template <class T, int DP, int NW, bool VEC, bool E4M3, bool CAREFUL>
 __device__ __forceinline__ bool cached_stretch(const CachedArgs& a, char* smem, const Stretch& x) {
@@ -559,9 +565,11 @@ __global__ void __launch_bounds__(64 * NW, 1) k_attn_cached_again(const CachedAr
 }
 
 // ---- few rows (at most 32 a key/value head): each wave takes every W-th tile of 32 keys through LDS of its own ------------------
-// Bound by memory where there is enough to read: 96 sequences of 3 thousand places on average, 8 heads of 128 in bf16, 239 us, 5.1 TB/s (a
-// large copy reaches 4.9); in 8 bits 32 sequences of 24 thousand, 4 heads, 168 us, 4.7 TB/s, where a wave's conversions and products
-// take turns with its loads (vector 31 %, LDS 31 %, matrix 12 % of the cycles).  The careful pass comes after the loop over the
+// Bound by memory where there is enough to read: 96 sequences of 3 thousand places on average, 8 heads of 128 in bf16, 234 us, 5.2 TB/s (a
+// large copy reaches 4.9); in 8 bits 32 sequences of 24 thousand, 4 heads, 163 us, 4.8 TB/s, where a wave's conversions and products
+// take turns with its loads (vector 32 %, LDS 32 %, matrix 12 % of the cycles).  fp32 queries, 32 sequences of 6 thousand, 8 heads: of 64
+// 159 us, 5.0 TB/s; of 128, whose 439 registers leave one wave a SIMD, 474, 3.3 TB/s, over 8 bits 285.  Rows of 8 bits that are no multiple
+// of 16 bytes are read byte by byte: 4 heads of 72 over 24 thousand places 929 us, of 80 152.  The careful pass comes after the loop over the
 // stretches: inside it, its registers would be spilled with theirs.
 constexpr int kCachedKeys = 32;
 template <class T, int DP, bool E4M3>
