@@ -475,8 +475,8 @@ __global__ void __launch_bounds__(256) k_cached_join(const CachedArgs a) {
 // kernels_attn.hip; in 8 bits with eight waves a workgroup, so that what a tile takes to bring in and to convert is shared by 256 rows
 // (bf16, parts of 1212 and 1839 queries over 14187 and 8463 places, 32 heads over 8 of 128: 578 us in a long run, 860 TFLOP/s; in a short
 // one, at the clock that it begins with, 691, and 750 with four waves, of which bringing in takes 110 and converting 70; a cache in bf16,
-// with four waves, 691 in a long run; in fp32, parts half as long over half as many places, 16 heads over 8, 587).  Results that are not finite are formed again by a kernel of its own: within this
-// one its registers cost long parts 2 to 7 %, which is more than the launch.
+// with four waves, 691 in a long run; in fp32, parts half as long over half as many places, 16 heads over 8, 587).  Results that are
+// not finite are formed again by a kernel of its own: within this one its registers cost long parts 2 to 7 %, which is more than the launch.
 template <class T, int DP, int NW, bool VEC, bool E4M3, bool CAREFUL>
 __device__ __forceinline__ bool cached_stretch(const CachedArgs& a, char* smem, const Stretch& x) {
   constexpr int BN = kFwdKeys<T>;

@@ -46,7 +46,7 @@ struct Deal {
   struct Part {
     int pair, t, hk, left, per;
   };
-  // with `tiles_of` pair p, whose units begin at x <= at(number) and end behind it
+  // from pair p, which has `tiles` tiles, and whose units begin at x <= at(number) and end behind it
   __host__ __device__ __forceinline__ Part within(int p, int tiles, int x, int number) const {
     const int u = units(tiles), i = (at(number) - x) % u, hk = times > 1 ? (at(number) - x) / u : head(number);
     if (!share) return Part{p, i, hk, std::min(per, total * heads - start(number)), per};
